@@ -1,0 +1,152 @@
+// kv_append.hip -- new keys and values rotated and written into a paged
+// cache, queries rotated on the way (dsim_kv_append).
+//
+// A token is (n_q_heads + 2 n_heads) rows of head_dim elements read once and
+// written once, and one row of the rotation table: 3 flops per 2 elements
+// moved, so memory bounds it.
+#include "numeric.h"
+#include "ops.h"
+
+namespace dsim {
+namespace {
+
+constexpr int kBlock = 256;
+
+template <class T, int VEC> __device__ inline vec<float, VEC> load_row(const void *p, int64_t at)
+{
+    return to_f32<T, VEC>(*reinterpret_cast<const vec<T, VEC> *>(static_cast<const T *>(p) + at));
+}
+
+template <class T, int VEC> __device__ inline void store_row(void *p, int64_t at, vec<float, VEC> x)
+{
+    *reinterpret_cast<vec<T, VEC> *>(static_cast<T *>(p) + at) = from_f32<T, VEC>(x);
+}
+
+// Where a token goes: its place in the cache (elements, without the head)
+// and its status.
+struct Place {
+    int64_t at;
+    int32_t status, pos;
+    bool skip;
+};
+
+__device__ inline Place place_of(const AppendArgs &a, int64_t t)
+{
+    Place p{0, 0, 0, false};
+    const int32_t s = a.seq[t];
+    p.pos = a.pos[t];
+    p.skip = s < 0;
+    if (p.skip) return p;
+    if (s >= a.c.n_seq) p.status |= DSIM_ST_BAD_SEQUENCE;
+    if (p.pos < 0 || (int64_t)p.pos >= (int64_t)a.c.table_width * a.c.page_size || (a.rope && p.pos >= a.n_rope))
+        p.status |= DSIM_ST_BAD_POSITION;
+    if (p.status) return p;
+    const int32_t page = a.c.block_table[s * a.c.table_stride + p.pos / a.c.page_size];
+    if (page < 0 || page >= a.c.n_pages)
+        p.status = DSIM_ST_BAD_PAGE;
+    else
+        p.at = page * a.c.page_stride + (p.pos % a.c.page_size) * a.c.slot_stride;
+    return p;
+}
+
+// T: type of the new rows; CT: of the cache; VEC: elements per load.  A
+// thread takes one chunk of VEC elements, or, where pairs (i, i + R/2) are
+// rotated, one chunk of each half.
+template <class T, class CT, int VEC> __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
+{
+    using V = vec<float, VEC>;
+    const int d = a.c.head_dim, rot = a.rot_dim;
+    const int n_rot = a.interleaved ? rot / VEC : rot / 2 / VEC;   // chunks that are rotated
+    const int per_head = n_rot + (d - rot) / VEC, per_value = d / VEC;
+    const int n_q = a.n_q_heads * per_head, n_k = a.c.n_heads * per_head, n_v = a.c.n_heads * per_value;
+    for (int64_t t = blockIdx.x; t < a.n_tok; t += gridDim.x) {
+        const Place p = place_of(a, t);
+        if (threadIdx.x == 0 && a.status) a.status[t] = p.status;
+        if (p.skip) continue;
+        const float *cs = a.rope ? a.rope + (p.status ? 0 : (int64_t)p.pos * rot) : nullptr;
+        for (int i = threadIdx.x; i < n_q + n_k + n_v; i += kBlock) {
+            if (i >= n_q + n_k) {   // a value: copied
+                if (p.status) continue;
+                const int j = i - n_q - n_k, h = j / per_value, e = j % per_value * VEC;
+                V x = load_row<T, VEC>(a.v.data, t * a.v.row_stride + h * a.v.head_stride + e);
+                if (a.c.v_scale) x /= a.c.v_scale[h];
+                store_row<CT, VEC>(a.c.v, p.at + h * a.c.head_stride + e, x);
+                continue;
+            }
+            const bool query = i < n_q;
+            const int j = query ? i : i - n_q, h = j / per_head, c = j % per_head;
+            const dsim_rows &src = query ? a.q : a.k;
+            const int64_t from = t * src.row_stride + h * src.head_stride;
+            const int64_t to = query ? t * a.q_out.row_stride + h * a.q_out.head_stride
+                                     : p.at + h * a.c.head_stride;
+            const bool turned = c < n_rot, two = turned && !a.interleaved;
+            const int e = turned ? c * VEC : rot + (c - n_rot) * VEC, e2 = e + rot / 2;
+            if (p.status) {
+                if (query) {
+                    const V nan = V(__builtin_nanf(""));
+                    store_row<T, VEC>(a.q_out.data, to + e, nan);
+                    if (two) store_row<T, VEC>(a.q_out.data, to + e2, nan);
+                }
+                continue;
+            }
+            V x = load_row<T, VEC>(src.data, from + e), y;
+            if (two) {
+                y = load_row<T, VEC>(src.data, from + e2);
+                const V cosv = *reinterpret_cast<const V *>(cs + e), sinv = *reinterpret_cast<const V *>(cs + rot / 2 + e);
+                const V z = x * cosv - y * sinv;
+                y = y * cosv + x * sinv;
+                x = z;
+            } else if (turned) {
+#pragma unroll
+                for (int k = 0; k < VEC; k += 2) {
+                    const float co = cs[(e + k) / 2], si = cs[rot / 2 + (e + k) / 2];
+                    const float z = x[k] * co - x[k + 1] * si;
+                    x[k + 1] = x[k + 1] * co + x[k] * si;
+                    x[k] = z;
+                }
+            }
+            if (query) {
+                store_row<T, VEC>(a.q_out.data, to + e, x);
+                if (two) store_row<T, VEC>(a.q_out.data, to + e2, y);
+            } else {
+                if (a.c.k_scale) {
+                    x /= a.c.k_scale[h];
+                    if (two) y /= a.c.k_scale[h];
+                }
+                store_row<CT, VEC>(a.c.k, to + e, x);
+                if (two) store_row<CT, VEC>(a.c.k, to + e2, y);
+            }
+        }
+    }
+}
+
+template <class T, class CT> void launch(const AppendArgs &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)(a.n_tok < (1 << 20) ? a.n_tok : (1 << 20)));
+    // chunks of 16 bytes of T; 4 elements where a half of the rotated part
+    // is no whole number of 8
+    if (sizeof(T) == 4 || a.rot_dim % 16)
+        hipLaunchKernelGGL((k_append<T, CT, 4>), grid, dim3(kBlock), 0, s, a);
+    else
+        hipLaunchKernelGGL((k_append<T, CT, 8>), grid, dim3(kBlock), 0, s, a);
+}
+
+}  // namespace
+
+dsim_status launch_append(const AppendArgs &a, hipStream_t s)
+{
+    if (a.dtype == DSIM_F32)
+        launch<float, float>(a, s);
+    else if (a.dtype == DSIM_F16 && a.c.dtype == DSIM_F16)
+        launch<f16, f16>(a, s);
+    else if (a.dtype == DSIM_BF16 && a.c.dtype == DSIM_BF16)
+        launch<bf16, bf16>(a, s);
+    else if (a.dtype == DSIM_F16)
+        launch<f16, e4m3>(a, s);
+    else
+        launch<bf16, e4m3>(a, s);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? DSIM_OK : hip_fail(e, "append launch");
+}
+
+}  // namespace dsim
