@@ -164,7 +164,7 @@ DSIM_API dsim_status dsim_paged_attention(const dsim_kv_cache *cache, int32_t dt
  *             logits_stride and out_stride elements apart (>= vocab, or any
  *             with n_rows = 1).  out may be logits (with the same stride);
  *             it must not overlap otherwise.
- * vocab 1..2^30, n_rows 0..2^20.
+ * vocab 1..2^30, n_rows 0..2^20, history_width below 2^30.
  */
 typedef struct {
     const void *logits;

@@ -198,7 +198,7 @@ dsim_status dsim_logit_adjust(const dsim_logits *args, void *hip_stream)
     if (a.vocab < 1 || a.vocab > (1 << 30)) return fail(DSIM_ERANGE, "vocab must be 1..2^30");
     if (a.n_rows < 0 || a.n_rows > (1 << 20)) return fail(DSIM_ERANGE, "n_rows must be 0..2^20");
     if (a.n_bias < 0 || a.n_bias > kMaxBias) return fail(DSIM_ERANGE, "n_bias must be 0..%d", kMaxBias);
-    if (a.history_width < 0) return fail(DSIM_EINVAL, "history_width must be >= 0");
+    if (a.history_width < 0 || a.history_width >= (1 << 30)) return fail(DSIM_ERANGE, "history_width must be in [0, 2^30)");
     if (a.n_rows == 0) return DSIM_OK;
     const int64_t rows = a.n_rows;
     if (!a.logits || !a.out) return fail(DSIM_EINVAL, "logits and out must not be NULL");

@@ -8,8 +8,10 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kBlock = 64 * kWaves;
-constexpr int kGrid = 512;        // two workgroups per CU
+constexpr int kGrid = 512;        // runs that the work is cut into
+constexpr int kPerSimd = 2;       // resident waves that the registers allow
 constexpr int kMinTiles = 4;      // a tile for every wave
+constexpr int kExtra = 8;         // what a context costs beside its tiles, in tiles
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // How the elements of a (query, cache) type pair go through the matrix
@@ -49,11 +51,23 @@ struct Params {
     float *lse;
     int32_t *status;
     float *part;          // partial results, 2 per workgroup
-    int4 *cut;            // per workgroup: the context its last part is cut from
+    int4 *cut;            // contexts that are cut: by context, or by the workgroup that begins it
     int64_t n_pages, page_stride, slot_stride, head_stride, table_stride, q_row, q_head, out_row, out_head;
     float scale;          // times log2 e
     int32_t n_seq, n_heads, n_q_heads, d, page_size, table_width, window;
     int32_t group, tiles_of_heads, part_heads;
+    bool by_context;      // there are at most kGrid contexts
+    uint32_t div_mul, div_shift;   // t / page_size = t * div_mul >> div_shift, 0 <= t < 2^31
+};
+
+// Page and slot of a position.
+struct Place {
+    int32_t page, slot;   // of the sequence, of the page
+    __device__ static Place of(const Params &p, int32_t t)
+    {
+        const int32_t q = (int32_t)((uint64_t)(uint32_t)t * p.div_mul >> p.div_shift);
+        return {q, t - q * p.page_size};
+    }
 };
 
 // The keys of a sequence in tiles: first tile, number of tiles (at least
@@ -61,6 +75,7 @@ struct Params {
 template <int KEYS> struct Span {
     int32_t first_key, len, first_tile, n;
     bool bad;
+    __device__ int32_t cost() const { return n > 0 ? n + kExtra : 0; }
     __device__ static Span of(const Params &p, int32_t len)
     {
         Span s{0, len, 0, 0, false};
@@ -82,16 +97,39 @@ template <int NT> struct State {
     f32x4 o[NT];
 };
 
+// a value that is the same for all lanes, in scalar registers
+__device__ inline int64_t uniform(int64_t x)
+{
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// The values of the other groups' lanes r: halves and odd and even rows of a
+// wave exchanged.
+__device__ inline vec<float, 2> other_half(float x)
+{
+    const auto y = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return {__builtin_bit_cast(float, (uint32_t)y[0]), __builtin_bit_cast(float, (uint32_t)y[1])};
+}
+
+__device__ inline vec<float, 2> other_row(float x)
+{
+    const auto y = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return {__builtin_bit_cast(float, (uint32_t)y[0]), __builtin_bit_cast(float, (uint32_t)y[1])};
+}
+
 __device__ inline float max_groups(float x)
 {
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
+    const auto y = other_half(x);
+    const auto z = other_row(fmaxf(y[0], y[1]));
+    return fmaxf(z[0], z[1]);
 }
 
 __device__ inline float sum_groups(float x)
 {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
+    const auto y = other_half(x);
+    const auto z = other_row(y[0] + y[1]);
+    return z[0] + z[1];
 }
 
 // What sums held against the maximum `from` count against the maximum `to`.
@@ -102,14 +140,21 @@ __device__ inline float rescale(float from, float to)
     return from == -HUGE_VALF ? 1.0f : __builtin_amdgcn_exp2f(from - to);
 }
 
-// The running maximum takes in the scores s (base-2 logarithms); returns them
-// as weights, 2^SHIFT for a score at the maximum.
-template <int SHIFT, int N, int NT> __device__ inline void weigh(float (&s)[N], State<NT> &st)
+// The running maximum takes in the products s; returns them as weights, 2^SHIFT
+// for one at the maximum.  scale > 0: base-2 logarithms per unit of s.  `in`:
+// bit i says whether s[i] counts (looked at unless `all`); one that does not
+// becomes the weight `least` and adds nothing to the sum.
+template <int SHIFT, int N, int NT>
+__device__ inline void weigh(float (&s)[N], float scale, bool all, uint32_t in, float least, State<NT> &st)
 {
+    if (!all) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] = in >> i & 1 ? s[i] : -HUGE_VALF;
+    }
     float top = s[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) top = fmaxf(top, s[i]);
-    top = max_groups(top);
+    top = max_groups(top) * scale;
     if (__builtin_amdgcn_ballot_w64(top > st.m) != 0) {
         const float m = fmaxf(st.m, top);
         const float f = rescale(st.m, m);
@@ -121,13 +166,17 @@ template <int SHIFT, int N, int NT> __device__ inline void weigh(float (&s)[N], 
     const float m = st.m == -HUGE_VALF ? 0.0f : st.m - SHIFT;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        s[i] = __builtin_amdgcn_exp2f(s[i] - m);
+        s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -m));
         st.l += s[i];
+    }
+    if (!all) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] = in >> i & 1 ? s[i] : least;
     }
 }
 
 // 16-bit queries; keys and values of the same type or e4m3.
-template <class T, class CT, int DP> struct Pass {
+template <class T, class CT, int DP, bool EXACT> struct Pass {
     static constexpr int kKeys = 32, kE = DP / 16, kTiles = DP / 16;
     static constexpr bool k8 = __is_same(CT, e4m3);
     static constexpr int kChunk = 16 / sizeof(CT);            // elements per 16-byte load of a key
@@ -136,13 +185,15 @@ template <class T, class CT, int DP> struct Pass {
     // fp16 ends at 2^-24: weights from 2^15 down keep a long tail of small
     // ones, which together may weigh as much as the largest
     static constexpr int kShift = __is_same(T, f16) ? 15 : 0;
+    // of a key that does not count: not 0, so that the attended value that
+    // stands in its place may be infinite
+    static constexpr float kLeast = __is_same(T, f16) ? 0x1p-24f : 0x1p-100f;
     using Query = vec<T, 8>[kSteps * kParts];
 
-    struct Data {
-        u32x4 k[2][kSteps];
-        vec<CT, kE> v[8];
-    };
+    using Keys = u32x4[2][kSteps];
+    using Values = vec<CT, kE>[8];
 
+    // negated for a negative scale
     __device__ static void load_query(const Params &p, const T *q, bool used, int g, Query &out)
     {
 #pragma unroll
@@ -150,28 +201,33 @@ template <class T, class CT, int DP> struct Pass {
 #pragma unroll
             for (int h = 0; h < kParts; ++h) {
                 const int at = (4 * s + g) * kChunk + 8 * h;
-                out[s * kParts + h] = used && at < p.d ? *reinterpret_cast<const vec<T, 8> *>(q + at) : vec<T, 8>(0);
+                vec<T, 8> x = used && at < p.d ? *reinterpret_cast<const vec<T, 8> *>(q + at) : vec<T, 8>(0);
+                out[s * kParts + h] = p.scale < 0.0f ? -x : x;
             }
     }
 
-    // off: the lane's key's place (key lane % 32 of the tile)
-    __device__ static void load(const Params &p, const CT *k, const CT *v, int64_t off, int r, int g, Data &x)
+    // rows: where the tile's keys lie
+    template <class Rows> __device__ static void load_keys(const Params &p, const Rows &rows, int r, int g, Keys &x)
     {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const CT *row = k + __shfl(off, t * 16 + r);
+            const CT *row = rows.key(t, r);
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) {
                 const int at = (4 * s + g) * kChunk;
-                x.k[t][s] = *reinterpret_cast<const u32x4 *>(row + (at < p.d ? at : 0));
+                x[t][s] = *reinterpret_cast<const u32x4 *>(row + (EXACT || at < p.d ? at : 0));
             }
         }
-        const int at = kE * r < p.d ? kE * r : 0;
+    }
+
+    template <class Rows> __device__ static void load_values(const Params &p, const Rows &rows, int r, int g, Values &x)
+    {
+        const int at = EXACT || kE * r < p.d ? kE * r : 0;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                x.v[4 * t + i] = *reinterpret_cast<const vec<CT, kE> *>(v + __shfl(off, t * 16 + 4 * g + i) + at);
+                x[4 * t + i] = *reinterpret_cast<const vec<CT, kE> *>(rows.value(t, 4 * g + i) + at);
     }
 
     __device__ static vec<T, 8> part(u32x4 x, int h, bool in)
@@ -186,13 +242,19 @@ template <class T, class CT, int DP> struct Pass {
         return in ? y : vec<T, 8>(0);
     }
 
+    // two of the four e4m3 of a word, exactly
+    template <bool HIGH> __device__ static vec<T, 2> widen2(uint32_t w)
+    {
+        if constexpr (__is_same(T, f16))
+            return __builtin_bit_cast(vec<T, 2>, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH));
+        else
+            return __builtin_bit_cast(vec<T, 2>, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HIGH));
+    }
+
     __device__ static vec<T, 8> widen8(uint32_t lo, uint32_t hi)
     {
-        vec<float, 8> f;
-        const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)lo, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)lo, true);
-        const auto c = __builtin_amdgcn_cvt_pk_f32_fp8((int)hi, false), d = __builtin_amdgcn_cvt_pk_f32_fp8((int)hi, true);
-        f[0] = a[0], f[1] = a[1], f[2] = b[0], f[3] = b[1], f[4] = c[0], f[5] = c[1], f[6] = d[0], f[7] = d[1];
-        return __builtin_convertvector(f, vec<T, 8>);
+        const vec<T, 2> a = widen2<false>(lo), b = widen2<true>(lo), c = widen2<false>(hi), d = widen2<true>(hi);
+        return {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
     }
 
     // A weight as the sum of two numbers of T: with one the output would carry
@@ -209,11 +271,11 @@ template <class T, class CT, int DP> struct Pass {
             for (int i = 0; i < 8; ++i) {
                 const uint32_t bits = __builtin_bit_cast(uint32_t, s[i]);
                 rest[i] = fmaxf(s[i] - __builtin_bit_cast(float, bits & 0xffff0000u), 0x1p-126f);
-                if (i % 2)
-                    w[i / 2] |= bits & 0xffff0000u;
-                else
-                    w[i / 2] = bits >> 16;
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                w[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, s[2 * i + 1]), __builtin_bit_cast(uint32_t, s[2 * i]),
+                                             0x07060302);
             hi = __builtin_bit_cast(vec<T, 8>, w);
         } else {
 #pragma unroll
@@ -228,11 +290,9 @@ template <class T, class CT, int DP> struct Pass {
         lo = __builtin_convertvector(rest, vec<T, 8>);
     }
 
-    // valid: bit 4 t + i of the lane's keys; all: every key of the tile counts
-    __device__ static void compute(const Params &p, Data &x, const Query &q, float scale, int g, uint32_t valid,
-                                   bool all, State<kTiles> &st)
+    // products of the lane's keys 16 t + 4 g + i with query head r
+    __device__ static void scores(const Params &p, const Keys &x, const Query &q, int g, float (&s)[8])
     {
-        float s[8];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             f32x4 acc = {0, 0, 0, 0};
@@ -240,24 +300,20 @@ template <class T, class CT, int DP> struct Pass {
             for (int i = 0; i < kSteps; ++i)
 #pragma unroll
                 for (int h = 0; h < kParts; ++h)
-                    acc = Mfma<T>::mul(part(x.k[t][i], h, (4 * i + g) * kChunk < p.d), q[i * kParts + h], acc);
+                    acc = Mfma<T>::mul(part(x[t][i], h, EXACT || (4 * i + g) * kChunk < p.d), q[i * kParts + h], acc);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[4 * t + i] = acc[i] * scale;
+            for (int i = 0; i < 4; ++i) s[4 * t + i] = acc[i];
         }
-        if (!all) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const bool in = valid >> i & 1;
-                s[i] = in ? s[i] : -HUGE_VALF;
-                x.v[i] = in ? x.v[i] : vec<CT, kE>(0);   // what lies there may be infinite or NaN
-            }
-        }
-        weigh<kShift>(s, st);
+    }
+
+    // the values of those keys, times their weights
+    __device__ static void outputs(const Values &x, const float (&s)[8], State<kTiles> &st)
+    {
         vec<T, 8> hi, lo;
         split(s, hi, lo);
         vec<T, kE> row[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) row[i] = to_t(x.v[i]);
+        for (int i = 0; i < 8; ++i) row[i] = to_t(x[i]);
 #pragma unroll
         for (int e = 0; e < kE; ++e) {
             vec<T, 8> a;
@@ -275,9 +331,11 @@ template <class T, class CT, int DP> struct Pass {
             vec<T, kE> y;
 #pragma unroll
             for (int i = 0; i < kE / 4; ++i) {
-                const vec<T, 8> z = widen8(w[i], 0);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) y[4 * i + j] = z[j];
+                const vec<T, 2> a = widen2<false>(w[i]), b = widen2<true>(w[i]);
+                y[4 * i] = a[0];
+                y[4 * i + 1] = a[1];
+                y[4 * i + 2] = b[0];
+                y[4 * i + 3] = b[1];
             }
             return y;
         } else {
@@ -290,78 +348,144 @@ template <class T, class CT, int DP> struct Pass {
 };
 
 // fp32: the same with products of four reduction indices, 16 keys a tile.
-template <int DP> struct Pass<float, float, DP> {
+template <int DP, bool EXACT> struct Pass<float, float, DP, EXACT> {
     static constexpr int kKeys = 16, kTiles = DP / 16, kSteps = DP / 16, kQuads = DP / 64, kShift = 0;
     using Query = f32x4[kSteps];
 
-    struct Data {
-        f32x4 k[kSteps];
-        f32x4 v[4][kQuads];
-    };
+    using Keys = f32x4[kSteps];
+    using Values = f32x4[4][kQuads];
+    static constexpr float kLeast = 0x1p-100f;
 
     __device__ static void load_query(const Params &p, const float *q, bool used, int g, Query &out)
     {
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             const int at = (4 * s + g) * 4;
-            out[s] = used && at < p.d ? *reinterpret_cast<const f32x4 *>(q + at) : f32x4{0, 0, 0, 0};
+            const f32x4 x = used && at < p.d ? *reinterpret_cast<const f32x4 *>(q + at) : f32x4{0, 0, 0, 0};
+            out[s] = p.scale < 0.0f ? -x : x;
         }
     }
 
-    __device__ static void load(const Params &p, const float *k, const float *v, int64_t off, int r, int g, Data &x)
+    template <class Rows> __device__ static void load_keys(const Params &p, const Rows &rows, int r, int g, Keys &x)
     {
-        const float *row = k + __shfl(off, r);
+        const float *row = rows.key(0, r);
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             const int at = (4 * s + g) * 4;
-            x.k[s] = *reinterpret_cast<const f32x4 *>(row + (at < p.d ? at : 0));
+            x[s] = *reinterpret_cast<const f32x4 *>(row + (EXACT || at < p.d ? at : 0));
         }
+    }
+
+    template <class Rows> __device__ static void load_values(const Params &p, const Rows &rows, int r, int g, Values &x)
+    {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float *val = v + __shfl(off, 4 * g + i);
+            const float *val = rows.value(0, 4 * g + i);
 #pragma unroll
             for (int j = 0; j < kQuads; ++j) {
                 const int at = 64 * j + 4 * r;
-                x.v[i][j] = *reinterpret_cast<const f32x4 *>(val + (at < p.d ? at : 0));
+                x[i][j] = *reinterpret_cast<const f32x4 *>(val + (EXACT || at < p.d ? at : 0));
             }
         }
     }
 
-    __device__ static void compute(const Params &p, Data &x, const Query &q, float scale, int g, uint32_t valid,
-                                   bool all, State<kTiles> &st)
+    __device__ static void scores(const Params &p, const Keys &x, const Query &q, int g, float (&s)[4])
     {
         f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            const bool in = (4 * i + g) * 4 < p.d;
+            const bool inside = EXACT || (4 * i + g) * 4 < p.d;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(in ? x.k[i][e] : 0.0f, q[i][e], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(inside ? x[i][e] : 0.0f, q[i][e], acc, 0, 0, 0);
         }
-        float s[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = acc[i] * scale;
-        if (!all) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bool in = valid >> i & 1;
-                s[i] = in ? s[i] : -HUGE_VALF;
-#pragma unroll
-                for (int j = 0; j < kQuads; ++j) x.v[i][j] = in ? x.v[i][j] : f32x4{0, 0, 0, 0};
-            }
-        }
-        weigh<kShift>(s, st);
+        for (int i = 0; i < 4; ++i) s[i] = acc[i];
+    }
+
+    __device__ static void outputs(const Values &x, const float (&s)[4], State<kTiles> &st)
+    {
 #pragma unroll
         for (int j = 0; j < kQuads; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    st.o[4 * j + e] =
-                        __builtin_amdgcn_mfma_f32_16x16x4f32(x.v[i][j][e], s[i], st.o[4 * j + e], 0, 0, 0);
+                    st.o[4 * j + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i][j][e], s[i], st.o[4 * j + e], 0, 0, 0);
     }
 
     __device__ static int dim(int g, int i, int e) { return 64 * (e / 4) + (4 * g + i) * 4 + e % 4; }
+};
+
+// Where the keys of a tile lie, in two steps so that the table's entries can
+// be on their way while an earlier tile is worked on: `fetch` reads the table
+// for the tile that begins at k0, `resolve` checks the pages and sets the
+// addresses.  A key outside the attended ones stands for the nearest of them,
+// so nothing else is read, neither of the table nor of the cache.
+// Pages of a multiple of 16 slots: 16 keys lie in one page, whose number and
+// address are the same for all lanes.
+template <class CT, int KEYS, bool WHOLE> struct Rows {
+    static constexpr int kN = KEYS / 16;
+    int32_t page[kN], slot[kN], low[kN], high[kN];
+    const CT *k[kN], *v[kN];
+    uint32_t slot_bytes;
+
+    __device__ void fetch(const Params &p, const int32_t *row, int32_t k0, int32_t first_key, int32_t len, int lane)
+    {
+#pragma unroll
+        for (int t = 0; t < kN; ++t) {
+            const int32_t key = min(max(k0 + 16 * t, first_key & ~15), (len - 1) & ~15);
+            const Place at = Place::of(p, key);
+            page[t] = row[at.page];
+            slot[t] = at.slot;
+            low[t] = max(first_key - key, 0);
+            high[t] = min(len - 1 - key, 15);
+        }
+    }
+    __device__ bool resolve(const Params &p, const CT *kb, const CT *vb)
+    {
+        slot_bytes = (uint32_t)p.slot_stride * (uint32_t)sizeof(CT);
+        bool ok = true;
+#pragma unroll
+        for (int t = 0; t < kN; ++t) {
+            ok &= page[t] >= 0 && page[t] < p.n_pages;
+            const int64_t off = page[t] * p.page_stride + slot[t] * p.slot_stride;
+            k[t] = kb + off;
+            v[t] = vb + off;
+        }
+        return ok;
+    }
+    __device__ const CT *at(const CT *base, int t, int i) const
+    {
+        return reinterpret_cast<const CT *>(reinterpret_cast<const char *>(base) +
+                                            __umul24(min(max(i, low[t]), high[t]), slot_bytes));
+    }
+    __device__ const CT *key(int t, int i) const { return at(k[t], t, i); }
+    __device__ const CT *value(int t, int i) const { return at(v[t], t, i); }
+};
+
+// Any page size: lane l holds the place of key l % KEYS.
+template <class CT, int KEYS> struct Rows<CT, KEYS, false> {
+    int32_t page, slot;
+    int64_t off;
+    const CT *kb, *vb;
+
+    __device__ void fetch(const Params &p, const int32_t *row, int32_t k0, int32_t first_key, int32_t len, int lane)
+    {
+        const Place at = Place::of(p, min(max(k0 + lane % KEYS, first_key), len - 1));
+        page = row[at.page];
+        slot = at.slot;
+    }
+    __device__ bool resolve(const Params &p, const CT *kbase, const CT *vbase)
+    {
+        const bool ok = page >= 0 && page < p.n_pages;
+        off = page * p.page_stride + slot * p.slot_stride;
+        kb = kbase;
+        vb = vbase;
+        return __builtin_amdgcn_ballot_w64(!ok) == 0;
+    }
+    __device__ const CT *key(int t, int i) const { return kb + __shfl(off, 16 * t + i); }
+    __device__ const CT *value(int t, int i) const { return vb + __shfl(off, 16 * t + i); }
 };
 
 // A result row's elements: out = x / l, or what a row without keys or with an
@@ -381,34 +505,44 @@ __device__ inline void write_lse(const Params &p, int b, int head, float m, floa
             bad ? __builtin_nanf("") : empty ? -HUGE_VALF : (m + (__builtin_log2f(l) - SHIFT)) * kLn2;
 }
 
-// m, l of 16 heads and 16 x d outputs
-__device__ inline float *part_of(const Params &p, int64_t slot)
-{
-    return p.part + slot * ((int64_t)p.part_heads * (p.d + 2));
-}
+// A part of a context: d outputs of each head, then the heads' maxima and
+// sums; 16-byte aligned.
+__host__ __device__ inline int64_t part_size(int heads, int d) { return (int64_t)heads * d + (2 * heads + 3) / 4 * 4; }
 
-// The tiles of all (sequence, cache head, tile of 16 query heads) are laid
-// end to end and cut into equal runs, one per workgroup; a workgroup's waves
+struct Part {
+    float *o, *m, *l;
+    __device__ static Part of(const Params &p, int64_t slot)
+    {
+        float *o = p.part + slot * part_size(p.part_heads, p.d), *m = o + p.part_heads * p.d;
+        return {o, m, m + p.part_heads};
+    }
+};
+
+// The tiles of all contexts -- (sequence, cache head, tile of 16 query heads)
+// -- are laid end to end, each context behind kExtra that stand for its
+// beginning and end, and cut into equal runs, one per workgroup; a workgroup's waves
 // take the tiles of each context in turn and are joined in shared memory.  A
 // context that lies in one run is finished here; the parts of the others go
 // to the workspace (slot 0: a context begun by an earlier workgroup, slot 1:
 // one that a later workgroup goes on with) for k_join.
-template <class T, class CT, int DP> __global__ __launch_bounds__(kBlock) void k_attend(Params p)
+template <class T, class CT, int DP, bool WHOLE, bool EXACT>
+__global__ __launch_bounds__(kBlock, kPerSimd) void k_attend(Params p)
 {
-    using P = Pass<T, CT, DP>;
+    using P = Pass<T, CT, DP, EXACT>;
     constexpr int kKeys = P::kKeys, NT = P::kTiles, kPad = DP + 4;
     __shared__ float s_o[kWaves][kTileHeads][kPad];
     __shared__ float s_m[kWaves][kTileHeads], s_l[kWaves][kTileHeads];
     __shared__ int64_t s_sum[kWaves];
     __shared__ int32_t s_seq, s_bad;
     __shared__ int64_t s_at;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int units = p.n_heads * p.tiles_of_heads;   // contexts per sequence
 
     // this workgroup's run: tiles counted per thread, summed over the block
     const int per = (p.n_seq + kBlock - 1) / kBlock, lo = tid * per, hi = min(p.n_seq, lo + per);
     int64_t mine = 0;
-    for (int b = lo; b < hi; ++b) mine += Span<kKeys>::of(p, p.seq_len[b]).n;
+    for (int b = lo; b < hi; ++b) mine += Span<kKeys>::of(p, p.seq_len[b]).cost();
     int64_t incl = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -424,11 +558,11 @@ template <class T, class CT, int DP> __global__ __launch_bounds__(kBlock) void k
         if (w < wave) before += s_sum[w];
         total += s_sum[w];
     }
-    total *= units;
-    const int64_t even = (total + gridDim.x - 1) / gridDim.x, run = even > kMinTiles ? even : kMinTiles;
+    total = uniform(total) * units;
+    const int64_t even = (total + gridDim.x - 1) / gridDim.x, run = even > kExtra + kMinTiles ? even : kExtra + kMinTiles;
     const int64_t begin = blockIdx.x * run;
     if (begin >= total) {
-        if (tid == 0) p.cut[blockIdx.x] = make_int4(0, 0, 0, 0);
+        if (tid == 0 && !p.by_context) p.cut[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
     }
     const int64_t end = begin + run < total ? begin + run : total;
@@ -436,7 +570,7 @@ template <class T, class CT, int DP> __global__ __launch_bounds__(kBlock) void k
     if (begin >= excl && begin < excl + mine * units) {
         int64_t at = excl;
         for (int b = lo; b < hi; ++b) {
-            const int64_t n = (int64_t)Span<kKeys>::of(p, p.seq_len[b]).n * units;
+            const int64_t n = (int64_t)Span<kKeys>::of(p, p.seq_len[b]).cost() * units;
             if (begin < at + n) {
                 s_seq = b;
                 s_at = begin - at;
@@ -446,19 +580,23 @@ template <class T, class CT, int DP> __global__ __launch_bounds__(kBlock) void k
         }
     }
     __syncthreads();
-    int b = s_seq;
-    int64_t at = s_at, left = end - begin;
+    int b = __builtin_amdgcn_readfirstlane(s_seq);
+    int64_t at = uniform(s_at), left = end - begin;
     int4 cut = make_int4(0, 0, 0, 0);
 
     while (left > 0) {
         const Span<kKeys> sp = Span<kKeys>::of(p, p.seq_len[b]);
-        if (at >= (int64_t)sp.n * units) {   // (also a sequence that is left alone)
+        const int cost = sp.cost();
+        if (at >= (int64_t)cost * units) {   // (also a sequence that is left alone)
             ++b;
             at = 0;
             continue;
         }
-        const int unit = (int)(at / sp.n), t0 = (int)(at % sp.n);
-        const int n = (int)(sp.n - t0 < left ? sp.n - t0 : left);
+        const int unit = (int)(at / cost), c0 = (int)(at % cost), c1 = (int)(cost - c0 < left ? cost : c0 + left);
+        at += c1 - c0;
+        left -= c1 - c0;
+        const int t0 = max(c0 - kExtra, 0), n = max(c1 - kExtra, 0) - t0;
+        if (n == 0) continue;   // the next run begins the context
         const int kv = unit / p.tiles_of_heads, hb = unit % p.tiles_of_heads * kTileHeads;
         const int heads = min(kTileHeads, p.group - hb), q0 = kv * p.group + hb;
         const bool whole = n == sp.n;
@@ -476,32 +614,57 @@ template <class T, class CT, int DP> __global__ __launch_bounds__(kBlock) void k
             typename P::Query q;
             P::load_query(p, static_cast<const T *>(p.q) + b * p.q_row + (q0 + (r < heads ? r : 0)) * p.q_head,
                           r < heads, g, q);
-            const float scale = p.scale * (p.k_scale ? p.k_scale[kv] : 1.0f);
+            // (not 0, which times the -inf of a key that does not count were NaN)
+            const float scale = fmaxf(fabsf(p.scale) * (p.k_scale ? p.k_scale[kv] : 1.0f), 0x1p-120f);
             const CT *kb = static_cast<const CT *>(p.k) + kv * p.head_stride;
             const CT *vb = static_cast<const CT *>(p.v) + kv * p.head_stride;
-            bool wrong = false;
-            for (int t = t0 + wave; t < t0 + n; t += kWaves) {
-                const int k0 = (sp.first_tile + t) * kKeys;
-                // keys outside [first_key, len) stand for the nearest inside
-                const int key = min(max(k0 + lane % kKeys, sp.first_key), sp.len - 1);
-                int32_t page = row[key / p.page_size];
-                if (page < 0 || page >= p.n_pages) {
-                    wrong = true;
-                    page = 0;
+            // The next tile's keys are on their way as soon as the scores are
+            // known, its values as soon as the outputs are; the table's
+            // entries a tile ahead of both.
+            typename P::Keys keys;
+            typename P::Values values;
+            Rows<CT, kKeys, WHOLE> rows;
+            const int last = t0 + n;
+            auto fetch = [&](int t) {
+                rows.fetch(p, row, (sp.first_tile + min(t, last - 1)) * kKeys, sp.first_key, sp.len, lane);
+            };
+            bool ok = true;
+            int t = t0 + wave;
+            if (t < last) {
+                fetch(t);
+                ok = rows.resolve(p, kb, vb);
+                if (ok) {
+                    P::load_keys(p, rows, r, g, keys);
+                    P::load_values(p, rows, r, g, values);
+                    fetch(t + kWaves);
                 }
-                const int64_t off = page * p.page_stride + key % p.page_size * p.slot_stride;
-                if (__builtin_amdgcn_ballot_w64(wrong) != 0) break;
-                typename P::Data x;
-                P::load(p, kb, vb, off, r, g, x);
-                const bool all = k0 >= sp.first_key && sp.len - k0 >= kKeys;
-                uint32_t valid = 0;
-#pragma unroll
-                for (int i = 0; i < kKeys / 4; ++i) {
-                    const int j = k0 + i / 4 * 16 + 4 * g + i % 4;
-                    if (j >= sp.first_key && j < sp.len) valid |= 1u << i;
-                }
-                P::compute(p, x, q, scale, g, valid, all, st);
             }
+            while (ok && t < last) {
+                const int next = t + kWaves;
+                if (next < last) ok = rows.resolve(p, kb, vb);
+                const bool more = ok && next < last;
+                const int k0 = (sp.first_tile + t) * kKeys;
+                const bool all = k0 >= sp.first_key && sp.len - k0 >= kKeys;
+                uint32_t in = 0;
+                if (!all) {
+#pragma unroll
+                    for (int i = 0; i < kKeys / 4; ++i) {
+                        const int j = k0 + i / 4 * 16 + 4 * g + i % 4;
+                        if (j >= sp.first_key && j < sp.len) in |= 1u << i;
+                    }
+                }
+                float s[kKeys / 4];
+                P::scores(p, keys, q, g, s);
+                if (more) P::load_keys(p, rows, r, g, keys);
+                weigh<P::kShift>(s, scale, all, in, P::kLeast, st);
+                P::outputs(values, s, st);
+                if (more) {
+                    P::load_values(p, rows, r, g, values);
+                    fetch(next + kWaves);
+                }
+                t = next;
+            }
+            const bool wrong = !ok;
             if (wrong) s_bad = DSIM_ST_BAD_PAGE;
         }
 
@@ -524,7 +687,7 @@ template <class T, class CT, int DP> __global__ __launch_bounds__(kBlock) void k
         }
         __syncthreads();
         const int32_t bad = s_bad;
-        float *part = part_of(p, 2 * blockIdx.x + (t0 == 0 ? 1 : 0));
+        const Part part = Part::of(p, 2 * blockIdx.x + (t0 == 0 ? 1 : 0));
         const float vs = p.v_scale ? p.v_scale[kv] : 1.0f;
         for (int i = tid; i < heads * p.d; i += kBlock) {
             const int h = i / p.d, d = i % p.d;
@@ -542,69 +705,93 @@ template <class T, class CT, int DP> __global__ __launch_bounds__(kBlock) void k
                 write_row<T>(p, b, q0 + h, d, o, sum, sp.len == 0, bad);
                 if (d == 0) write_lse<P::kShift>(p, b, q0 + h, m, sum, sp.len == 0, bad);
             } else {
-                part[2 * p.part_heads + h * p.d + d] = o;
+                part.o[h * p.d + d] = o;
                 if (d == 0) {
-                    part[h] = m;
-                    part[p.part_heads + h] = bad ? -1.0f : sum;   // (a sum is never negative)
+                    part.m[h] = m;
+                    part.l[h] = bad ? -1.0f : sum;   // (a sum is never negative)
                 }
             }
         }
-        if (whole) {
-            if (tid == 0 && p.status) p.status[b] = bad;
-        } else if (t0 == 0) {
-            // this part, then the runs of the workgroups behind, the last
-            // possibly short
-            cut = make_int4(1 + (int)((sp.n - n + run - 1) / run), b, q0, heads);
+        if (whole && tid == 0 && p.status) p.status[b] = bad;
+        if (t0 == 0) {
+            // parts: this one, then the runs of the workgroups behind, the
+            // last possibly short; 0 if nothing is cut off
+            cut = make_int4(whole ? 0 : 1 + (int)((sp.n - n + run - 1) / run), b, q0, (int)blockIdx.x);
+            if (p.by_context && tid == 0) p.cut[b * units + unit] = cut;
         }
-        at += n;
-        left -= n;
         __syncthreads();
     }
-    if (tid == 0) p.cut[blockIdx.x] = cut;
+    if (tid == 0 && !p.by_context) p.cut[blockIdx.x] = cut;
 }
 
-// Joins the parts of the contexts that workgroups begun and others went on
-// with: workgroup (w, h) takes head h of the one begun by workgroup w.
-template <class T, int SHIFT> __global__ __launch_bounds__(kBlock) void k_join(Params p)
+// Joins the parts of the contexts that are cut.  W waves of a workgroup take
+// one head of a context; their threads are `ways` rows of head_dim / 4, row w
+// taking four elements each of the parts w, w + ways, ...  The first of
+// those are on their way before the weights they get are known.
+template <class T, int SHIFT, int W> __global__ __launch_bounds__(kBlock) void k_join(Params p)
 {
-    __shared__ float s_w[kGrid];
-    __shared__ float s_red[kWaves];
-    const int w0 = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int4 cut = p.cut[w0];
-    const int n = cut.x, b = cut.y, q0 = cut.z;
-    if (n == 0 || h >= cut.w) return;
-    auto part = [&](int i) { return part_of(p, i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)); };
+    constexpr int kThreads = 64 * W, kHeads = kBlock / kThreads, kAhead = 8;
+    __shared__ float s_m[kWaves], s_l[kWaves];
+    __shared__ int s_wrong[kWaves];
+    __shared__ f32x4 s_o[kBlock];
+    const int4 cut = p.cut[blockIdx.x];
+    const int n = cut.x, b = cut.y, q0 = cut.z, w0 = cut.w;
+    const int tid = threadIdx.x % kThreads, lane = tid & 63, wave = threadIdx.x / 64, mine = threadIdx.x / kThreads;
+    const int h = blockIdx.y * kHeads + mine, first = wave / W * W;
+    // (nobody begins the context of a row that is left alone)
+    if (p.by_context && p.seq_len[blockIdx.x / (p.n_heads * p.tiles_of_heads)] < 0) return;
+    if (n == 0) return;
+    const bool used = h < p.part_heads && q0 + h < (q0 / p.group + 1) * p.group;   // (a last tile may have fewer heads)
+    auto part = [&](int i) { return Part::of(p, i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)); };
+    const int quads = p.d / 4, ways = kThreads / quads, way = tid / quads, d4 = tid - way * quads;
+    const int count = used && way < ways ? n : 0;
+    auto output = [&](int i) { return *reinterpret_cast<const f32x4 *>(part(i).o + h * p.d + 4 * d4); };
+    f32x4 ahead[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+        if (way + j * ways < count) ahead[j] = output(way + j * ways);
+
     float m = -HUGE_VALF;
     int wrong = 0;
-    for (int i = tid; i < n; i += kBlock) {
-        m = fmaxf(m, part(i)[h]);
-        wrong |= part(i)[p.part_heads + h] < 0.0f;
+    for (int i = tid; used && i < n; i += kThreads) {
+        m = fmaxf(m, part(i).m[h]);
+        wrong |= part(i).l[h] < 0.0f;
     }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-    if (lane == 0) s_red[wave] = m;
-    wrong = __syncthreads_or(wrong);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, s_red[w]);
-    __syncthreads();
-    float l = 0.0f;
-    for (int i = tid; i < n; i += kBlock) {
-        const float f = rescale(part(i)[h], m);
-        s_w[i] = f;
-        l += f * part(i)[p.part_heads + h];
+    wrong = __builtin_amdgcn_ballot_w64(wrong) != 0;
+    if (W > 1) {
+        if (lane == 0) {
+            s_m[wave] = m;
+            s_wrong[wave] = wrong;
+        }
+        __syncthreads();
+        for (int w = first; w < first + W; ++w) {
+            m = fmaxf(m, s_m[w]);
+            wrong |= s_wrong[w];
+        }
     }
+    float l = 0.0f;
+    for (int i = tid; used && i < n; i += kThreads) l += rescale(part(i).m[h], m) * part(i).l[h];
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o);
-    if (lane == 0) s_red[wave] = l;
-    __syncthreads();
-    l = 0.0f;
+    f32x4 o = {0, 0, 0, 0};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) l += s_red[w];
+    for (int j = 0; j < kAhead; ++j)
+        if (way + j * ways < count) o += rescale(part(way + j * ways).m[h], m) * ahead[j];
+#pragma unroll 4
+    for (int i = way + kAhead * ways; i < count; i += ways) o += rescale(part(i).m[h], m) * output(i);
+    s_o[threadIdx.x] = o;
+    if (lane == 0) s_l[wave] = l;
+    __syncthreads();
+    if (!used) return;
+    l = 0.0f;
+    for (int w = first; w < first + W; ++w) l += s_l[w];
     const int32_t bad = wrong ? DSIM_ST_BAD_PAGE : 0;
-    for (int d = tid; d < p.d; d += kBlock) {
-        float o = 0.0f;
-        for (int i = 0; i < n; ++i) o += s_w[i] * part(i)[2 * p.part_heads + h * p.d + d];
-        write_row<T>(p, b, q0 + h, d, o, l, false, bad);
+    if (tid < quads) {
+        for (int w = 1; w < ways; ++w) o += s_o[mine * kThreads + w * quads + tid];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) write_row<T>(p, b, q0 + h, 4 * tid + k, o[k], l, false, bad);
     }
     if (tid == 0) {
         write_lse<SHIFT>(p, b, q0 + h, m, l, false, bad);
@@ -612,19 +799,33 @@ template <class T, int SHIFT> __global__ __launch_bounds__(kBlock) void k_join(P
     }
 }
 
-template <class T, class CT> dsim_status launch(const Params &p, hipStream_t s)
+template <class T, class CT, int DP> dsim_status launch(const Params &p, hipStream_t s)
 {
-    if (p.d <= 64)
-        hipLaunchKernelGGL((k_attend<T, CT, 64>), dim3(kGrid), dim3(kBlock), 0, s, p);
-    else if (p.d <= 128)
-        hipLaunchKernelGGL((k_attend<T, CT, 128>), dim3(kGrid), dim3(kBlock), 0, s, p);
+    // 16 slots of a page at offsets of 24-bit products
+    const bool whole = p.page_size % 16 == 0 && p.slot_stride * (int64_t)sizeof(CT) < 1 << 24;
+    if (whole && p.d == DP)
+        hipLaunchKernelGGL((k_attend<T, CT, DP, true, true>), dim3(kGrid), dim3(kBlock), 0, s, p);
+    else if (whole)
+        hipLaunchKernelGGL((k_attend<T, CT, DP, true, false>), dim3(kGrid), dim3(kBlock), 0, s, p);
     else
-        hipLaunchKernelGGL((k_attend<T, CT, 256>), dim3(kGrid), dim3(kBlock), 0, s, p);
+        hipLaunchKernelGGL((k_attend<T, CT, DP, false, false>), dim3(kGrid), dim3(kBlock), 0, s, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return hip_fail(e, "paged attention launch");
-    hipLaunchKernelGGL((k_join<T, Pass<T, CT, 64>::kShift>), dim3(kGrid, (unsigned)p.part_heads), dim3(kBlock), 0, s, p);
+    // a context is cut at most once per run: of few there may be many parts
+    constexpr int kShift = Pass<T, CT, DP, true>::kShift;
+    const int64_t contexts = (int64_t)p.n_seq * p.n_heads * p.tiles_of_heads;
+    const unsigned x = (unsigned)(contexts < kGrid ? contexts : kGrid);
+    if (contexts * 16 <= kGrid)
+        hipLaunchKernelGGL((k_join<T, kShift, 4>), dim3(x, (unsigned)p.part_heads), dim3(kBlock), 0, s, p);
+    else
+        hipLaunchKernelGGL((k_join<T, kShift, 1>), dim3(x, (unsigned)(p.part_heads + 3) / 4), dim3(kBlock), 0, s, p);
     e = hipGetLastError();
     return e == hipSuccess ? DSIM_OK : hip_fail(e, "paged attention join launch");
+}
+
+template <class T, class CT> dsim_status launch(const Params &p, hipStream_t s)
+{
+    return p.d <= 64 ? launch<T, CT, 64>(p, s) : p.d <= 128 ? launch<T, CT, 128>(p, s) : launch<T, CT, 256>(p, s);
 }
 
 }  // namespace
@@ -632,7 +833,7 @@ template <class T, class CT> dsim_status launch(const Params &p, hipStream_t s)
 size_t attend_workspace(int32_t n_q_heads, int32_t n_heads, int32_t head_dim)
 {
     const int group = n_q_heads / n_heads, heads = group < kTileHeads ? group : kTileHeads;
-    return (size_t)kGrid * (sizeof(int4) + 2 * (size_t)heads * (size_t)(head_dim + 2) * sizeof(float));
+    return (size_t)kGrid * (sizeof(int4) + 2 * (size_t)part_size(heads, head_dim) * sizeof(float));
 }
 
 dsim_status launch_attend(const AttendArgs &a, hipStream_t s)
@@ -666,10 +867,16 @@ dsim_status launch_attend(const AttendArgs &a, hipStream_t s)
     p.d = a.c.head_dim;
     p.page_size = a.c.page_size;
     p.table_width = a.c.table_width;
+    // ceil(2^(31 + l) / n), l = ceil(log2 n): exact for t < 2^31
+    int l = 0;
+    while ((1 << l) < p.page_size) ++l;
+    p.div_shift = 31 + l;
+    p.div_mul = (uint32_t)((((uint64_t)1 << p.div_shift) + p.page_size - 1) / p.page_size);
     p.window = a.window;
     p.group = a.n_q_heads / a.c.n_heads;
     p.tiles_of_heads = (p.group + kTileHeads - 1) / kTileHeads;
     p.part_heads = p.group < kTileHeads ? p.group : kTileHeads;
+    p.by_context = (int64_t)p.n_seq * p.n_heads * p.tiles_of_heads <= kGrid;
     if (a.dtype == DSIM_F32) return launch<float, float>(p, s);
     if (a.dtype == DSIM_F16) return a.c.dtype == DSIM_E4M3 ? launch<f16, e4m3>(p, s) : launch<f16, f16>(p, s);
     return a.c.dtype == DSIM_E4M3 ? launch<bf16, e4m3>(p, s) : launch<bf16, bf16>(p, s);
