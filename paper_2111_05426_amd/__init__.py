@@ -7,7 +7,9 @@ The simulation runs in the HIP kernels of ``libdsim.so`` behind the C ABI in
 ``paper_2111_05426_amd.frontend`` binds the library's front end, which
 turns programs written op by op into op tables (mixed abstract/concrete
 interpretation, host C++), ``paper_2111_05426_amd.programs``
-writes example programs for it, and ``paper_2111_05426_amd.calibrate`` fits the
-empirical MatMul cost on the GPU it runs on.
+writes example programs for it, ``paper_2111_05426_amd.ops`` binds the
+operators of a single-token step (``include/dsim_ops.h``: paged cache append,
+paged attention, logit adjustment), and ``paper_2111_05426_amd.calibrate`` fits
+the empirical costs on the GPU it runs on.
 """
-__all__ = ["dsim", "workloads", "frontend", "programs", "calibrate"]
+__all__ = ["dsim", "workloads", "frontend", "programs", "ops", "calibrate"]

@@ -1,19 +1,24 @@
-"""Build libdsim.so (HIP, gfx950) in-tree with hipcc.
+"""Build libdsim.so (HIP, gfx950) and the operators' Python binding in-tree.
 
     python -m paper_2111_05426_amd.build
 
-Every translation unit is compiled as HIP for gfx950 with FMA contraction
-off (the simulator's fp64 results must not depend on contraction choices)
-and packed-fp32 instructions disabled.
+Every translation unit of the library is compiled as HIP for gfx950 with FMA
+contraction off (the simulator's fp64 results must not depend on contraction
+choices) and packed-fp32 instructions disabled.  The binding (_ops.so) is
+host C++ against torch's headers, linked to libdsim.so beside it.
 """
 import glob
 import os
 import subprocess
 import sys
+import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdsim.so")
+BINDING = os.path.join(HERE, "_ops.so")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -26,14 +31,46 @@ def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.cpp")) + glob.glob(os.path.join(CSRC, "*.hip")))
 
 
-def build(verbose=False):
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    tmp = LIB + ".tmp"
-    cmd = [hipcc] + FLAGS + ["-x", "hip"] + sources() + ["-o", tmp]
+def binding_sources():
+    return sorted(glob.glob(os.path.join(HERE, "binding", "*.cpp")))
+
+
+def _run(cmd, verbose):
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)
-    os.replace(tmp, LIB)
+
+
+def _build_library(hipcc, verbose):
+    # one compiler a source, at most as many at once as MAX_JOBS allows
+    jobs = max(1, min(8, int(os.environ.get("MAX_JOBS") or os.cpu_count() or 1)))
+    flags = [f for f in FLAGS if f != "-shared"]
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(jobs) as pool:
+        objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in sources()]
+        list(pool.map(lambda so: _run([hipcc] + flags + ["-x", "hip", "-c", so[0], "-o", so[1]], verbose),
+                      zip(sources(), objects)))
+        _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objects + ["-o", LIB + ".tmp"], verbose)
+    os.replace(LIB + ".tmp", LIB)
+
+
+def _build_binding(verbose):
+    import torch
+    root = os.path.dirname(os.path.abspath(torch.__file__))
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
+           "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", "-I", INCLUDE, "-isystem", os.path.join(root, "include"),
+           "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+           "-isystem", os.path.join(rocm, "include"), "-isystem", sysconfig.get_paths()["include"]]
+    cmd += binding_sources() + ["-o", BINDING + ".tmp", "-L", HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN",
+                                "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
+                                "-lc10_hip"]
+    _run(cmd, verbose)
+    os.replace(BINDING + ".tmp", BINDING)
+
+
+def build(verbose=False):
+    _build_library(os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), verbose)
+    _build_binding(verbose)
     return LIB
 
 
