@@ -13,7 +13,7 @@
 namespace dsim {
 namespace {
 
-constexpr uint32_t kPrompt = 1u << 31, kBiased = 1u << 30, kMade = kBiased - 1;
+constexpr uint32_t kPrompt = 1u << 31, kMade = kPrompt - 1;
 
 // N elements at any element's alignment
 template <class T, int N> __device__ inline vec<T, N> load_any(const T *p)
@@ -24,15 +24,31 @@ template <class T, int N> __device__ inline vec<T, N> load_any(const T *p)
 }
 template <class T, int N> __device__ inline void store_any(T *p, vec<T, N> x) { __builtin_memcpy(p, &x, sizeof x); }
 
-// SLICE tokens per workgroup of BLOCK threads.
+// tokens i .. i + 3 of n
+__device__ inline void tokens(const int32_t *h, int32_t i, int32_t n, int32_t (&t)[4])
+{
+    if (i < n - 3) {
+        const vec<int32_t, 4> v = load_any<int32_t, 4>(h + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) t[k] = v[k];
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) t[k] = i < n - k ? h[i + k] : -1;
+    }
+}
+
+// SLICE tokens per workgroup of BLOCK threads.  Every load that needs no
+// other's result is on its way at once: the logits, the first tokens of the
+// history (as many as its rows are wide, whatever the row's length) and the
+// first biases; one wait for memory, not four in a row, is what a workgroup
+// takes beside its share of the bandwidth.
 template <class T, int SLICE, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void k_logits(dsim_logits a, int32_t slices)
 {
-    constexpr int N = 16 / sizeof(T), kLoads = SLICE / (N * BLOCK);
+    constexpr int N = 16 / sizeof(T), kLoads = SLICE / (N * BLOCK), kAhead = 1;
     static_assert(SLICE % (N * BLOCK) == 0, "whole vectors");
-    extern __shared__ uint32_t s_mem[];
-    uint32_t *s_count = s_mem;                                  // generated tokens, kPrompt, kBiased
-    int32_t *s_bias = reinterpret_cast<int32_t *>(s_mem + SLICE);   // the last bias of a token that has one
+    // first the history's counts, then the biases' places
+    __shared__ uint32_t s_of[SLICE];
     const int64_t b = blockIdx.x / slices;
     const int tid = threadIdx.x;
     const T *in = static_cast<const T *>(a.logits) + b * a.logits_stride;
@@ -51,82 +67,123 @@ __global__ __launch_bounds__(BLOCK) void k_logits(dsim_logits a, int32_t slices)
 #pragma unroll
             for (int k = 0; k < N; ++k) x[j][k] = t + k >= 0 && t + k < a.vocab ? in[t + k] : (T)0.0f;
     }
-    if (counting || biased) {
+    const int32_t *h = a.history + b * a.history_stride;
+    const int32_t *ids = a.bias_id + b * a.n_bias;
+    int32_t token[kAhead][4], id = -1, len = 0, prompt = 0;
+    float rep = 1.0f, freq = 0.0f, pres = 0.0f;
+    if (counting) {
 #pragma unroll
-        for (int i = 0; i < SLICE / (4 * BLOCK); ++i)
-            reinterpret_cast<u32x4 *>(s_count)[i * BLOCK + tid] = u32x4{0, 0, 0, 0};
-        __syncthreads();
-        if (counting) {
-            const int32_t len = min(max(a.history_len[b], 0), a.history_width);
-            const int32_t prompt = a.prompt_len ? min(max(a.prompt_len[b], 0), len) : 0;
-            const int32_t *h = a.history + b * a.history_stride;
-#pragma unroll 4
-            for (int i = tid; i < len; i += BLOCK) {
-                const int32_t id = h[i];
-                const uint32_t at = (uint32_t)id - (uint32_t)lo;
-                if (id >= 0 && id < a.vocab && at < (uint32_t)SLICE) {
-                    if (i < prompt)
-                        atomicOr(&s_count[at], kPrompt);
-                    else
-                        atomicAdd(&s_count[at], 1u);
-                }
-            }
-        }
-        if (biased) {
-            const int32_t *ids = a.bias_id + b * a.n_bias;
-            for (int i = tid; i < a.n_bias; i += BLOCK) {
-                const uint32_t at = (uint32_t)ids[i] - (uint32_t)lo;
-                if (ids[i] >= 0 && ids[i] < a.vocab && at < (uint32_t)SLICE) {
-                    atomicOr(&s_count[at], kBiased);
-                    s_bias[at] = -1;
-                }
-            }
-            __syncthreads();
-            for (int i = tid; i < a.n_bias; i += BLOCK) {
-                const uint32_t at = (uint32_t)ids[i] - (uint32_t)lo;
-                if (ids[i] >= 0 && ids[i] < a.vocab && at < (uint32_t)SLICE) atomicMax(&s_bias[at], i);
-            }
-        }
-        __syncthreads();
+        for (int i = 0; i < kAhead; ++i) tokens(h, (i * BLOCK + tid) * 4, a.history_width, token[i]);
+        len = min(max(a.history_len[b], 0), a.history_width);
+        prompt = a.prompt_len ? min(max(a.prompt_len[b], 0), len) : 0;
+        if (a.repetition) rep = a.repetition[b];
+        if (a.frequency) freq = a.frequency[b];
+        if (a.presence) pres = a.presence[b];
     }
-    const float rep = a.repetition ? a.repetition[b] : 1.0f, freq = a.frequency ? a.frequency[b] : 0.0f,
-                pres = a.presence ? a.presence[b] : 0.0f;
-    const uint32_t *mask = a.mask ? a.mask + b * a.mask_stride : nullptr;
-    const int32_t last = (a.vocab - 1) / 32;
+    if (biased && tid < a.n_bias) id = ids[tid];
+    // the mask's bits of a vector's tokens
+    uint32_t bits[kLoads];
+    if (a.mask) {
+        const uint32_t *mask = a.mask + b * a.mask_stride;
+        const int32_t last = (a.vocab - 1) / 32;
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-        const int i = (j * BLOCK + tid) * N;
-        const int32_t t = lo + i;
-        if (t + N <= 0 || t >= a.vocab) continue;
-        vec<float, N> y = to_f32<T, N>(x[j]);
-        if (counting || biased) {
+        for (int j = 0; j < kLoads; ++j) {
+            const int32_t t = lo + (j * BLOCK + tid) * N, first = max(min(t, a.vocab - 1), 0);
+            // (the second word is the one after the first unless `first`
+            // begins a word: then no bit of it counts)
+            const uint64_t w = (uint64_t)mask[min((first + 31) / 32, last)] << 32 | mask[first / 32];
+            bits[j] = (uint32_t)(w >> (first % 32)) << (t < 0 ? -t : 0);
+        }
+    }
+
+    auto clear = [&]() {
+#pragma unroll
+        for (int i = 0; i < SLICE / (4 * BLOCK); ++i) reinterpret_cast<u32x4 *>(s_of)[i * BLOCK + tid] = u32x4{0, 0, 0, 0};
+    };
+    // a token's place in the slice, if it has one
+    auto place = [&](int32_t t, uint32_t &at) {
+        at = (uint32_t)t - (uint32_t)lo;
+        return t >= 0 && t < a.vocab && at < (uint32_t)SLICE;
+    };
+    float y[kLoads][N];   // (single registers: whole vectors get copied at every branch)
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+        for (int k = 0; k < N; ++k) y[j][k] = (float)x[j][k];
+
+    if (counting) {
+        clear();
+        __syncthreads();
+        auto count = [&](int i, int32_t t) {
+            uint32_t at;
+            if (i < len && place(t, at)) {
+                if (i < prompt)
+                    atomicOr(&s_of[at], kPrompt);
+                else
+                    atomicAdd(&s_of[at], 1u);
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) count((i * BLOCK + tid) * 4 + k, token[i][k]);
+#pragma unroll 4
+        for (int i = (kAhead * BLOCK + tid) * 4; i < len; i += BLOCK * 4) {
+            int32_t more[4];
+            tokens(h, i, len, more);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) count(i + k, more[k]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j)
 #pragma unroll
             for (int q = 0; q < N / 4; ++q) {
-                const u32x4 c4 = reinterpret_cast<const u32x4 *>(s_count + i)[q];
+                const u32x4 c4 = reinterpret_cast<const u32x4 *>(s_of + (j * BLOCK + tid) * N)[q];
                 if ((c4[0] | c4[1] | c4[2] | c4[3]) == 0) continue;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const uint32_t c = c4[k], made = c & kMade;
-                    float v = y[4 * q + k];
-                    if (c & ~kBiased) {
+                    const uint32_t made = c4[k] & kMade;
+                    float v = y[j][4 * q + k];
+                    if (c4[k]) {
                         v = v > 0.0f ? v / rep : v * rep;
                         v = v - (freq * (float)made + (made ? pres : 0.0f));
                     }
-                    if (c & kBiased) v = v + a.bias[b * a.n_bias + s_bias[i + 4 * q + k]];
-                    y[4 * q + k] = v;
+                    y[j][4 * q + k] = v;
                 }
             }
-        }
-        if (mask) {
-            const int32_t first = max(t, 0);
-            const uint64_t w = (uint64_t)mask[min((first + 31) / 32, last)] << 32 | mask[first / 32];
-            // bits of tokens first.., the second word being the one after the
-            // first unless `first` begins a word (then no bit of it counts)
-            const uint32_t bits = (uint32_t)(w >> (first % 32)) << (first - t);
+    }
+    if (biased) {
+        if (counting) __syncthreads();
+        clear();
+        __syncthreads();
+        uint32_t at;
+        if (place(id, at)) atomicMax(&s_of[at], (uint32_t)tid + 1);
+        for (int i = BLOCK + tid; i < a.n_bias; i += BLOCK)
+            if (place(ids[i], at)) atomicMax(&s_of[at], (uint32_t)i + 1);
+        __syncthreads();
 #pragma unroll
-            for (int k = 0; k < N; ++k) y[k] = bits >> k & 1 ? y[k] : -HUGE_VALF;
+        for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+            for (int q = 0; q < N / 4; ++q) {
+                const u32x4 i4 = reinterpret_cast<const u32x4 *>(s_of + (j * BLOCK + tid) * N)[q];
+                if ((i4[0] | i4[1] | i4[2] | i4[3]) == 0) continue;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (i4[k]) y[j][4 * q + k] = y[j][4 * q + k] + a.bias[b * a.n_bias + i4[k] - 1];
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+        const int32_t t = lo + (j * BLOCK + tid) * N;
+        if (a.mask) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) y[j][k] = bits[j] >> k & 1 ? y[j][k] : -HUGE_VALF;
         }
-        const vec<T, N> z = from_f32<T, N>(y);
+        vec<float, N> w;
+#pragma unroll
+        for (int k = 0; k < N; ++k) w[k] = y[j][k];
+        const vec<T, N> z = from_f32<T, N>(w);
         if (t >= 0 && t + N <= a.vocab)
             store_any<T, N>(out + t, z);
         else
@@ -142,8 +199,7 @@ template <class T, int SLICE, int BLOCK> dsim_status launch(const dsim_logits &a
     const int32_t slices = (int32_t)(((int64_t)a.vocab + N - 1 + SLICE - 1) / SLICE);   // (a row may begin inside a vector)
     const int64_t blocks = a.n_rows * slices;
     if (blocks >= ((int64_t)1 << 32) / BLOCK) return fail(DSIM_ERANGE, "logits: n_rows * vocab is too large for one call");
-    const size_t shared = (size_t)SLICE * 4 * (a.n_bias > 0 ? 2 : 1);
-    hipLaunchKernelGGL((k_logits<T, SLICE, BLOCK>), dim3((unsigned)blocks), dim3(BLOCK), shared, s, a, slices);
+    hipLaunchKernelGGL((k_logits<T, SLICE, BLOCK>), dim3((unsigned)blocks), dim3(BLOCK), 0, s, a, slices);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? DSIM_OK : hip_fail(e, "logits launch");
 }
