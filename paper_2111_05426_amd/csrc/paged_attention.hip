@@ -293,17 +293,19 @@ template <class T, class CT, int DP, bool EXACT> struct Pass {
     // products of the lane's keys 16 t + 4 g + i with query head r
     __device__ static void scores(const Params &p, const Keys &x, const Query &q, int g, float (&s)[8])
     {
+        // (products that need one another's result stand apart)
+        f32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            f32x4 acc = {0, 0, 0, 0};
+        for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i)
+            for (int h = 0; h < kParts; ++h)
 #pragma unroll
-                for (int h = 0; h < kParts; ++h)
-                    acc = Mfma<T>::mul(part(x[t][i], h, EXACT || (4 * i + g) * kChunk < p.d), q[i * kParts + h], acc);
+                for (int t = 0; t < 2; ++t)
+                    acc[t] = Mfma<T>::mul(part(x[t][i], h, EXACT || (4 * i + g) * kChunk < p.d), q[i * kParts + h], acc[t]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[4 * t + i] = acc[i];
-        }
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[4 * t + i] = acc[t][i];
     }
 
     // the values of those keys, times their weights
@@ -314,13 +316,18 @@ template <class T, class CT, int DP, bool EXACT> struct Pass {
         vec<T, kE> row[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) row[i] = to_t(x[i]);
+        constexpr int kTogether = 4;
 #pragma unroll
-        for (int e = 0; e < kE; ++e) {
-            vec<T, 8> a;
+        for (int e0 = 0; e0 < kE; e0 += kTogether) {
+            vec<T, 8> a[kTogether];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) a[i] = row[i][e];
-            st.o[e] = Mfma<T>::mul(a, hi, st.o[e]);
-            st.o[e] = Mfma<T>::mul(a, lo, st.o[e]);
+            for (int e = 0; e < kTogether; ++e)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) a[e][i] = row[i][e0 + e];
+#pragma unroll
+            for (int e = 0; e < kTogether; ++e) st.o[e0 + e] = Mfma<T>::mul(a[e], hi, st.o[e0 + e]);
+#pragma unroll
+            for (int e = 0; e < kTogether; ++e) st.o[e0 + e] = Mfma<T>::mul(a[e], lo, st.o[e0 + e]);
         }
     }
 
@@ -391,26 +398,27 @@ template <int DP, bool EXACT> struct Pass<float, float, DP, EXACT> {
 
     __device__ static void scores(const Params &p, const Keys &x, const Query &q, int g, float (&s)[4])
     {
-        f32x4 acc = {0, 0, 0, 0};
+        // four sums, so that no product waits for the one before
+        f32x4 acc[4] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             const bool inside = EXACT || (4 * i + g) * 4 < p.d;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(inside ? x[i][e] : 0.0f, q[i][e], acc, 0, 0, 0);
+                acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(inside ? x[i][e] : 0.0f, q[i][e], acc[e], 0, 0, 0);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = acc[i];
+        for (int i = 0; i < 4; ++i) s[i] = (acc[0][i] + acc[1][i]) + (acc[2][i] + acc[3][i]);
     }
 
     __device__ static void outputs(const Values &x, const float (&s)[4], State<kTiles> &st)
     {
 #pragma unroll
-        for (int j = 0; j < kQuads; ++j)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int j = 0; j < kQuads; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int e = 0; e < 4; ++e)
                     st.o[4 * j + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i][j][e], s[i], st.o[4 * j + e], 0, 0, 0);
     }
 
