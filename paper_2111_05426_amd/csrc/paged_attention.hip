@@ -8,8 +8,11 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kBlock = 64 * kWaves;
-constexpr int kGrid = 512;        // runs that the work is cut into
-constexpr int kPerSimd = 2;       // resident waves that the registers allow
+constexpr int kCus = 256;
+// Workgroups per CU by the padded head dimension and the size of the cache's
+// elements, all resident at once.
+constexpr int per_cu(int dp, int size) { return dp <= 128 || size == 1 ? 2 : 1; }
+constexpr int kMaxGrid = kCus * 2;
 constexpr int kMinTiles = 4;      // a tile for every wave
 constexpr int kExtra = 8;         // what a context costs beside its tiles, in tiles
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -56,7 +59,8 @@ struct Params {
     float scale;          // times log2 e
     int32_t n_seq, n_heads, n_q_heads, d, page_size, table_width, window;
     int32_t group, tiles_of_heads, part_heads;
-    bool by_context;      // there are at most kGrid contexts
+    int32_t grid;         // runs that the work is cut into
+    bool by_context;      // there are at most as many contexts
     uint32_t div_mul, div_shift;   // t / page_size = t * div_mul >> div_shift, 0 <= t < 2^31
 };
 
@@ -496,13 +500,14 @@ template <class CT, int KEYS> struct Rows<CT, KEYS, false> {
     __device__ const CT *value(int t, int i) const { return vb + __shfl(off, 16 * t + i); }
 };
 
-// A result row's elements: out = x / l, or what a row without keys or with an
-// error has.
+// Four elements of a result row: out = x / l, or what a row without keys or
+// with an error has.
 template <class T>
-__device__ inline void write_row(const Params &p, int b, int head, int d, float x, float l, bool empty, int32_t bad)
+__device__ inline void write_row(const Params &p, int b, int head, int d, f32x4 x, float l, bool empty, int32_t bad)
 {
-    const float y = bad ? __builtin_nanf("") : empty ? 0.0f : x / l;
-    static_cast<T *>(p.out)[b * p.out_row + head * p.out_head + d] = (T)y;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = bad ? __builtin_nanf("") : empty ? 0.0f : x[k] / l;
+    *reinterpret_cast<vec<T, 4> *>(static_cast<T *>(p.out) + b * p.out_row + head * p.out_head + d) = from_f32<T, 4>(x);
 }
 
 template <int SHIFT>
@@ -534,14 +539,14 @@ struct Part {
 // to the workspace (slot 0: a context begun by an earlier workgroup, slot 1:
 // one that a later workgroup goes on with) for k_join.
 template <class T, class CT, int DP, bool WHOLE, bool EXACT>
-__global__ __launch_bounds__(kBlock, kPerSimd) void k_attend(Params p)
+__global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Params p)
 {
     using P = Pass<T, CT, DP, EXACT>;
     constexpr int kKeys = P::kKeys, NT = P::kTiles, kPad = DP + 4;
     __shared__ float s_o[kWaves][kTileHeads][kPad];
-    __shared__ float s_m[kWaves][kTileHeads], s_l[kWaves][kTileHeads];
+    __shared__ float s_m[kWaves][kTileHeads], s_l[kWaves][kTileHeads], s_top[kTileHeads];
     __shared__ int64_t s_sum[kWaves];
-    __shared__ int32_t s_seq, s_bad;
+    __shared__ int32_t s_seq, s_len, s_bad[2];
     __shared__ int64_t s_at;
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -558,7 +563,7 @@ __global__ __launch_bounds__(kBlock, kPerSimd) void k_attend(Params p)
         if (lane >= o) incl += x;
     }
     if (lane == 63) s_sum[wave] = incl;
-    if (tid == 0) s_seq = -1;
+    if (tid < 2) s_bad[tid] = 0;
     __syncthreads();
     int64_t total = 0, before = 0;
 #pragma unroll
@@ -567,7 +572,8 @@ __global__ __launch_bounds__(kBlock, kPerSimd) void k_attend(Params p)
         total += s_sum[w];
     }
     total = uniform(total) * units;
-    const int64_t even = (total + gridDim.x - 1) / gridDim.x, run = even > kExtra + kMinTiles ? even : kExtra + kMinTiles;
+    constexpr int kRuns = kCus * per_cu(DP, sizeof(CT));   // the grid
+    const int64_t even = (total + kRuns - 1) / kRuns, run = even > kExtra + kMinTiles ? even : kExtra + kMinTiles;
     const int64_t begin = blockIdx.x * run;
     if (begin >= total) {
         if (tid == 0 && !p.by_context) p.cut[blockIdx.x] = make_int4(0, 0, 0, 0);
@@ -578,9 +584,11 @@ __global__ __launch_bounds__(kBlock, kPerSimd) void k_attend(Params p)
     if (begin >= excl && begin < excl + mine * units) {
         int64_t at = excl;
         for (int b = lo; b < hi; ++b) {
-            const int64_t n = (int64_t)Span<kKeys>::of(p, p.seq_len[b]).cost() * units;
+            const int32_t len = p.seq_len[b];
+            const int64_t n = (int64_t)Span<kKeys>::of(p, len).cost() * units;
             if (begin < at + n) {
                 s_seq = b;
+                s_len = len;
                 s_at = begin - at;
                 break;
             }
@@ -589,23 +597,29 @@ __global__ __launch_bounds__(kBlock, kPerSimd) void k_attend(Params p)
     }
     __syncthreads();
     int b = __builtin_amdgcn_readfirstlane(s_seq);
-    int64_t at = uniform(s_at), left = end - begin;
-    int4 cut = make_int4(0, 0, 0, 0);
-
-    while (left > 0) {
-        const Span<kKeys> sp = Span<kKeys>::of(p, p.seq_len[b]);
+    Span<kKeys> sp = Span<kKeys>::of(p, __builtin_amdgcn_readfirstlane(s_len));
+    int64_t left = end - begin;
+    int unit, c0;
+    {
+        const int64_t at = uniform(s_at);
         const int cost = sp.cost();
-        if (at >= (int64_t)cost * units) {   // (also a sequence that is left alone)
-            ++b;
-            at = 0;
-            continue;
+        unit = at >> 32 == 0 ? (int)((uint32_t)at / (uint32_t)cost) : (int)(at / cost);   // (64 bits take 0.3 us)
+        c0 = (int)(at - (int64_t)unit * cost);
+    }
+    int4 cut = make_int4(0, 0, 0, 0);
+    int turn = 0;
+
+    for (; left > 0; ++unit, c0 = 0) {
+        while (unit == units || sp.n == 0) {   // the next sequence (one may be left alone)
+            sp = Span<kKeys>::of(p, p.seq_len[++b]);
+            unit = 0;
         }
-        const int unit = (int)(at / cost), c0 = (int)(at % cost), c1 = (int)(cost - c0 < left ? cost : c0 + left);
-        at += c1 - c0;
+        const int cost = sp.cost(), c1 = (int)(cost - c0 < left ? cost : c0 + left);
         left -= c1 - c0;
         const int t0 = max(c0 - kExtra, 0), n = max(c1 - kExtra, 0) - t0;
         if (n == 0) continue;   // the next run begins the context
-        const int kv = unit / p.tiles_of_heads, hb = unit % p.tiles_of_heads * kTileHeads;
+        const int kv = p.tiles_of_heads == 1 ? unit : unit / p.tiles_of_heads;
+        const int hb = (unit - kv * p.tiles_of_heads) * kTileHeads;
         const int heads = min(kTileHeads, p.group - hb), q0 = kv * p.group + hb;
         const bool whole = n == sp.n;
         const int32_t *row = p.table + b * p.table_stride;
@@ -615,9 +629,6 @@ __global__ __launch_bounds__(kBlock, kPerSimd) void k_attend(Params p)
         st.l = 0.0f;
 #pragma unroll
         for (int e = 0; e < NT; ++e) st.o[e] = f32x4{0, 0, 0, 0};
-        if (tid == 0) s_bad = sp.bad ? DSIM_ST_BAD_POSITION : 0;
-        __syncthreads();
-
         if (sp.len > 0) {
             typename P::Query q;
             P::load_query(p, static_cast<const T *>(p.q) + b * p.q_row + (q0 + (r < heads ? r : 0)) * p.q_head,
@@ -672,16 +683,14 @@ __global__ __launch_bounds__(kBlock, kPerSimd) void k_attend(Params p)
                 }
                 t = next;
             }
-            const bool wrong = !ok;
-            if (wrong) s_bad = DSIM_ST_BAD_PAGE;
+            if (!ok) s_bad[turn] = DSIM_ST_BAD_PAGE;
         }
 
-        // join the waves
+        // Join the waves.  Two barriers a context: what the next one writes
+        // before its first is not read after this one's second, but for
+        // s_bad, which takes turns.
         const float l = sum_groups(st.l);
-        if (g == 0) {
-            s_m[wave][r] = st.m;
-            s_l[wave][r] = l;
-        }
+        if (g == 0) s_m[wave][r] = st.m;
         __syncthreads();
         float top = s_m[0][r];
 #pragma unroll
@@ -689,33 +698,40 @@ __global__ __launch_bounds__(kBlock, kPerSimd) void k_attend(Params p)
         const float f = rescale(st.m, top);
         if (r < heads) {
 #pragma unroll
-            for (int e = 0; e < NT; ++e)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s_o[wave][r][P::dim(g, i, e)] = st.o[e][i] * f;
+                for (int e = 0; e < NT; e += 4)
+                    *reinterpret_cast<f32x4 *>(&s_o[wave][r][P::dim(g, i, e)]) =
+                        f32x4{st.o[e][i], st.o[e + 1][i], st.o[e + 2][i], st.o[e + 3][i]} * f;
         }
+        if (g == 0) {
+            s_l[wave][r] = l * f;
+            if (wave == 0) s_top[r] = top;
+        }
+        if (tid == 0) s_bad[turn ^ 1] = 0;
         __syncthreads();
-        const int32_t bad = s_bad;
+        const int32_t bad = sp.bad ? DSIM_ST_BAD_POSITION : s_bad[turn];
+        turn ^= 1;
         const Part part = Part::of(p, 2 * blockIdx.x + (t0 == 0 ? 1 : 0));
         const float vs = p.v_scale ? p.v_scale[kv] : 1.0f;
-        for (int i = tid; i < heads * p.d; i += kBlock) {
-            const int h = i / p.d, d = i % p.d;
-            float m = s_m[0][h];
+        const int quads = EXACT ? DP / 4 : p.d / 4;
+        for (int i = tid; i < heads * quads; i += kBlock) {
+            const int h = i / quads, d = 4 * (i - h * quads);
+            float sum = s_l[0][h];
+            f32x4 o = *reinterpret_cast<const f32x4 *>(&s_o[0][h][d]);
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_m[w][h]);
-            float sum = 0.0f, o = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                sum += s_l[w][h] * rescale(s_m[w][h], m);
-                o += s_o[w][h][d];
+            for (int w = 1; w < kWaves; ++w) {
+                sum += s_l[w][h];
+                o += *reinterpret_cast<const f32x4 *>(&s_o[w][h][d]);
             }
             o *= vs;
             if (whole) {
                 write_row<T>(p, b, q0 + h, d, o, sum, sp.len == 0, bad);
-                if (d == 0) write_lse<P::kShift>(p, b, q0 + h, m, sum, sp.len == 0, bad);
+                if (d == 0) write_lse<P::kShift>(p, b, q0 + h, s_top[h], sum, sp.len == 0, bad);
             } else {
-                part.o[h * p.d + d] = o;
+                *reinterpret_cast<f32x4 *>(part.o + h * p.d + d) = o;
                 if (d == 0) {
-                    part.m[h] = m;
+                    part.m[h] = s_top[h];
                     part.l[h] = bad ? -1.0f : sum;   // (a sum is never negative)
                 }
             }
@@ -727,15 +743,15 @@ __global__ __launch_bounds__(kBlock, kPerSimd) void k_attend(Params p)
             cut = make_int4(whole ? 0 : 1 + (int)((sp.n - n + run - 1) / run), b, q0, (int)blockIdx.x);
             if (p.by_context && tid == 0) p.cut[b * units + unit] = cut;
         }
-        __syncthreads();
     }
     if (tid == 0 && !p.by_context) p.cut[blockIdx.x] = cut;
 }
 
-// Joins the parts of the contexts that are cut.  W waves of a workgroup take
-// one head of a context; their threads are `ways` rows of head_dim / 4, row w
-// taking four elements each of the parts w, w + ways, ...  The first of
-// those are on their way before the weights they get are known.
+// Joins the parts of the contexts that are cut.  W = 1: a wave takes a head
+// of a context; W = 4: four waves take a quarter of its outputs.  Their
+// threads are `ways` rows, row w taking four elements each of the parts w,
+// w + ways, ...  The first of those are on their way before the weights they
+// get are known.
 template <class T, int SHIFT, int W> __global__ __launch_bounds__(kBlock) void k_join(Params p)
 {
     constexpr int kThreads = 64 * W, kHeads = kBlock / kThreads, kAhead = 8;
@@ -751,9 +767,10 @@ template <class T, int SHIFT, int W> __global__ __launch_bounds__(kBlock) void k
     if (n == 0) return;
     const bool used = h < p.part_heads && q0 + h < (q0 / p.group + 1) * p.group;   // (a last tile may have fewer heads)
     auto part = [&](int i) { return Part::of(p, i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)); };
-    const int quads = p.d / 4, ways = kThreads / quads, way = tid / quads, d4 = tid - way * quads;
+    const int quads = p.d / 4 / W, ways = kThreads / quads, way = tid / quads;
+    const int d0 = 4 * (tid - way * quads + (int)blockIdx.z * quads);
     const int count = used && way < ways ? n : 0;
-    auto output = [&](int i) { return *reinterpret_cast<const f32x4 *>(part(i).o + h * p.d + 4 * d4); };
+    auto output = [&](int i) { return *reinterpret_cast<const f32x4 *>(part(i).o + h * p.d + d0); };
     f32x4 ahead[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j)
@@ -798,40 +815,42 @@ template <class T, int SHIFT, int W> __global__ __launch_bounds__(kBlock) void k
     const int32_t bad = wrong ? DSIM_ST_BAD_PAGE : 0;
     if (tid < quads) {
         for (int w = 1; w < ways; ++w) o += s_o[mine * kThreads + w * quads + tid];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) write_row<T>(p, b, q0 + h, 4 * tid + k, o[k], l, false, bad);
+        write_row<T>(p, b, q0 + h, d0, o, l, false, bad);
     }
-    if (tid == 0) {
+    if (tid == 0 && blockIdx.z == 0) {
         write_lse<SHIFT>(p, b, q0 + h, m, l, false, bad);
         if (p.status) p.status[b] = bad;
     }
 }
 
-template <class T, class CT, int DP> dsim_status launch(const Params &p, hipStream_t s)
+template <class T, class CT, int DP> dsim_status launch(Params &p, hipStream_t s)
 {
+    const int64_t contexts = (int64_t)p.n_seq * p.n_heads * p.tiles_of_heads;
+    p.grid = kCus * per_cu(DP, sizeof(CT));
+    p.by_context = contexts <= p.grid;
+    const dim3 grid((unsigned)p.grid), block(kBlock);
     // 16 slots of a page at offsets of 24-bit products
     const bool whole = p.page_size % 16 == 0 && p.slot_stride * (int64_t)sizeof(CT) < 1 << 24;
     if (whole && p.d == DP)
-        hipLaunchKernelGGL((k_attend<T, CT, DP, true, true>), dim3(kGrid), dim3(kBlock), 0, s, p);
+        hipLaunchKernelGGL((k_attend<T, CT, DP, true, true>), grid, block, 0, s, p);
     else if (whole)
-        hipLaunchKernelGGL((k_attend<T, CT, DP, true, false>), dim3(kGrid), dim3(kBlock), 0, s, p);
+        hipLaunchKernelGGL((k_attend<T, CT, DP, true, false>), grid, block, 0, s, p);
     else
-        hipLaunchKernelGGL((k_attend<T, CT, DP, false, false>), dim3(kGrid), dim3(kBlock), 0, s, p);
+        hipLaunchKernelGGL((k_attend<T, CT, DP, false, false>), grid, block, 0, s, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return hip_fail(e, "paged attention launch");
-    // a context is cut at most once per run: of few there may be many parts
+    // few contexts have many parts each
     constexpr int kShift = Pass<T, CT, DP, true>::kShift;
-    const int64_t contexts = (int64_t)p.n_seq * p.n_heads * p.tiles_of_heads;
-    const unsigned x = (unsigned)(contexts < kGrid ? contexts : kGrid);
-    if (contexts * 16 <= kGrid)
-        hipLaunchKernelGGL((k_join<T, kShift, 4>), dim3(x, (unsigned)p.part_heads), dim3(kBlock), 0, s, p);
+    const unsigned x = (unsigned)(p.by_context ? contexts : p.grid), heads = (unsigned)p.part_heads;
+    if (contexts * 32 <= p.grid)
+        hipLaunchKernelGGL((k_join<T, kShift, 4>), dim3(x, heads, 4), block, 0, s, p);
     else
-        hipLaunchKernelGGL((k_join<T, kShift, 1>), dim3(x, (unsigned)(p.part_heads + 3) / 4), dim3(kBlock), 0, s, p);
+        hipLaunchKernelGGL((k_join<T, kShift, 1>), dim3(x, (heads + 3) / 4), block, 0, s, p);
     e = hipGetLastError();
     return e == hipSuccess ? DSIM_OK : hip_fail(e, "paged attention join launch");
 }
 
-template <class T, class CT> dsim_status launch(const Params &p, hipStream_t s)
+template <class T, class CT> dsim_status launch(Params &p, hipStream_t s)
 {
     return p.d <= 64 ? launch<T, CT, 64>(p, s) : p.d <= 128 ? launch<T, CT, 128>(p, s) : launch<T, CT, 256>(p, s);
 }
@@ -841,7 +860,7 @@ template <class T, class CT> dsim_status launch(const Params &p, hipStream_t s)
 size_t attend_workspace(int32_t n_q_heads, int32_t n_heads, int32_t head_dim)
 {
     const int group = n_q_heads / n_heads, heads = group < kTileHeads ? group : kTileHeads;
-    return (size_t)kGrid * (sizeof(int4) + 2 * (size_t)part_size(heads, head_dim) * sizeof(float));
+    return (size_t)kMaxGrid * (sizeof(int4) + 2 * (size_t)part_size(heads, head_dim) * sizeof(float));
 }
 
 dsim_status launch_attend(const AttendArgs &a, hipStream_t s)
@@ -858,7 +877,7 @@ dsim_status launch_attend(const AttendArgs &a, hipStream_t s)
     p.lse = a.lse;
     p.status = a.status;
     p.cut = static_cast<int4 *>(a.ws);
-    p.part = reinterpret_cast<float *>(p.cut + kGrid);
+    p.part = reinterpret_cast<float *>(p.cut + kMaxGrid);
     p.n_pages = a.c.n_pages;
     p.page_stride = a.c.page_stride;
     p.slot_stride = a.c.slot_stride;
@@ -884,7 +903,6 @@ dsim_status launch_attend(const AttendArgs &a, hipStream_t s)
     p.group = a.n_q_heads / a.c.n_heads;
     p.tiles_of_heads = (p.group + kTileHeads - 1) / kTileHeads;
     p.part_heads = p.group < kTileHeads ? p.group : kTileHeads;
-    p.by_context = (int64_t)p.n_seq * p.n_heads * p.tiles_of_heads <= kGrid;
     if (a.dtype == DSIM_F32) return launch<float, float>(p, s);
     if (a.dtype == DSIM_F16) return a.c.dtype == DSIM_E4M3 ? launch<f16, e4m3>(p, s) : launch<f16, f16>(p, s);
     return a.c.dtype == DSIM_E4M3 ? launch<bf16, e4m3>(p, s) : launch<bf16, bf16>(p, s);
