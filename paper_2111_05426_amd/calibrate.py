@@ -1,4 +1,5 @@
-"""Empirical MatMul cost for the simulator's device model.
+"""Empirical costs for the simulator's device model: MatMul, and the
+memory-bound operators of a single-token step.
 
 The paper's simulator gives matrix multiplications an empirical cost: a
 linear regression in the sizes of the input tensors, fitted on timings of
@@ -36,6 +37,22 @@ Every coefficient must be >= 0 for the device model.  The result is a
 The products are the measured op, not part of the simulator: they run
 through the framework's matmul (hipBLASLt), as the op a simulated program
 would call.
+
+Every other compute op of a simulated program is priced by the roofline
+launch + max(flops / F, bytes / B).  What a step that answers one token runs
+beside its products moves far more bytes than it computes, so two constants
+of the device model price it, launch_s and mem_bytes_per_s:
+
+    python -m paper_2111_05426_amd.calibrate --op decode [--dtype fp16] [--reps 20] [--out FILE]
+
+times the framework's own operators of such a step (ops.py: the cache append,
+the paged attention and the logit adjustment) over batches and contexts of
+the GPT models that the simulator studies and fits
+
+    t = launch_s + bytes / mem_bytes_per_s
+
+by non-negative least squares on relative error, bytes being what the op
+cannot do without.
 """
 import argparse
 import json
@@ -182,8 +199,96 @@ def measure(shapes=SHAPES, dtype="fp16", reps=20, warmup=3):
     return rows
 
 
+# (batch, context, heads, head size) of single-token steps: GPT-2-small's
+# heads and an eighth of GPT-3's (a tensor rank's share), one request to a
+# full batch, short answers to contexts beyond GPT-3's
+DECODE_SHAPES = [(1, 128, 12, 64), (1, 4096, 12, 64), (16, 1024, 12, 64), (64, 1024, 12, 64), (256, 512, 12, 64),
+                 (1, 2048, 12, 128), (1, 65536, 12, 128), (32, 2048, 12, 128), (128, 2048, 12, 128),
+                 (512, 1024, 12, 128)]
+DECODE_VOCAB, DECODE_PAGE = 50257, 16
+
+
+def fit_roofline(nbytes, seconds):
+    """Non-negative least squares of t = launch + bytes / rate on relative
+    error.  Returns ((launch, rate), worst relative error)."""
+    (launch, _, per_byte), worst = fit(np.zeros(len(nbytes)), nbytes, seconds)
+    return (launch, 1.0 / per_byte if per_byte > 0.0 else float("inf")), worst
+
+
+def _timed(call, reps, warmup):
+    """Seconds per call of `reps` back-to-back ones."""
+    import torch
+    for _ in range(warmup):
+        call()
+    torch.cuda.synchronize()
+    e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    e0.record()
+    for _ in range(reps):
+        call()
+    e1.record()
+    torch.cuda.synchronize()
+    return e0.elapsed_time(e1) * 1e-3 / reps
+
+
+def measure_decode(shapes=DECODE_SHAPES, dtype="fp16", reps=20, warmup=3):
+    """Seconds per call of a single-token step's operators; rows of (op,
+    batch, context, heads, head size, bytes, seconds)."""
+    import torch
+    from . import ops
+    dt = {"fp16": torch.float16, "bf16": torch.bfloat16, "fp32": torch.float32}[dtype]
+    e = torch.tensor([], dtype=dt).element_size()
+    gen = torch.Generator(device="cuda").manual_seed(0)
+
+    def randn(*shape):
+        return torch.randn(*shape, device="cuda", generator=gen).to(dt)
+
+    rows = []
+    for batch, context, heads, d in shapes:
+        width = -(-context // DECODE_PAGE)
+        cache = {n: randn(batch * width, heads, DECODE_PAGE, d).transpose(1, 2) for n in ("k", "v")}
+        table = torch.randperm(batch * width, device="cuda", generator=gen).to(torch.int32).view(batch, width)
+        seq = torch.arange(batch, dtype=torch.int32, device="cuda")
+        length = torch.full((batch,), context, dtype=torch.int32, device="cuda")
+        last = length - 1
+        rope = ops.rope_table(context, d)
+        qkv = randn(batch, 3 * heads, d)
+        q, k, v = qkv.split(heads, dim=1)
+        q_out, out = torch.empty_like(q), torch.empty_like(q)
+        ws = ops.alloc_paged_attention_workspace(heads, heads, d)
+        logits, adjusted = randn(batch, DECODE_VOCAB), torch.empty(batch, DECODE_VOCAB, dtype=dt, device="cuda")
+        tokens = torch.randint(0, DECODE_VOCAB, (batch, context), device="cuda", generator=gen, dtype=torch.int32)
+        penalty = torch.full((batch,), 1.1, device="cuda")
+        for op, nbytes, call in (
+                ("append", batch * (6 * heads * d * e + 12) + d * 4,
+                 lambda: ops.dsim_kv_append(cache, table, k, v, seq, last, rope=rope, q=q, q_out=q_out)),
+                ("attention", 2 * batch * heads * d * e * (context + 1) + 4 * batch * (width + 1),
+                 lambda: ops.dsim_paged_attention(q_out, cache, table, length, out, workspace=ws)),
+                ("logits", batch * (2 * DECODE_VOCAB * e + 4 * context + 8),
+                 lambda: ops.dsim_logit_adjust(logits, adjusted, history=tokens, history_len=length,
+                                               repetition=penalty))):
+            rows.append((op, batch, context, heads, d, nbytes, _timed(call, reps, warmup)))
+        del cache, logits, adjusted, tokens
+    return rows
+
+
+def main_decode(args):
+    import torch
+    rows = measure_decode(dtype=args.dtype, reps=args.reps)
+    (launch, rate), worst = fit_roofline([r[5] for r in rows], [r[6] for r in rows])
+    out = {"device": torch.cuda.get_device_name(0), "dtype": args.dtype, "reps": args.reps,
+           "decode": {"launch_s": launch, "mem_bytes_per_s": rate}, "worst_relative_error": worst,
+           "samples": [dict(op=r[0], batch=r[1], context=r[2], heads=r[3], head_dim=r[4], bytes=r[5], seconds=r[6],
+                            fitted=launch + r[5] / rate) for r in rows]}
+    if args.out:
+        with open(args.out, "w") as f:
+            f.write(json.dumps(out, indent=1))
+    print(json.dumps({k: out[k] for k in ("device", "dtype", "decode", "worst_relative_error")}))
+    return 0
+
+
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
+    ap.add_argument("--op", default="matmul", choices=("matmul", "decode"))
     ap.add_argument("--dtype", default="fp16", choices=("fp16", "bf16", "fp32"))
     ap.add_argument("--reps", type=int, default=20)
     ap.add_argument("--out", default=None, help="write the samples and the fit as JSON")
@@ -192,6 +297,8 @@ def main(argv=None):
     if not torch.cuda.is_available():
         print("calibrate needs a GPU", file=sys.stderr)
         return 1
+    if args.op == "decode":
+        return main_decode(args)
     rows = measure(dtype=args.dtype, reps=args.reps)
     fl, by, kk, sec = ([r[i] for r in rows] for i in (3, 4, 2, 5))
     lin, worst_lin = fit(fl, by, sec)

@@ -124,6 +124,54 @@ def test_append_many_tokens():
     check_append(F16, F16, 1, 1, 16, 16, [3000, 1, 2000], rot=16)
 
 
+def test_append_more_tokens_than_workgroups():
+    n = (1 << 20) + 5
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k, v = (torch.randn(n, 1, 16, device="cuda", generator=g).half() for _ in range(2))
+    cache = ops.alloc_kv_cache(-(-n // 64) + 1, 64, 1, 16, F16)
+    table = torch.randperm(-(-n // 64) + 1, device="cuda", generator=g).to(torch.int32)[None]
+    pos = torch.arange(n, device="cuda", dtype=torch.int32)
+    ops.dsim_kv_append(cache, table, k, v, torch.zeros_like(pos), pos)
+    at = table[0, pos.long() // 64].long(), pos.long() % 64
+    assert torch.equal(cache["k"][at], k) and torch.equal(cache["v"][at], v)
+
+
+def test_append_two_tokens_of_one_place():
+    """Not a call to make: each element is one of theirs, and nothing else
+    changes."""
+    g = gen(3)
+    cache = {n: torch.zeros(2, 16, 2, 64, dtype=F16, device="cuda") for n in ("k", "v")}
+    k, v = (randn(g, 3, 2, 64).half() for _ in range(2))
+    one = torch.tensor([0, 0, 0], dtype=torch.int32, device="cuda")
+    ops.dsim_kv_append(cache, torch.tensor([[1]], dtype=torch.int32, device="cuda"), k.cuda(), v.cuda(), one,
+                       torch.tensor([4, 4, 9], dtype=torch.int32, device="cuda"))
+    for c, x in ((cache["k"].cpu(), k), (cache["v"].cpu(), v)):
+        assert torch.all((c[1, 4] == x[0]) | (c[1, 4] == x[1])) and torch.equal(c[1, 9], x[2])
+        c[1, 4], c[1, 9] = 0, 0
+        assert not c.any()
+
+
+def test_cache_beyond_32_bits():
+    """Pages whose elements lie behind 2^31 of them: appended, then attended to."""
+    heads, d, slots = 8, 128, 16
+    pages = (1 << 31) // (heads * d * slots) + 70
+    cache = ops.alloc_kv_cache(pages, slots, heads, d, BF16)
+    table = torch.tensor([[pages - 1, 3, pages - 2, pages - 60]], dtype=torch.int32)
+    n = 60
+    g = gen(7)
+    k, v, q = randn(g, n, heads, d).bfloat16(), randn(g, n, heads, d).bfloat16(), randn(g, 1, 16, d).bfloat16()
+    pos = torch.arange(n, dtype=torch.int32)
+    ops.dsim_kv_append(cache, table.cuda(), k.cuda(), v.cuda(), torch.zeros_like(pos).cuda(), pos.cuda())
+    for c, x in ((cache["k"], k), (cache["v"], v)):
+        assert torch.equal(c[table[0, pos.long() // slots].long().cuda(), (pos.long() % slots).cuda()].cpu(), x)
+    out = torch.empty(1, 16, d, dtype=BF16, device="cuda")
+    ops.dsim_paged_attention(q.cuda(), cache, table.cuda(), torch.tensor([n], dtype=torch.int32, device="cuda"), out)
+    near = torch.arange(4, dtype=torch.int32)[None]
+    pad = lambda x: torch.cat([x, x[:4]]).view(4, slots, heads, d)   # noqa: E731
+    ref, _, bound = plain.attend(q, pad(k), pad(v), near, torch.tensor([n]), d ** -0.5)
+    assert torch.all((out.cpu().double() - ref).abs() <= bound + (ref.abs() + bound) * 2.0 ** -8)
+
+
 def test_append_special_values():
     """Infinities, NaN, the largest and smallest numbers, in 16 bits and into
     an 8-bit cache (where what lies beyond its range becomes its largest)."""
@@ -225,7 +273,7 @@ TYPES = [(F32, F32), (F16, F16), (BF16, BF16), (F16, E4M3), (BF16, E4M3)]
 
 @pytest.mark.parametrize("dtype,cache", TYPES)
 @pytest.mark.parametrize("heads,kv,d", [(12, 12, 64), (8, 2, 128), (16, 1, 96), (5, 5, 80), (2, 1, 256), (3, 3, 16),
-                                        (4, 4, 112), (40, 2, 64), (6, 2, 208)])
+                                        (4, 4, 112), (40, 2, 64), (6, 2, 208), (64, 1, 48), (17, 1, 144)])
 def test_attend(dtype, cache, heads, kv, d):
     check_attend(dtype, cache, heads, kv, d, 16, [1, 16, 17, 100, 0, 33, 250], scales=cache == E4M3 and heads > 4)
 
@@ -255,13 +303,39 @@ def test_attend_window(dtype, window):
 @pytest.mark.parametrize("dtype,cache", TYPES)
 def test_attend_long(dtype, cache):
     """Contexts that the work's cuts go through, among short ones and empty rows."""
-    check_attend(dtype, cache, 4, 2, 64, 16, [5000, 3, 0, 9001, -1, 700, 1], seed=3)
+    lens = [5000, 3, 0, 9001, -1, 700, 1]
+    check_attend(dtype, cache, 4, 2, 64, 16, lens, seed=3)
+    check_attend(dtype, cache, 4, 1, 128, 32, lens, seed=4, window=4000)
+    check_attend(dtype, cache, 2, 2, 256, 16, lens, seed=5)
+    check_attend(dtype, cache, 20, 1, 80, 48, lens, seed=6)
+    check_attend(dtype, cache, 2, 1, 64, 5, lens, seed=7)
 
 
 def test_attend_many_sequences():
     g = gen(5)
     lens = torch.randint(-1, 60, (700,), generator=g).tolist()
     check_attend(BF16, BF16, 2, 1, 64, 16, lens)
+
+
+def test_attend_many_contexts_and_cuts():
+    """More contexts than runs, some of them cut."""
+    g = gen(6)
+    lens = torch.randint(1, 400, (90,), generator=g).tolist() + [7000, 2500]
+    check_attend(BF16, BF16, 8, 8, 64, 16, lens)
+    check_attend(BF16, E4M3, 36, 9, 64, 16, lens, window=3000)
+
+
+def test_attend_shared_pages():
+    """Sequences that share their first pages."""
+    g = gen(12)
+    table, pages = deal(g, [100, 130], 16)
+    table[1, :5] = table[0, :5]
+    keys, values = cache_like(g, pages, 16, 2, 64, F16)
+    q, lens = randn(g, 2, 4, 64).half(), torch.tensor([100, 130], dtype=torch.int32)
+    out = torch.empty(2, 4, 64, dtype=F16, device="cuda")
+    ops.dsim_paged_attention(q.cuda(), dict(k=to_gpu(keys), v=to_gpu(values)), table.cuda(), lens.cuda(), out)
+    ref, _, bound = plain.attend(q, keys, values, table.clamp(min=0), lens, 0.125)
+    assert torch.all((out.cpu().double() - ref).abs() <= bound + (ref.abs() + bound) * 2.0 ** -11 + 2.0 ** -25)
 
 
 def test_attend_one_context():
@@ -504,6 +578,23 @@ def test_logits_nothing():
     assert torch.all(x == 1)
 
 
+def test_logits_beyond_32_bits():
+    """Rows behind 2^31 elements, in place."""
+    vocab = 50257
+    n = (1 << 31) // vocab + 9
+    x = torch.zeros(n, vocab, dtype=F16, device="cuda")
+    check = [0, 1, n // 2, n - 2, n - 1]
+    small, a = logits_case(9, len(check), vocab, F16, 40, 3, True)
+    x[check] = small.cuda()
+
+    def spread(t):
+        big = torch.zeros(n, *t.shape[1:], dtype=t.dtype, device="cuda")
+        big[check] = t.cuda()
+        return big
+    ops.dsim_logit_adjust(x, x, **{k: spread(v) for k, v in a.items()})
+    assert plain.same(x[check].cpu(), plain.logits(small, **a))
+
+
 # ---------------------------------------------------------------------------
 # Together
 # ---------------------------------------------------------------------------
@@ -621,6 +712,29 @@ def test_workspace_of_the_call_on_another_stream():
     assert torch.equal(first, out)
     ref, _, bound = plain.attend(q, keys, values, table.clamp(min=0), torch.tensor([3000]), 0.125)
     assert torch.all((out.cpu().double() - ref).abs() <= bound + (ref.abs() + bound) * 2.0 ** -11 + 2.0 ** -25)
+
+
+def test_two_calls_at_once():
+    """Attention over one cache on two streams, each with its own workspace."""
+    g = gen(10)
+    lens = [4000, 17, 900, 2500]
+    table, pages = deal(g, lens, 16)
+    keys, values = cache_like(g, pages, 16, 2, 128, BF16)
+    cache, table = dict(k=to_gpu(keys), v=to_gpu(values)), table.cuda()
+    lens = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    qs = [randn(g, 4, 8, 128).bfloat16().cuda() for _ in range(2)]
+    alone = [torch.empty_like(q) for q in qs]
+    for q, out in zip(qs, alone):
+        ops.dsim_paged_attention(q, cache, table, lens, out)
+    streams, outs = [torch.cuda.Stream() for _ in qs], [torch.zeros_like(q) for q in qs]
+    spaces = [ops.alloc_paged_attention_workspace(8, 2, 128) for _ in qs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for q, out, ws, s in zip(qs, outs, spaces, streams):
+            ops.dsim_paged_attention(q, cache, table, lens, out, workspace=ws, stream=s)
+    torch.cuda.synchronize()
+    for a, b in zip(alone, outs):
+        assert torch.equal(a, b)
 
 
 def test_step_in_captured_graphs():
