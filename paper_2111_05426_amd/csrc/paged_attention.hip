@@ -61,6 +61,7 @@ struct Params {
     int32_t group, tiles_of_heads, part_heads;
     int32_t grid;         // runs that the work is cut into
     bool by_context;      // there are at most as many contexts
+    bool direct;          // a workgroup per context, nothing is cut
     uint32_t div_mul, div_shift;   // t / page_size = t * div_mul >> div_shift, 0 <= t < 2^31
 };
 
@@ -552,59 +553,70 @@ __global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Param
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int units = p.n_heads * p.tiles_of_heads;   // contexts per sequence
 
-    // this workgroup's run: tiles counted per thread, summed over the block
-    const int per = (p.n_seq + kBlock - 1) / kBlock, lo = tid * per, hi = min(p.n_seq, lo + per);
-    int64_t mine = 0;
-    for (int b = lo; b < hi; ++b) mine += Span<kKeys>::of(p, p.seq_len[b]).cost();
-    int64_t incl = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int64_t x = __shfl_up(incl, o);
-        if (lane >= o) incl += x;
-    }
-    if (lane == 63) s_sum[wave] = incl;
+    int b, unit, c0 = 0;
+    int64_t left, run = 0;
+    Span<kKeys> sp;
     if (tid < 2) s_bad[tid] = 0;
-    __syncthreads();
-    int64_t total = 0, before = 0;
+    if (p.direct) {
+        b = blockIdx.x / units;
+        unit = blockIdx.x - b * units;
+        sp = Span<kKeys>::of(p, p.seq_len[b]);
+        left = sp.cost();
+        __syncthreads();
+    } else {
+        // this workgroup's run: tiles counted per thread, summed over the block
+        const int per = (p.n_seq + kBlock - 1) / kBlock, lo = tid * per, hi = min(p.n_seq, lo + per);
+        int64_t mine = 0;
+        for (int b = lo; b < hi; ++b) mine += Span<kKeys>::of(p, p.seq_len[b]).cost();
+        int64_t incl = mine;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) before += s_sum[w];
-        total += s_sum[w];
-    }
-    total = uniform(total) * units;
-    constexpr int kRuns = kCus * per_cu(DP, sizeof(CT));   // the grid
-    const int64_t even = (total + kRuns - 1) / kRuns, run = even > kExtra + kMinTiles ? even : kExtra + kMinTiles;
-    const int64_t begin = blockIdx.x * run;
-    if (begin >= total) {
-        if (tid == 0 && !p.by_context) p.cut[blockIdx.x] = make_int4(0, 0, 0, 0);
-        return;
-    }
-    const int64_t end = begin + run < total ? begin + run : total;
-    const int64_t excl = (before + incl - mine) * units;
-    if (begin >= excl && begin < excl + mine * units) {
-        int64_t at = excl;
-        for (int b = lo; b < hi; ++b) {
-            const int32_t len = p.seq_len[b];
-            const int64_t n = (int64_t)Span<kKeys>::of(p, len).cost() * units;
-            if (begin < at + n) {
-                s_seq = b;
-                s_len = len;
-                s_at = begin - at;
-                break;
-            }
-            at += n;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int64_t x = __shfl_up(incl, o);
+            if (lane >= o) incl += x;
         }
-    }
-    __syncthreads();
-    int b = __builtin_amdgcn_readfirstlane(s_seq);
-    Span<kKeys> sp = Span<kKeys>::of(p, __builtin_amdgcn_readfirstlane(s_len));
-    int64_t left = end - begin;
-    int unit, c0;
-    {
-        const int64_t at = uniform(s_at);
-        const int cost = sp.cost();
-        unit = at >> 32 == 0 ? (int)((uint32_t)at / (uint32_t)cost) : (int)(at / cost);   // (64 bits take 0.3 us)
-        c0 = (int)(at - (int64_t)unit * cost);
+        if (lane == 63) s_sum[wave] = incl;
+        __syncthreads();
+        int64_t total = 0, before = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) before += s_sum[w];
+            total += s_sum[w];
+        }
+        total = uniform(total) * units;
+        constexpr int kRuns = kCus * per_cu(DP, sizeof(CT));   // the grid
+        const int64_t even = (total + kRuns - 1) / kRuns;
+        run = even > kExtra + kMinTiles ? even : kExtra + kMinTiles;
+        const int64_t begin = blockIdx.x * run;
+        if (begin >= total) {
+            if (tid == 0 && !p.by_context) p.cut[blockIdx.x] = make_int4(0, 0, 0, 0);
+            return;
+        }
+        const int64_t end = begin + run < total ? begin + run : total;
+        const int64_t excl = (before + incl - mine) * units;
+        if (begin >= excl && begin < excl + mine * units) {
+            int64_t at = excl;
+            for (int b = lo; b < hi; ++b) {
+                const int32_t len = p.seq_len[b];
+                const int64_t n = (int64_t)Span<kKeys>::of(p, len).cost() * units;
+                if (begin < at + n) {
+                    s_seq = b;
+                    s_len = len;
+                    s_at = begin - at;
+                    break;
+                }
+                at += n;
+            }
+        }
+        __syncthreads();
+        b = __builtin_amdgcn_readfirstlane(s_seq);
+        sp = Span<kKeys>::of(p, __builtin_amdgcn_readfirstlane(s_len));
+        left = end - begin;
+        {
+            const int64_t at = uniform(s_at);
+            const int cost = sp.cost();
+            unit = at >> 32 == 0 ? (int)((uint32_t)at / (uint32_t)cost) : (int)(at / cost);   // (64 bits take 0.3 us)
+            c0 = (int)(at - (int64_t)unit * cost);
+        }
     }
     int4 cut = make_int4(0, 0, 0, 0);
     int turn = 0;
@@ -744,7 +756,7 @@ __global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Param
             if (p.by_context && tid == 0) p.cut[b * units + unit] = cut;
         }
     }
-    if (tid == 0 && !p.by_context) p.cut[blockIdx.x] = cut;
+    if (tid == 0 && !p.by_context && !p.direct) p.cut[blockIdx.x] = cut;
 }
 
 // Joins the parts of the contexts that are cut.  W = 1: a wave takes a head
@@ -827,8 +839,19 @@ template <class T, class CT, int DP> dsim_status launch(Params &p, hipStream_t s
 {
     const int64_t contexts = (int64_t)p.n_seq * p.n_heads * p.tiles_of_heads;
     p.grid = kCus * per_cu(DP, sizeof(CT));
-    p.by_context = contexts <= p.grid;
-    const dim3 grid((unsigned)p.grid), block(kBlock);
+    // Contexts that cannot be long (the block table has no room, or the window
+    // is short) take a workgroup each and need neither the cut nor the join:
+    // up to 32 tiles (fp32, whose products take longer than its loads: 16).
+    // bf16, 8 cache heads of 128, up to 512 tokens: one sequence 11.0 us (cut
+    // 15.2), 256 67.6 (71.1); up to 2,048: one 25.6 (15.6), 64 63.4 (64.3).
+    // fp32, 12 heads of 80, up to 256 tokens: one 13.9 (18.1), 256 96 (94);
+    // up to 512: one 20.8 (18.3), 256 149 (141).
+    constexpr int kKeys = Pass<T, CT, DP, true>::kKeys;
+    int64_t most = (int64_t)p.table_width * p.page_size;
+    if (p.window > 0 && p.window + kKeys < most) most = p.window + kKeys;
+    p.direct = most <= (sizeof(CT) == 4 ? 16 : 32) * kKeys && contexts < 1 << 24;
+    p.by_context = !p.direct && contexts <= p.grid;
+    const dim3 grid((unsigned)(p.direct ? contexts : p.grid)), block(kBlock);
     // 16 slots of a page at offsets of 24-bit products
     const bool whole = p.page_size % 16 == 0 && p.slot_stride * (int64_t)sizeof(CT) < 1 << 24;
     if (whole && p.d == DP)
@@ -839,6 +862,7 @@ template <class T, class CT, int DP> dsim_status launch(Params &p, hipStream_t s
         hipLaunchKernelGGL((k_attend<T, CT, DP, false, false>), grid, block, 0, s, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return hip_fail(e, "paged attention launch");
+    if (p.direct) return DSIM_OK;
     // few contexts have many parts each
     constexpr int kShift = Pass<T, CT, DP, true>::kShift;
     const unsigned x = (unsigned)(p.by_context ? contexts : p.grid), heads = (unsigned)p.part_heads;

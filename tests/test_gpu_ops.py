@@ -275,13 +275,16 @@ TYPES = [(F32, F32), (F16, F16), (BF16, BF16), (F16, E4M3), (BF16, E4M3)]
 @pytest.mark.parametrize("heads,kv,d", [(12, 12, 64), (8, 2, 128), (16, 1, 96), (5, 5, 80), (2, 1, 256), (3, 3, 16),
                                         (4, 4, 112), (40, 2, 64), (6, 2, 208), (64, 1, 48), (17, 1, 144)])
 def test_attend(dtype, cache, heads, kv, d):
-    check_attend(dtype, cache, heads, kv, d, 16, [1, 16, 17, 100, 0, 33, 250], scales=cache == E4M3 and heads > 4)
+    lens = [1, 16, 17, 100, 0, 33, 250]
+    check_attend(dtype, cache, heads, kv, d, 16, lens, scales=cache == E4M3 and heads > 4)
+    check_attend(dtype, cache, heads, kv, d, 16, lens, scales=cache == E4M3 and heads > 4, width=200)
 
 
 @pytest.mark.parametrize("dtype,cache", TYPES)
 @pytest.mark.parametrize("slots", [1, 3, 16, 48, 64, 256])
 def test_attend_page_sizes(dtype, cache, slots):
     check_attend(dtype, cache, 4, 2, 64, slots, [1, 31, 32, 65, 129, 300], seed=slots)
+    check_attend(dtype, cache, 4, 2, 64, slots, [1, 31, 32, 65, 129, 300], seed=slots, width=2000 // slots + 1)
 
 
 @pytest.mark.parametrize("order", ["head", "slot", "gaps"])
@@ -298,6 +301,7 @@ def test_attend_window(dtype, window):
         for b, n in enumerate(at["lens"]):
             at["table"][b, :max(0, n - window) // 16] = -1
     check_attend(dtype, dtype, 4, 2, 64, 16, [1, 14, 41, 64, 500, 0], window=window, edit=edit)
+    check_attend(dtype, dtype, 4, 2, 64, 16, [1, 14, 41, 64, 500, 0], window=window, edit=edit, width=90)
 
 
 @pytest.mark.parametrize("dtype,cache", TYPES)
@@ -315,6 +319,7 @@ def test_attend_many_sequences():
     g = gen(5)
     lens = torch.randint(-1, 60, (700,), generator=g).tolist()
     check_attend(BF16, BF16, 2, 1, 64, 16, lens)
+    check_attend(BF16, BF16, 2, 1, 64, 16, lens, width=100)
 
 
 def test_attend_many_contexts_and_cuts():
@@ -362,6 +367,7 @@ def test_attend_garbage_behind_the_end(dtype, cache):
                     x[pg, sl] = value
     check_attend(dtype, cache, 4, 2, 64, 16, [1, 17, 31, 100, 250, 0], edit=edit)
     check_attend(dtype, cache, 4, 2, 64, 16, [1, 17, 31, 100, 250, 0], edit=edit, window=20)
+    check_attend(dtype, cache, 4, 2, 64, 16, [1, 17, 31, 100, 250, 0], edit=edit, width=200)
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16, F32])
@@ -423,11 +429,12 @@ def test_attend_not_a_number():
                     assert torch.all(out[..., 5].isnan()) and torch.all(out[..., :5].isfinite())
 
 
-def test_attend_errors_in_device_data():
+@pytest.mark.parametrize("longest", [9000, 600])
+def test_attend_errors_in_device_data(longest):
     """A length beyond the block table and a page outside the cache are
     flagged, give NaN, and leave the other sequences right."""
     g = gen(2)
-    lens = [50, 400, 9000, 33, 10]
+    lens = [50, 400, longest, 33, 10]
     table, pages = deal(g, lens, 16)
     keys, values = cache_like(g, pages, 16, 2, 64, F16)
     q = randn(g, 5, 4, 64).half()
@@ -435,7 +442,7 @@ def test_attend_errors_in_device_data():
     seq_len = torch.tensor(lens, dtype=torch.int32)
     seq_len[0] = table.shape[1] * 16 + 1
     table[1, 3] = pages
-    table[2, 500] = -1
+    table[2, longest // 16 - 10] = -1
     out = torch.zeros(5, 4, 64, dtype=F16, device="cuda")
     lse, status = torch.zeros(5, 4, device="cuda"), torch.full((5,), -7, dtype=torch.int32, device="cuda")
     ops.dsim_paged_attention(q.cuda(), dict(k=to_gpu(keys), v=to_gpu(values)), table.cuda(), seq_len.cuda(), out,
