@@ -6,6 +6,7 @@
 // moved, so memory bounds it, and latency a call of few tokens.  On MI355X
 // 24,588 tokens of prompts (bf16, 32 query and 8 cache heads of 128, 606 MB)
 // take 114 us, 5.3 TB/s; one token of 12 heads of 64 takes 3.3 us.
+// (Loading a thread's next chunk before the one at hand is stored: 128 us.)
 #include "numeric.h"
 #include "ops.h"
 
@@ -51,10 +52,14 @@ __device__ inline Place place_of(const AppendArgs &a, int64_t t)
     return p;
 }
 
+// j / n for mul = ceil(2^32 / n), 0 for n = 1; exact for j < 2^26, n <= 64 (a
+// call's chunks a token: 2^17, a row's: 64)
+__device__ inline int divide(int j, uint32_t mul) { return mul ? (int)__umulhi((uint32_t)j, mul) : j; }
+
 // T: type of the new rows; CT: of the cache; VEC: elements per load.  A
 // thread takes one chunk of VEC elements, or, where pairs (i, i + R/2) are
 // rotated, one chunk of each half.
-template <class T, class CT, int VEC> __global__ __launch_bounds__(kMaxBlock) void k_append(AppendArgs a)
+template <class T, class CT, int VEC> __global__ __launch_bounds__(kMaxBlock) void k_append(AppendArgs a, uint32_t mul_head, uint32_t mul_value)
 {
     using V = vec<float, VEC>;
     const int d = a.c.head_dim, rot = a.rot_dim;
@@ -69,14 +74,14 @@ template <class T, class CT, int VEC> __global__ __launch_bounds__(kMaxBlock) vo
         for (int i = threadIdx.x; i < n_q + n_k + n_v; i += blockDim.x) {
             if (i >= n_q + n_k) {   // a value: copied
                 if (p.status) continue;
-                const int j = i - n_q - n_k, h = j / per_value, e = j % per_value * VEC;
+                const int j = i - n_q - n_k, h = divide(j, mul_value), e = (j - h * per_value) * VEC;
                 V x = load_row<T, VEC>(a.v.data, t * a.v.row_stride + h * a.v.head_stride + e);
                 if (a.c.v_scale) x /= a.c.v_scale[h];
                 store_row<CT, VEC>(a.c.v, p.at + h * a.c.head_stride + e, x);
                 continue;
             }
             const bool query = i < n_q;
-            const int j = query ? i : i - n_q, h = j / per_head, c = j % per_head;
+            const int j = query ? i : i - n_q, h = divide(j, mul_head), c = j - h * per_head;
             const dsim_rows &src = query ? a.q : a.k;
             const int64_t from = t * src.row_stride + h * src.head_stride;
             const int64_t to = query ? t * a.q_out.row_stride + h * a.q_out.head_stride
@@ -99,11 +104,12 @@ template <class T, class CT, int VEC> __global__ __launch_bounds__(kMaxBlock) vo
                 y = y * cosv + x * sinv;
                 x = z;
             } else if (turned) {
+                using H = vec<float, VEC / 2>;
+                const H co = *reinterpret_cast<const H *>(cs + e / 2), si = *reinterpret_cast<const H *>(cs + (rot + e) / 2);
 #pragma unroll
                 for (int k = 0; k < VEC; k += 2) {
-                    const float co = cs[(e + k) / 2], si = cs[rot / 2 + (e + k) / 2];
-                    const float z = x[k] * co - x[k + 1] * si;
-                    x[k + 1] = x[k + 1] * co + x[k] * si;
+                    const float z = x[k] * co[k / 2] - x[k + 1] * si[k / 2];
+                    x[k + 1] = x[k + 1] * co[k / 2] + x[k] * si[k / 2];
                     x[k] = z;
                 }
             }
@@ -133,7 +139,8 @@ template <class T, class CT, int VEC> void launch(const AppendArgs &a, hipStream
     const int64_t most = a.n_tok < 1024 ? kMaxBlock : 128, rounds = (chunks + most - 1) / most;
     const int block = (int)((chunks + 64 * rounds - 1) / (64 * rounds)) * 64;
     const dim3 grid((unsigned)(a.n_tok < (1 << 20) ? a.n_tok : (1 << 20)));
-    hipLaunchKernelGGL((k_append<T, CT, VEC>), grid, dim3(block), 0, s, a);
+    const auto mul = [](int n) { return n > 1 ? (uint32_t)((((uint64_t)1 << 32) + n - 1) / n) : 0u; };
+    hipLaunchKernelGGL((k_append<T, CT, VEC>), grid, dim3(block), 0, s, a, mul(n_rot + rest), mul(a.c.head_dim / VEC));
 }
 
 template <class T, class CT> void launch(const AppendArgs &a, hipStream_t s)

@@ -102,7 +102,8 @@ def check_append(dtype, cache, heads, kv, d, slots, lens, past=0, rot=0, interle
 @pytest.mark.parametrize("dtype,cache", [(F32, F32), (F16, F16), (BF16, BF16), (F16, E4M3), (BF16, E4M3)])
 @pytest.mark.parametrize("heads,kv,d,rot,interleaved", [
     (12, 12, 64, 64, False), (8, 2, 128, 128, False), (4, 4, 64, 48, True), (5, 1, 80, 40, False), (2, 2, 16, 8, True),
-    (3, 3, 256, 0, False), (7, 7, 96, 96, True), (33, 3, 112, 56, False)])
+    (3, 3, 256, 0, False), (7, 7, 96, 96, True), (33, 3, 112, 56, False), (5, 3, 16, 16, False), (4, 2, 16, 16, True),
+    (300, 100, 32, 32, False)])
 def test_append(dtype, cache, heads, kv, d, rot, interleaved):
     check_append(dtype, cache, heads, kv, d, 16, [1, 5, 33, 16], rot=rot, interleaved=interleaved,
                  scales=cache == E4M3 and heads % 2 == 0)
