@@ -5,8 +5,8 @@
 // written once, and one row of the rotation table: 3 flops per 2 elements
 // moved, so memory bounds it, and latency a call of few tokens.  On MI355X
 // 24,588 tokens of prompts (bf16, 32 query and 8 cache heads of 128, 606 MB)
-// take 114 us, 5.3 TB/s; one token of 12 heads of 64 takes 3.3 us.
-// (Loading a thread's next chunk before the one at hand is stored: 128 us.)
+// take 108 us, 5.6 TB/s; one token of 12 heads of 64 takes 3.2 us.  (Loading a
+// thread's next chunk before the one at hand is stored costs 14 us more.)
 #include "numeric.h"
 #include "ops.h"
 
@@ -20,9 +20,10 @@ template <class T, int VEC> __device__ inline vec<float, VEC> load_row(const voi
     return to_f32<T, VEC>(*reinterpret_cast<const vec<T, VEC> *>(static_cast<const T *>(p) + at));
 }
 
+// (streaming stores: with plain ones the 24,588 tokens below take 114 us)
 template <class T, int VEC> __device__ inline void store_row(void *p, int64_t at, vec<float, VEC> x)
 {
-    *reinterpret_cast<vec<T, VEC> *>(static_cast<T *>(p) + at) = from_f32<T, VEC>(x);
+    __builtin_nontemporal_store(from_f32<T, VEC>(x), reinterpret_cast<vec<T, VEC> *>(static_cast<T *>(p) + at));
 }
 
 // Where a token goes: its place in the cache (elements, without the head)
@@ -133,7 +134,8 @@ template <class T, class CT, int VEC> void launch(const AppendArgs &a, hipStream
     // A workgroup takes a token.  Few tokens: a thread for every chunk, up to
     // 512 (bf16, 32 query and 8 cache heads of 128: 256 tokens 4.1 us, with
     // 128 threads 5.4).  Many: fewer and busier threads, so that fewer
-    // workgroups start (24,588 tokens 114 us, with 512 threads 173).
+    // workgroups start (24,588 tokens 114 us, with 512 threads 173, both
+    // with plain stores).
     const int n_rot = a.interleaved ? a.rot_dim / VEC : a.rot_dim / 2 / VEC, rest = (a.c.head_dim - a.rot_dim) / VEC;
     const int64_t chunks = (int64_t)(a.n_q_heads + a.c.n_heads) * (n_rot + rest) + (int64_t)a.c.n_heads * (a.c.head_dim / VEC);
     const int64_t most = a.n_tok < 1024 ? kMaxBlock : 128, rounds = (chunks + most - 1) / most;

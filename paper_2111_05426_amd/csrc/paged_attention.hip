@@ -1,894 +1,19 @@
-// paged_attention.hip -- attention of one new token per sequence over its
-// paged keys and values (dsim_paged_attention).
-#include "numeric.h"
-#include "ops.h"
+// paged_attention.hip -- dsim_paged_attention on the host: its workspace and
+// its launch; the kernels are in paged_attention.h.
+#include "paged_attention.h"
 
 namespace dsim {
-namespace {
-
-constexpr int kWaves = 4;
-constexpr int kBlock = 64 * kWaves;
-constexpr int kCus = 256;
-// Workgroups per CU by the padded head dimension and the size of the cache's
-// elements, all resident at once.
-constexpr int per_cu(int dp, int size) { return dp <= 128 || size == 1 ? 2 : 1; }
-constexpr int kMaxGrid = kCus * 2;
-constexpr int kMinTiles = 4;      // a tile for every wave
-constexpr int kExtra = 8;         // what a context costs beside its tiles, in tiles
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-// How the elements of a (query, cache) type pair go through the matrix
-// instructions.  One tile is kKeys keys of one cache head and 16 query heads
-// (those of the group, the rest zero):
-//   scores   S[key][head] = K[key][:] . q[head][:]      rows = keys
-//   output   O[d][head]  += V[key][d] P[key][head]      rows = d
-// A lane l = 16 g + r of a 16 x 16 product holds row r of the left operand
-// and column r of the right one for the reduction indices of its group g,
-// and of the result column r, rows 4 g + i.  The result of the scores is
-// therefore, lane for lane, the right operand of the output product, and the
-// order of the reduction index is free as long as both operands agree:
-//   keys: the lane's own rows 4 g + i of each 16-key product;
-//   head dimension: chunk c = 4 step + g.
-// Row r of output product e stands for d = E r + e, so a lane loads E
-// consecutive elements of each of its keys' values and transposes inside its
-// own registers; nothing crosses lanes and shared memory is not used.
-template <class T> struct Mfma;
-template <> struct Mfma<f16> {
-    __device__ static f32x4 mul(vec<f16, 8> a, vec<f16, 8> b, f32x4 c)
-    {
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-    }
-};
-template <> struct Mfma<bf16> {
-    __device__ static f32x4 mul(vec<bf16, 8> a, vec<bf16, 8> b, f32x4 c)
-    {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-    }
-};
-
-struct Params {
-    const void *k, *v, *q;
-    void *out;
-    const float *k_scale, *v_scale;
-    const int32_t *table, *seq_len;
-    float *lse;
-    int32_t *status;
-    float *part;          // partial results, 2 per workgroup
-    int4 *cut;            // contexts that are cut: by context, or by the workgroup that begins it
-    int64_t n_pages, page_stride, slot_stride, head_stride, table_stride, q_row, q_head, out_row, out_head;
-    float scale;          // times log2 e
-    int32_t n_seq, n_heads, n_q_heads, d, page_size, table_width, window;
-    int32_t group, tiles_of_heads, part_heads;
-    int32_t grid;         // runs that the work is cut into
-    bool by_context;      // there are at most as many contexts
-    bool direct;          // a workgroup per context, nothing is cut
-    uint32_t div_mul, div_shift;   // t / page_size = t * div_mul >> div_shift, 0 <= t < 2^31
-};
-
-// Page and slot of a position.
-struct Place {
-    int32_t page, slot;   // of the sequence, of the page
-    __device__ static Place of(const Params &p, int32_t t)
-    {
-        const int32_t q = (int32_t)((uint64_t)(uint32_t)t * p.div_mul >> p.div_shift);
-        return {q, t - q * p.page_size};
-    }
-};
-
-// The keys of a sequence in tiles: first tile, number of tiles (at least
-// one, so that somebody writes the row; none if the row is left alone).
-template <int KEYS> struct Span {
-    int32_t first_key, len, first_tile, n;
-    bool bad;
-    __device__ int32_t cost() const { return n > 0 ? n + kExtra : 0; }
-    __device__ static Span of(const Params &p, int32_t len)
-    {
-        Span s{0, len, 0, 0, false};
-        if (len < 0) return s;
-        s.bad = (int64_t)len > (int64_t)p.table_width * p.page_size;
-        if (s.bad) s.len = 0;
-        s.first_key = p.window > 0 && s.len > p.window ? s.len - p.window : 0;
-        s.first_tile = s.first_key / KEYS;
-        const int32_t end = (int32_t)(((int64_t)s.len + KEYS - 1) / KEYS);
-        s.n = end > s.first_tile ? end - s.first_tile : 1;
-        return s;
-    }
-};
-
-// Running state of one wave: for column r (a query head) the maximum m, this
-// lane's share of the sum l, and the output's rows.
-template <int NT> struct State {
-    float m, l;
-    f32x4 o[NT];
-};
-
-// a value that is the same for all lanes, in scalar registers
-__device__ inline int64_t uniform(int64_t x)
-{
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
-    return (int64_t)((uint64_t)hi << 32 | lo);
-}
-
-// The values of the other groups' lanes r: halves and odd and even rows of a
-// wave exchanged.
-__device__ inline vec<float, 2> other_half(float x)
-{
-    const auto y = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
-    return {__builtin_bit_cast(float, (uint32_t)y[0]), __builtin_bit_cast(float, (uint32_t)y[1])};
-}
-
-__device__ inline vec<float, 2> other_row(float x)
-{
-    const auto y = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
-    return {__builtin_bit_cast(float, (uint32_t)y[0]), __builtin_bit_cast(float, (uint32_t)y[1])};
-}
-
-__device__ inline float max_groups(float x)
-{
-    const auto y = other_half(x);
-    const auto z = other_row(fmaxf(y[0], y[1]));
-    return fmaxf(z[0], z[1]);
-}
-
-__device__ inline float sum_groups(float x)
-{
-    const auto y = other_half(x);
-    const auto z = other_row(y[0] + y[1]);
-    return z[0] + z[1];
-}
-
-// What sums held against the maximum `from` count against the maximum `to`.
-// Where there was none (-inf) they are held against 0: zero, or NaN, which
-// has to stay.
-__device__ inline float rescale(float from, float to)
-{
-    return from == -HUGE_VALF ? 1.0f : __builtin_amdgcn_exp2f(from - to);
-}
-
-// The running maximum takes in the products s; returns them as weights, 2^SHIFT
-// for one at the maximum.  scale > 0: base-2 logarithms per unit of s.  `in`:
-// bit i says whether s[i] counts (looked at unless `all`); one that does not
-// becomes the weight `least` and adds nothing to the sum.
-template <int SHIFT, int N, int NT>
-__device__ inline void weigh(float (&s)[N], float scale, bool all, uint32_t in, float least, State<NT> &st)
-{
-    if (!all) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) s[i] = in >> i & 1 ? s[i] : -HUGE_VALF;
-    }
-    float top = s[0];
-#pragma unroll
-    for (int i = 1; i < N; ++i) top = fmaxf(top, s[i]);
-    top = max_groups(top) * scale;
-    if (__builtin_amdgcn_ballot_w64(top > st.m) != 0) {
-        const float m = fmaxf(st.m, top);
-        const float f = rescale(st.m, m);
-        st.l *= f;
-#pragma unroll
-        for (int e = 0; e < NT; ++e) st.o[e] *= f;
-        st.m = m;
-    }
-    const float m = st.m == -HUGE_VALF ? 0.0f : st.m - SHIFT;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -m));
-        st.l += s[i];
-    }
-    if (!all) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) s[i] = in >> i & 1 ? s[i] : least;
-    }
-}
-
-// 16-bit queries; keys and values of the same type or e4m3.
-template <class T, class CT, int DP, bool EXACT> struct Pass {
-    static constexpr int kKeys = 32, kE = DP / 16, kTiles = DP / 16;
-    static constexpr bool k8 = __is_same(CT, e4m3);
-    static constexpr int kChunk = 16 / sizeof(CT);            // elements per 16-byte load of a key
-    static constexpr int kSteps = DP / (4 * kChunk);          // loads of a key per lane
-    static constexpr int kParts = kChunk / 8;                 // products per load
-    // fp16 ends at 2^-24: weights from 2^15 down keep a long tail of small
-    // ones, which together may weigh as much as the largest
-    static constexpr int kShift = __is_same(T, f16) ? 15 : 0;
-    // of a key that does not count: not 0, so that the attended value that
-    // stands in its place may be infinite
-    static constexpr float kLeast = __is_same(T, f16) ? 0x1p-24f : 0x1p-100f;
-    using Query = vec<T, 8>[kSteps * kParts];
-
-    using Keys = u32x4[2][kSteps];
-    using Values = vec<CT, kE>[8];
-
-    // negated for a negative scale
-    __device__ static void load_query(const Params &p, const T *q, bool used, int g, Query &out)
-    {
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-            for (int h = 0; h < kParts; ++h) {
-                const int at = (4 * s + g) * kChunk + 8 * h;
-                vec<T, 8> x = used && at < p.d ? *reinterpret_cast<const vec<T, 8> *>(q + at) : vec<T, 8>(0);
-                out[s * kParts + h] = p.scale < 0.0f ? -x : x;
-            }
-    }
-
-    // rows: where the tile's keys lie
-    template <class Rows> __device__ static void load_keys(const Params &p, const Rows &rows, int r, int g, Keys &x)
-    {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const CT *row = rows.key(t, r);
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                const int at = (4 * s + g) * kChunk;
-                x[t][s] = *reinterpret_cast<const u32x4 *>(row + (EXACT || at < p.d ? at : 0));
-            }
-        }
-    }
-
-    template <class Rows> __device__ static void load_values(const Params &p, const Rows &rows, int r, int g, Values &x)
-    {
-        const int at = EXACT || kE * r < p.d ? kE * r : 0;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                x[4 * t + i] = *reinterpret_cast<const vec<CT, kE> *>(rows.value(t, 4 * g + i) + at);
-    }
-
-    __device__ static vec<T, 8> part(u32x4 x, int h, bool in)
-    {
-        vec<T, 8> y;
-        if constexpr (k8) {
-            const uint32_t lo = h ? x[2] : x[0], hi = h ? x[3] : x[1];
-            y = widen8(lo, hi);
-        } else {
-            y = __builtin_bit_cast(vec<T, 8>, x);
-        }
-        return in ? y : vec<T, 8>(0);
-    }
-
-    // two of the four e4m3 of a word, exactly
-    template <bool HIGH> __device__ static vec<T, 2> widen2(uint32_t w)
-    {
-        if constexpr (__is_same(T, f16))
-            return __builtin_bit_cast(vec<T, 2>, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH));
-        else
-            return __builtin_bit_cast(vec<T, 2>, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HIGH));
-    }
-
-    __device__ static vec<T, 8> widen8(uint32_t lo, uint32_t hi)
-    {
-        const vec<T, 2> a = widen2<false>(lo), b = widen2<true>(lo), c = widen2<false>(hi), d = widen2<true>(hi);
-        return {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-    }
-
-    // A weight as the sum of two numbers of T: with one the output would carry
-    // an error as large as its own rounding.  The first is cut off, the
-    // second is never 0 (at least the type's smallest that the products keep,
-    // 2^-39 of the largest weight in fp16), so that an infinite value times
-    // both is that infinity.
-    __device__ static void split(const float (&s)[8], vec<T, 8> &hi, vec<T, 8> &lo)
-    {
-        vec<float, 8> rest;
-        if constexpr (__is_same(T, bf16)) {
-            vec<uint32_t, 4> w;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t bits = __builtin_bit_cast(uint32_t, s[i]);
-                rest[i] = fmaxf(s[i] - __builtin_bit_cast(float, bits & 0xffff0000u), 0x1p-126f);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                w[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, s[2 * i + 1]), __builtin_bit_cast(uint32_t, s[2 * i]),
-                                             0x07060302);
-            hi = __builtin_bit_cast(vec<T, 8>, w);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                const auto two = __builtin_amdgcn_cvt_pkrtz(s[i], s[i + 1]);
-                hi[i] = (T)two[0];
-                hi[i + 1] = (T)two[1];
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) rest[i] = fmaxf(s[i] - (float)hi[i], 0x1p-24f);
-        }
-        lo = __builtin_convertvector(rest, vec<T, 8>);
-    }
-
-    // products of the lane's keys 16 t + 4 g + i with query head r
-    __device__ static void scores(const Params &p, const Keys &x, const Query &q, int g, float (&s)[8])
-    {
-        // (products that need one another's result stand apart)
-        f32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i)
-#pragma unroll
-            for (int h = 0; h < kParts; ++h)
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-                    acc[t] = Mfma<T>::mul(part(x[t][i], h, EXACT || (4 * i + g) * kChunk < p.d), q[i * kParts + h], acc[t]);
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[4 * t + i] = acc[t][i];
-    }
-
-    // the values of those keys, times their weights
-    __device__ static void outputs(const Values &x, const float (&s)[8], State<kTiles> &st)
-    {
-        vec<T, 8> hi, lo;
-        split(s, hi, lo);
-        vec<T, kE> row[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) row[i] = to_t(x[i]);
-        constexpr int kTogether = 4;
-#pragma unroll
-        for (int e0 = 0; e0 < kE; e0 += kTogether) {
-            vec<T, 8> a[kTogether];
-#pragma unroll
-            for (int e = 0; e < kTogether; ++e)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) a[e][i] = row[i][e0 + e];
-#pragma unroll
-            for (int e = 0; e < kTogether; ++e) st.o[e0 + e] = Mfma<T>::mul(a[e], hi, st.o[e0 + e]);
-#pragma unroll
-            for (int e = 0; e < kTogether; ++e) st.o[e0 + e] = Mfma<T>::mul(a[e], lo, st.o[e0 + e]);
-        }
-    }
-
-    __device__ static vec<T, kE> to_t(vec<CT, kE> x)
-    {
-        if constexpr (k8) {
-            const auto w = __builtin_bit_cast(vec<uint32_t, kE / 4>, x);
-            vec<T, kE> y;
-#pragma unroll
-            for (int i = 0; i < kE / 4; ++i) {
-                const vec<T, 2> a = widen2<false>(w[i]), b = widen2<true>(w[i]);
-                y[4 * i] = a[0];
-                y[4 * i + 1] = a[1];
-                y[4 * i + 2] = b[0];
-                y[4 * i + 3] = b[1];
-            }
-            return y;
-        } else {
-            return x;
-        }
-    }
-
-    // the element of d that row 4 g + i of output product e stands for
-    __device__ static int dim(int g, int i, int e) { return (4 * g + i) * kE + e; }
-};
-
-// fp32: the same with products of four reduction indices, 16 keys a tile.
-template <int DP, bool EXACT> struct Pass<float, float, DP, EXACT> {
-    static constexpr int kKeys = 16, kTiles = DP / 16, kSteps = DP / 16, kQuads = DP / 64, kShift = 0;
-    using Query = f32x4[kSteps];
-
-    using Keys = f32x4[kSteps];
-    using Values = f32x4[4][kQuads];
-    static constexpr float kLeast = 0x1p-100f;
-
-    __device__ static void load_query(const Params &p, const float *q, bool used, int g, Query &out)
-    {
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const int at = (4 * s + g) * 4;
-            const f32x4 x = used && at < p.d ? *reinterpret_cast<const f32x4 *>(q + at) : f32x4{0, 0, 0, 0};
-            out[s] = p.scale < 0.0f ? -x : x;
-        }
-    }
-
-    template <class Rows> __device__ static void load_keys(const Params &p, const Rows &rows, int r, int g, Keys &x)
-    {
-        const float *row = rows.key(0, r);
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const int at = (4 * s + g) * 4;
-            x[s] = *reinterpret_cast<const f32x4 *>(row + (EXACT || at < p.d ? at : 0));
-        }
-    }
-
-    template <class Rows> __device__ static void load_values(const Params &p, const Rows &rows, int r, int g, Values &x)
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float *val = rows.value(0, 4 * g + i);
-#pragma unroll
-            for (int j = 0; j < kQuads; ++j) {
-                const int at = 64 * j + 4 * r;
-                x[i][j] = *reinterpret_cast<const f32x4 *>(val + (EXACT || at < p.d ? at : 0));
-            }
-        }
-    }
-
-    __device__ static void scores(const Params &p, const Keys &x, const Query &q, int g, float (&s)[4])
-    {
-        // four sums, so that no product waits for the one before
-        f32x4 acc[4] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const bool inside = EXACT || (4 * i + g) * 4 < p.d;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(inside ? x[i][e] : 0.0f, q[i][e], acc[e], 0, 0, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = (acc[0][i] + acc[1][i]) + (acc[2][i] + acc[3][i]);
-    }
-
-    __device__ static void outputs(const Values &x, const float (&s)[4], State<kTiles> &st)
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < kQuads; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    st.o[4 * j + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i][j][e], s[i], st.o[4 * j + e], 0, 0, 0);
-    }
-
-    __device__ static int dim(int g, int i, int e) { return 64 * (e / 4) + (4 * g + i) * 4 + e % 4; }
-};
-
-// Where the keys of a tile lie, in two steps so that the table's entries can
-// be on their way while an earlier tile is worked on: `fetch` reads the table
-// for the tile that begins at k0, `resolve` checks the pages and sets the
-// addresses.  A key outside the attended ones stands for the nearest of them,
-// so nothing else is read, neither of the table nor of the cache.
-// Pages of a multiple of 16 slots: 16 keys lie in one page, whose number and
-// address are the same for all lanes.
-template <class CT, int KEYS, bool WHOLE> struct Rows {
-    static constexpr int kN = KEYS / 16;
-    int32_t page[kN], slot[kN], low[kN], high[kN];
-    const CT *k[kN], *v[kN];
-    uint32_t slot_bytes;
-
-    __device__ void fetch(const Params &p, const int32_t *row, int32_t k0, int32_t first_key, int32_t len, int lane)
-    {
-#pragma unroll
-        for (int t = 0; t < kN; ++t) {
-            const int32_t key = min(max(k0 + 16 * t, first_key & ~15), (len - 1) & ~15);
-            const Place at = Place::of(p, key);
-            page[t] = row[at.page];
-            slot[t] = at.slot;
-            low[t] = max(first_key - key, 0);
-            high[t] = min(len - 1 - key, 15);
-        }
-    }
-    __device__ bool resolve(const Params &p, const CT *kb, const CT *vb)
-    {
-        slot_bytes = (uint32_t)p.slot_stride * (uint32_t)sizeof(CT);
-        bool ok = true;
-#pragma unroll
-        for (int t = 0; t < kN; ++t) {
-            ok &= page[t] >= 0 && page[t] < p.n_pages;
-            const int64_t off = page[t] * p.page_stride + slot[t] * p.slot_stride;
-            k[t] = kb + off;
-            v[t] = vb + off;
-        }
-        return ok;
-    }
-    __device__ const CT *at(const CT *base, int t, int i) const
-    {
-        return reinterpret_cast<const CT *>(reinterpret_cast<const char *>(base) +
-                                            __umul24(min(max(i, low[t]), high[t]), slot_bytes));
-    }
-    __device__ const CT *key(int t, int i) const { return at(k[t], t, i); }
-    __device__ const CT *value(int t, int i) const { return at(v[t], t, i); }
-};
-
-// Any page size: lane l holds the place of key l % KEYS.
-template <class CT, int KEYS> struct Rows<CT, KEYS, false> {
-    int32_t page, slot;
-    int64_t off;
-    const CT *kb, *vb;
-
-    __device__ void fetch(const Params &p, const int32_t *row, int32_t k0, int32_t first_key, int32_t len, int lane)
-    {
-        const Place at = Place::of(p, min(max(k0 + lane % KEYS, first_key), len - 1));
-        page = row[at.page];
-        slot = at.slot;
-    }
-    __device__ bool resolve(const Params &p, const CT *kbase, const CT *vbase)
-    {
-        const bool ok = page >= 0 && page < p.n_pages;
-        off = page * p.page_stride + slot * p.slot_stride;
-        kb = kbase;
-        vb = vbase;
-        return __builtin_amdgcn_ballot_w64(!ok) == 0;
-    }
-    __device__ const CT *key(int t, int i) const { return kb + __shfl(off, 16 * t + i); }
-    __device__ const CT *value(int t, int i) const { return vb + __shfl(off, 16 * t + i); }
-};
-
-// Four elements of a result row: out = x / l, or what a row without keys or
-// with an error has.
-template <class T>
-__device__ inline void write_row(const Params &p, int b, int head, int d, f32x4 x, float l, bool empty, int32_t bad)
-{
-#pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = bad ? __builtin_nanf("") : empty ? 0.0f : x[k] / l;
-    *reinterpret_cast<vec<T, 4> *>(static_cast<T *>(p.out) + b * p.out_row + head * p.out_head + d) = from_f32<T, 4>(x);
-}
-
-template <int SHIFT>
-__device__ inline void write_lse(const Params &p, int b, int head, float m, float l, bool empty, int32_t bad)
-{
-    if (p.lse)
-        p.lse[(int64_t)b * p.n_q_heads + head] =
-            bad ? __builtin_nanf("") : empty ? -HUGE_VALF : (m + (__builtin_log2f(l) - SHIFT)) * kLn2;
-}
-
-// A part of a context: d outputs of each head, then the heads' maxima and
-// sums; 16-byte aligned.
-__host__ __device__ inline int64_t part_size(int heads, int d) { return (int64_t)heads * d + (2 * heads + 3) / 4 * 4; }
-
-struct Part {
-    float *o, *m, *l;
-    __device__ static Part of(const Params &p, int64_t slot)
-    {
-        float *o = p.part + slot * part_size(p.part_heads, p.d), *m = o + p.part_heads * p.d;
-        return {o, m, m + p.part_heads};
-    }
-};
-
-// The tiles of all contexts -- (sequence, cache head, tile of 16 query heads)
-// -- are laid end to end, each context behind kExtra that stand for its
-// beginning and end, and cut into equal runs, one per workgroup; a workgroup's waves
-// take the tiles of each context in turn and are joined in shared memory.  A
-// context that lies in one run is finished here; the parts of the others go
-// to the workspace (slot 0: a context begun by an earlier workgroup, slot 1:
-// one that a later workgroup goes on with) for k_join.
-template <class T, class CT, int DP, bool WHOLE, bool EXACT>
-__global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Params p)
-{
-    using P = Pass<T, CT, DP, EXACT>;
-    constexpr int kKeys = P::kKeys, NT = P::kTiles, kPad = DP + 4;
-    __shared__ float s_o[kWaves][kTileHeads][kPad];
-    __shared__ float s_m[kWaves][kTileHeads], s_l[kWaves][kTileHeads], s_top[kTileHeads];
-    __shared__ int64_t s_sum[kWaves];
-    __shared__ int32_t s_seq, s_len, s_bad[2];
-    __shared__ int64_t s_at;
-    const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int units = p.n_heads * p.tiles_of_heads;   // contexts per sequence
-
-    int b, unit, c0 = 0;
-    int64_t left, run = 0;
-    Span<kKeys> sp;
-    if (tid < 2) s_bad[tid] = 0;
-    if (p.direct) {
-        b = blockIdx.x / units;
-        unit = blockIdx.x - b * units;
-        sp = Span<kKeys>::of(p, p.seq_len[b]);
-        left = sp.cost();
-        __syncthreads();
-    } else {
-        // this workgroup's run: tiles counted per thread, summed over the block
-        const int per = (p.n_seq + kBlock - 1) / kBlock, lo = tid * per, hi = min(p.n_seq, lo + per);
-        int64_t mine = 0;
-        for (int b = lo; b < hi; ++b) mine += Span<kKeys>::of(p, p.seq_len[b]).cost();
-        int64_t incl = mine;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int64_t x = __shfl_up(incl, o);
-            if (lane >= o) incl += x;
-        }
-        if (lane == 63) s_sum[wave] = incl;
-        __syncthreads();
-        int64_t total = 0, before = 0;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            if (w < wave) before += s_sum[w];
-            total += s_sum[w];
-        }
-        total = uniform(total) * units;
-        constexpr int kRuns = kCus * per_cu(DP, sizeof(CT));   // the grid
-        const int64_t even = (total + kRuns - 1) / kRuns;
-        run = even > kExtra + kMinTiles ? even : kExtra + kMinTiles;
-        const int64_t begin = blockIdx.x * run;
-        if (begin >= total) {
-            if (tid == 0 && !p.by_context) p.cut[blockIdx.x] = make_int4(0, 0, 0, 0);
-            return;
-        }
-        const int64_t end = begin + run < total ? begin + run : total;
-        const int64_t excl = (before + incl - mine) * units;
-        if (begin >= excl && begin < excl + mine * units) {
-            int64_t at = excl;
-            for (int b = lo; b < hi; ++b) {
-                const int32_t len = p.seq_len[b];
-                const int64_t n = (int64_t)Span<kKeys>::of(p, len).cost() * units;
-                if (begin < at + n) {
-                    s_seq = b;
-                    s_len = len;
-                    s_at = begin - at;
-                    break;
-                }
-                at += n;
-            }
-        }
-        __syncthreads();
-        b = __builtin_amdgcn_readfirstlane(s_seq);
-        sp = Span<kKeys>::of(p, __builtin_amdgcn_readfirstlane(s_len));
-        left = end - begin;
-        {
-            const int64_t at = uniform(s_at);
-            const int cost = sp.cost();
-            unit = at >> 32 == 0 ? (int)((uint32_t)at / (uint32_t)cost) : (int)(at / cost);   // (64 bits take 0.3 us)
-            c0 = (int)(at - (int64_t)unit * cost);
-        }
-    }
-    int4 cut = make_int4(0, 0, 0, 0);
-    int turn = 0;
-
-    for (; left > 0; ++unit, c0 = 0) {
-        while (unit == units || sp.n == 0) {   // the next sequence (one may be left alone)
-            sp = Span<kKeys>::of(p, p.seq_len[++b]);
-            unit = 0;
-        }
-        const int cost = sp.cost(), c1 = (int)(cost - c0 < left ? cost : c0 + left);
-        left -= c1 - c0;
-        const int t0 = max(c0 - kExtra, 0), n = max(c1 - kExtra, 0) - t0;
-        if (n == 0) continue;   // the next run begins the context
-        const int kv = p.tiles_of_heads == 1 ? unit : unit / p.tiles_of_heads;
-        const int hb = (unit - kv * p.tiles_of_heads) * kTileHeads;
-        const int heads = min(kTileHeads, p.group - hb), q0 = kv * p.group + hb;
-        const bool whole = n == sp.n;
-        const int32_t *row = p.table + b * p.table_stride;
-
-        State<NT> st;
-        st.m = -HUGE_VALF;
-        st.l = 0.0f;
-#pragma unroll
-        for (int e = 0; e < NT; ++e) st.o[e] = f32x4{0, 0, 0, 0};
-        if (sp.len > 0) {
-            typename P::Query q;
-            P::load_query(p, static_cast<const T *>(p.q) + b * p.q_row + (q0 + (r < heads ? r : 0)) * p.q_head,
-                          r < heads, g, q);
-            // (not 0, which times the -inf of a key that does not count were NaN)
-            const float scale = fmaxf(fabsf(p.scale) * (p.k_scale ? p.k_scale[kv] : 1.0f), 0x1p-120f);
-            const CT *kb = static_cast<const CT *>(p.k) + kv * p.head_stride;
-            const CT *vb = static_cast<const CT *>(p.v) + kv * p.head_stride;
-            // The next tile's keys are on their way as soon as the scores are
-            // known, its values as soon as the outputs are; the table's
-            // entries a tile ahead of both.
-            typename P::Keys keys;
-            typename P::Values values;
-            Rows<CT, kKeys, WHOLE> rows;
-            const int last = t0 + n;
-            auto fetch = [&](int t) {
-                rows.fetch(p, row, (sp.first_tile + min(t, last - 1)) * kKeys, sp.first_key, sp.len, lane);
-            };
-            bool ok = true;
-            int t = t0 + wave;
-            if (t < last) {
-                fetch(t);
-                ok = rows.resolve(p, kb, vb);
-                if (ok) {
-                    P::load_keys(p, rows, r, g, keys);
-                    P::load_values(p, rows, r, g, values);
-                    fetch(t + kWaves);
-                }
-            }
-            while (ok && t < last) {
-                const int next = t + kWaves;
-                if (next < last) ok = rows.resolve(p, kb, vb);
-                const bool more = ok && next < last;
-                const int k0 = (sp.first_tile + t) * kKeys;
-                const bool all = k0 >= sp.first_key && sp.len - k0 >= kKeys;
-                uint32_t in = 0;
-                if (!all) {
-#pragma unroll
-                    for (int i = 0; i < kKeys / 4; ++i) {
-                        const int j = k0 + i / 4 * 16 + 4 * g + i % 4;
-                        if (j >= sp.first_key && j < sp.len) in |= 1u << i;
-                    }
-                }
-                float s[kKeys / 4];
-                P::scores(p, keys, q, g, s);
-                if (more) P::load_keys(p, rows, r, g, keys);
-                weigh<P::kShift>(s, scale, all, in, P::kLeast, st);
-                P::outputs(values, s, st);
-                if (more) {
-                    P::load_values(p, rows, r, g, values);
-                    fetch(next + kWaves);
-                }
-                t = next;
-            }
-            if (!ok) s_bad[turn] = DSIM_ST_BAD_PAGE;
-        }
-
-        // Join the waves.  Two barriers a context: what the next one writes
-        // before its first is not read after this one's second, but for
-        // s_bad, which takes turns.
-        const float l = sum_groups(st.l);
-        if (g == 0) s_m[wave][r] = st.m;
-        __syncthreads();
-        float top = s_m[0][r];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
-        const float f = rescale(st.m, top);
-        if (r < heads) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int e = 0; e < NT; e += 4)
-                    *reinterpret_cast<f32x4 *>(&s_o[wave][r][P::dim(g, i, e)]) =
-                        f32x4{st.o[e][i], st.o[e + 1][i], st.o[e + 2][i], st.o[e + 3][i]} * f;
-        }
-        if (g == 0) {
-            s_l[wave][r] = l * f;
-            if (wave == 0) s_top[r] = top;
-        }
-        if (tid == 0) s_bad[turn ^ 1] = 0;
-        __syncthreads();
-        const int32_t bad = sp.bad ? DSIM_ST_BAD_POSITION : s_bad[turn];
-        turn ^= 1;
-        const Part part = Part::of(p, 2 * blockIdx.x + (t0 == 0 ? 1 : 0));
-        const float vs = p.v_scale ? p.v_scale[kv] : 1.0f;
-        const int quads = EXACT ? DP / 4 : p.d / 4;
-        for (int i = tid; i < heads * quads; i += kBlock) {
-            const int h = i / quads, d = 4 * (i - h * quads);
-            float sum = s_l[0][h];
-            f32x4 o = *reinterpret_cast<const f32x4 *>(&s_o[0][h][d]);
-#pragma unroll
-            for (int w = 1; w < kWaves; ++w) {
-                sum += s_l[w][h];
-                o += *reinterpret_cast<const f32x4 *>(&s_o[w][h][d]);
-            }
-            o *= vs;
-            if (whole) {
-                write_row<T>(p, b, q0 + h, d, o, sum, sp.len == 0, bad);
-                if (d == 0) write_lse<P::kShift>(p, b, q0 + h, s_top[h], sum, sp.len == 0, bad);
-            } else {
-                *reinterpret_cast<f32x4 *>(part.o + h * p.d + d) = o;
-                if (d == 0) {
-                    part.m[h] = s_top[h];
-                    part.l[h] = bad ? -1.0f : sum;   // (a sum is never negative)
-                }
-            }
-        }
-        if (whole && tid == 0 && p.status) p.status[b] = bad;
-        if (t0 == 0) {
-            // parts: this one, then the runs of the workgroups behind, the
-            // last possibly short; 0 if nothing is cut off
-            cut = make_int4(whole ? 0 : 1 + (int)((sp.n - n + run - 1) / run), b, q0, (int)blockIdx.x);
-            if (p.by_context && tid == 0) p.cut[b * units + unit] = cut;
-        }
-    }
-    if (tid == 0 && !p.by_context && !p.direct) p.cut[blockIdx.x] = cut;
-}
-
-// Joins the parts of the contexts that are cut.  W = 1: a wave takes a head
-// of a context; W = 4: four waves take a quarter of its outputs.  Their
-// threads are `ways` rows, row w taking four elements each of the parts w,
-// w + ways, ...  The first of those are on their way before the weights they
-// get are known.
-template <class T, int SHIFT, int W> __global__ __launch_bounds__(kBlock) void k_join(Params p)
-{
-    constexpr int kThreads = 64 * W, kHeads = kBlock / kThreads, kAhead = 8;
-    __shared__ float s_m[kWaves], s_l[kWaves];
-    __shared__ int s_wrong[kWaves];
-    __shared__ f32x4 s_o[kBlock];
-    const int4 cut = p.cut[blockIdx.x];
-    const int n = cut.x, b = cut.y, q0 = cut.z, w0 = cut.w;
-    const int tid = threadIdx.x % kThreads, lane = tid & 63, wave = threadIdx.x / 64, mine = threadIdx.x / kThreads;
-    const int h = blockIdx.y * kHeads + mine, first = wave / W * W;
-    // (nobody begins the context of a row that is left alone)
-    if (p.by_context && p.seq_len[blockIdx.x / (p.n_heads * p.tiles_of_heads)] < 0) return;
-    if (n == 0) return;
-    const bool used = h < p.part_heads && q0 + h < (q0 / p.group + 1) * p.group;   // (a last tile may have fewer heads)
-    auto part = [&](int i) { return Part::of(p, i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)); };
-    const int quads = p.d / 4 / W, ways = kThreads / quads, way = tid / quads;
-    const int d0 = 4 * (tid - way * quads + (int)blockIdx.z * quads);
-    const int count = used && way < ways ? n : 0;
-    auto output = [&](int i) { return *reinterpret_cast<const f32x4 *>(part(i).o + h * p.d + d0); };
-    f32x4 ahead[kAhead];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-        if (way + j * ways < count) ahead[j] = output(way + j * ways);
-
-    float m = -HUGE_VALF;
-    int wrong = 0;
-    for (int i = tid; used && i < n; i += kThreads) {
-        m = fmaxf(m, part(i).m[h]);
-        wrong |= part(i).l[h] < 0.0f;
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-    wrong = __builtin_amdgcn_ballot_w64(wrong) != 0;
-    if (W > 1) {
-        if (lane == 0) {
-            s_m[wave] = m;
-            s_wrong[wave] = wrong;
-        }
-        __syncthreads();
-        for (int w = first; w < first + W; ++w) {
-            m = fmaxf(m, s_m[w]);
-            wrong |= s_wrong[w];
-        }
-    }
-    float l = 0.0f;
-    for (int i = tid; used && i < n; i += kThreads) l += rescale(part(i).m[h], m) * part(i).l[h];
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o);
-    f32x4 o = {0, 0, 0, 0};
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-        if (way + j * ways < count) o += rescale(part(way + j * ways).m[h], m) * ahead[j];
-#pragma unroll 4
-    for (int i = way + kAhead * ways; i < count; i += ways) o += rescale(part(i).m[h], m) * output(i);
-    s_o[threadIdx.x] = o;
-    if (lane == 0) s_l[wave] = l;
-    __syncthreads();
-    if (!used) return;
-    l = 0.0f;
-    for (int w = first; w < first + W; ++w) l += s_l[w];
-    const int32_t bad = wrong ? DSIM_ST_BAD_PAGE : 0;
-    if (tid < quads) {
-        for (int w = 1; w < ways; ++w) o += s_o[mine * kThreads + w * quads + tid];
-        write_row<T>(p, b, q0 + h, d0, o, l, false, bad);
-    }
-    if (tid == 0 && blockIdx.z == 0) {
-        write_lse<SHIFT>(p, b, q0 + h, m, l, false, bad);
-        if (p.status) p.status[b] = bad;
-    }
-}
-
-template <class T, class CT, int DP> dsim_status launch(Params &p, hipStream_t s)
-{
-    const int64_t contexts = (int64_t)p.n_seq * p.n_heads * p.tiles_of_heads;
-    p.grid = kCus * per_cu(DP, sizeof(CT));
-    // Contexts that cannot be long (the block table has no room, or the window
-    // is short) take a workgroup each and need neither the cut nor the join:
-    // up to 32 tiles (fp32, whose products take longer than its loads: 16).
-    // bf16, 8 cache heads of 128, up to 512 tokens: one sequence 11.0 us (cut
-    // 15.2), 256 67.6 (71.1); up to 2,048: one 25.6 (15.6), 64 63.4 (64.3).
-    // fp32, 12 heads of 80, up to 256 tokens: one 13.9 (18.1), 256 96 (94);
-    // up to 512: one 20.8 (18.3), 256 149 (141).
-    constexpr int kKeys = Pass<T, CT, DP, true>::kKeys;
-    int64_t most = (int64_t)p.table_width * p.page_size;
-    if (p.window > 0 && p.window + kKeys < most) most = p.window + kKeys;
-    p.direct = most <= (sizeof(CT) == 4 ? 16 : 32) * kKeys && contexts < 1 << 24;
-    p.by_context = !p.direct && contexts <= p.grid;
-    const dim3 grid((unsigned)(p.direct ? contexts : p.grid)), block(kBlock);
-    // 16 slots of a page at offsets of 24-bit products
-    const bool whole = p.page_size % 16 == 0 && p.slot_stride * (int64_t)sizeof(CT) < 1 << 24;
-    if (whole && p.d == DP)
-        hipLaunchKernelGGL((k_attend<T, CT, DP, true, true>), grid, block, 0, s, p);
-    else if (whole)
-        hipLaunchKernelGGL((k_attend<T, CT, DP, true, false>), grid, block, 0, s, p);
-    else
-        hipLaunchKernelGGL((k_attend<T, CT, DP, false, false>), grid, block, 0, s, p);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return hip_fail(e, "paged attention launch");
-    if (p.direct) return DSIM_OK;
-    // few contexts have many parts each
-    constexpr int kShift = Pass<T, CT, DP, true>::kShift;
-    const unsigned x = (unsigned)(p.by_context ? contexts : p.grid), heads = (unsigned)p.part_heads;
-    if (contexts * 32 <= p.grid)
-        hipLaunchKernelGGL((k_join<T, kShift, 4>), dim3(x, heads, 4), block, 0, s, p);
-    else
-        hipLaunchKernelGGL((k_join<T, kShift, 1>), dim3(x, (heads + 3) / 4), block, 0, s, p);
-    e = hipGetLastError();
-    return e == hipSuccess ? DSIM_OK : hip_fail(e, "paged attention join launch");
-}
-
-template <class T, class CT> dsim_status launch(Params &p, hipStream_t s)
-{
-    return p.d <= 64 ? launch<T, CT, 64>(p, s) : p.d <= 128 ? launch<T, CT, 128>(p, s) : launch<T, CT, 256>(p, s);
-}
-
-}  // namespace
 
 size_t attend_workspace(int32_t n_q_heads, int32_t n_heads, int32_t head_dim)
 {
+    using namespace attend;
     const int group = n_q_heads / n_heads, heads = group < kTileHeads ? group : kTileHeads;
     return (size_t)kMaxGrid * (sizeof(int4) + 2 * (size_t)part_size(heads, head_dim) * sizeof(float));
 }
 
 dsim_status launch_attend(const AttendArgs &a, hipStream_t s)
 {
+    using namespace attend;
     Params p{};
     p.k = a.c.k;
     p.v = a.c.v;
@@ -927,9 +52,8 @@ dsim_status launch_attend(const AttendArgs &a, hipStream_t s)
     p.group = a.n_q_heads / a.c.n_heads;
     p.tiles_of_heads = (p.group + kTileHeads - 1) / kTileHeads;
     p.part_heads = p.group < kTileHeads ? p.group : kTileHeads;
-    if (a.dtype == DSIM_F32) return launch<float, float>(p, s);
-    if (a.dtype == DSIM_F16) return a.c.dtype == DSIM_E4M3 ? launch<f16, e4m3>(p, s) : launch<f16, f16>(p, s);
-    return a.c.dtype == DSIM_E4M3 ? launch<bf16, e4m3>(p, s) : launch<bf16, bf16>(p, s);
+    if (a.dtype == DSIM_F32) return attend::launch_f32(p, s);
+    return (a.dtype == DSIM_F16 ? attend::launch_f16 : attend::launch_bf16)(p, a.c.dtype == DSIM_E4M3, s);
 }
 
 }  // namespace dsim

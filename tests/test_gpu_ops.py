@@ -331,6 +331,41 @@ def test_attend_many_contexts_and_cuts():
     check_attend(BF16, E4M3, 36, 9, 64, 16, lens, window=3000)
 
 
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("slots", [16, 7])
+def test_attend_large_cache(dtype, cache, slots):
+    """A few sequences in a cache that is larger than the last-level cache,
+    with block tables that have room for much of it (keys and values are then
+    read past the caches)."""
+    heads, d, lens = 4, 128, [1, 50, 3000, 0, 700]
+    e = torch.tensor([], dtype=cache).element_size()
+    pages = 320_000_000 // (2 * slots * heads * d * e)
+    g = gen(slots)
+    big = ops.alloc_kv_cache(pages, slots, heads, d, cache)
+    counts = [-(-n // slots) for n in lens]
+    used = torch.randperm(pages, generator=g)[:sum(counts)]
+    table = torch.zeros(len(lens), pages, dtype=torch.int32)
+    near = torch.zeros(len(lens), max(counts), dtype=torch.int32)   # the same pages numbered from 0
+    at = 0
+    for b, c in enumerate(counts):
+        table[b, :c] = used[at:at + c].to(torch.int32)
+        near[b, :c] = torch.arange(at, at + c)
+        at += c
+    keys, values = cache_like(g, len(used), slots, heads, d, F32 if cache == E4M3 else cache, "slot")
+    keys, values = keys.to(cache), values.to(cache)
+    for c, x in ((big["k"], keys), (big["v"], values)):
+        if cache == E4M3:
+            c.view(torch.uint8)[used.cuda()] = x.view(torch.uint8).cuda()
+        else:
+            c[used.cuda()] = x.cuda()
+    q = (2 * randn(g, len(lens), 8, d)).to(dtype)
+    out = torch.empty(q.shape, dtype=dtype, device="cuda")
+    ops.dsim_paged_attention(q.cuda(), big, table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), out)
+    ref, _, bound = plain.attend(q, keys, values, near, torch.tensor(lens), d ** -0.5)
+    room = bound + (ref.abs() + bound) * plain.HALF_STEP[dtype] + (2.0 ** -25 if dtype == F16 else 0)
+    assert torch.all((out.cpu().double() - ref).abs() <= room)
+
+
 def test_attend_shared_pages():
     """Sequences that share their first pages."""
     g = gen(12)
