@@ -97,13 +97,6 @@ template <int KEYS> struct Span {
     }
 };
 
-// Running state of one wave: for column r (a query head) the maximum m, this
-// lane's share of the sum l, and the output's rows.
-template <int NT> struct State {
-    float m, l;
-    f32x4 o[NT];
-};
-
 // a value that is the same for all lanes, in scalar registers
 __device__ inline int64_t uniform(int64_t x)
 {
@@ -123,6 +116,17 @@ __device__ inline vec<float, 2> other_row(float x)
 {
     const auto y = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
     return {__builtin_bit_cast(float, (uint32_t)y[0]), __builtin_bit_cast(float, (uint32_t)y[1])};
+}
+
+// Within each row of 16 lanes: the value N lanes on, and lane N's.
+template <int N> __device__ inline float turn(float x)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x120 + N, 0xf, 0xf, true));
+}
+
+template <int N> __device__ inline float spread(float x)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x150 + N, 0xf, 0xf, true));
 }
 
 __device__ inline float max_groups(float x)
@@ -147,12 +151,27 @@ __device__ inline float rescale(float from, float to)
     return from == -HUGE_VALF ? 1.0f : __builtin_amdgcn_exp2f(from - to);
 }
 
+// Running state of one wave: for column r (a query head) the maximum m, this
+// lane's share of the sum l, and the output's rows.
+template <int NT> struct Columns {
+    float m, l;
+    f32x4 o[NT];
+    __device__ void clear()
+    {
+        m = -HUGE_VALF;
+        l = 0.0f;
+#pragma unroll
+        for (int e = 0; e < NT; ++e) o[e] = f32x4{0, 0, 0, 0};
+    }
+    __device__ float sum() const { return sum_groups(l); }
+};
+
 // The running maximum takes in the products s; returns them as weights, 2^SHIFT
 // for one at the maximum.  scale > 0: base-2 logarithms per unit of s.  `in`:
 // bit i says whether s[i] counts (looked at unless `all`); one that does not
 // becomes the weight `least` and adds nothing to the sum.
 template <int SHIFT, int N, int NT>
-__device__ inline void weigh(float (&s)[N], float scale, bool all, uint32_t in, float least, State<NT> &st)
+__device__ inline void weigh(float (&s)[N], float scale, bool all, uint32_t in, float least, Columns<NT> &st)
 {
     if (!all) {
 #pragma unroll
@@ -188,9 +207,36 @@ template <bool STREAM, class V> __device__ inline V read(const void *p)
     return STREAM ? __builtin_nontemporal_load(static_cast<const V *>(p)) : *static_cast<const V *>(p);
 }
 
+// What the passes by columns share.  DIM: see dim() of each.
+template <class P, int DP, int KEYS> struct ByColumns {
+    static constexpr int kMine = KEYS / 4;   // keys that a lane has the scores of
+    using State = Columns<DP / 16>;
+
+    // the lane's key i in the tile
+    __device__ static int key(int i, int r, int g) { return i / 4 * 16 + 4 * g + i % 4; }
+
+    __device__ static void weigh(float (&s)[kMine], float scale, bool all, uint32_t in, State &st)
+    {
+        attend::weigh<P::kShift>(s, scale, all, in, P::kLeast, st);
+    }
+
+    // the outputs times f to shared memory, a row per head
+    template <int PAD> __device__ static void store(const State &st, float f, float (*o)[PAD], int heads, int r, int g)
+    {
+        if (r >= heads) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < DP / 16; e += 4)
+                *reinterpret_cast<f32x4 *>(&o[r][P::dim(g, i, e)]) =
+                    f32x4{st.o[e][i], st.o[e + 1][i], st.o[e + 2][i], st.o[e + 3][i]} * f;
+    }
+};
+
 // 16-bit queries; keys and values of the same type or e4m3.
-template <class T, class CT, int DP, bool EXACT, bool STREAM> struct Pass {
-    static constexpr int kKeys = 32, kE = DP / 16, kTiles = DP / 16;
+template <class T, class CT, int DP, bool EXACT, bool STREAM>
+struct Pass : ByColumns<Pass<T, CT, DP, EXACT, STREAM>, DP, 32> {
+    static constexpr int kKeys = 32, kE = DP / 16;
     static constexpr bool k8 = __is_same(CT, e4m3);
     static constexpr int kChunk = 16 / sizeof(CT);            // elements per 16-byte load of a key
     static constexpr int kSteps = DP / (4 * kChunk);          // loads of a key per lane
@@ -322,7 +368,7 @@ template <class T, class CT, int DP, bool EXACT, bool STREAM> struct Pass {
     }
 
     // the values of those keys, times their weights
-    __device__ static void outputs(const Values &x, const float (&s)[8], State<kTiles> &st)
+    __device__ static void outputs(const Values &x, const float (&s)[8], Columns<DP / 16> &st)
     {
         vec<T, 8> hi, lo;
         split(s, hi, lo);
@@ -368,8 +414,9 @@ template <class T, class CT, int DP, bool EXACT, bool STREAM> struct Pass {
 };
 
 // fp32: the same with products of four reduction indices, 16 keys a tile.
-template <int DP, bool EXACT, bool STREAM> struct Pass<float, float, DP, EXACT, STREAM> {
-    static constexpr int kKeys = 16, kTiles = DP / 16, kSteps = DP / 16, kQuads = DP / 64, kShift = 0;
+template <int DP, bool EXACT, bool STREAM>
+struct Pass<float, float, DP, EXACT, STREAM> : ByColumns<Pass<float, float, DP, EXACT, STREAM>, DP, 16> {
+    static constexpr int kKeys = 16, kSteps = DP / 16, kQuads = DP / 64, kShift = 0;
     using Query = f32x4[kSteps];
 
     using Keys = f32x4[kSteps];
@@ -424,7 +471,7 @@ template <int DP, bool EXACT, bool STREAM> struct Pass<float, float, DP, EXACT, 
         for (int i = 0; i < 4; ++i) s[i] = (acc[0][i] + acc[1][i]) + (acc[2][i] + acc[3][i]);
     }
 
-    __device__ static void outputs(const Values &x, const float (&s)[4], State<kTiles> &st)
+    __device__ static void outputs(const Values &x, const float (&s)[4], Columns<DP / 16> &st)
     {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -436,6 +483,108 @@ template <int DP, bool EXACT, bool STREAM> struct Pass<float, float, DP, EXACT, 
     }
 
     __device__ static int dim(int g, int i, int e) { return 64 * (e / 4) + (4 * g + i) * 4 + e % 4; }
+};
+
+// fp32, a cache head with one query head: fifteen of the matrix instructions'
+// sixteen columns would be empty, and in fp32 they are slow enough to show
+// (16 sequences of 12 heads of 80, window 1,000: 35.3 us, this way 29.3; 256
+// of up to 64 tokens 51 and 42; 64 of up to 4,096 the same), so the products
+// are ordinary ones.  Keys and values lie as above; a lane sums its
+// chunks of key r's product, the groups' sums are added, and the weights of
+// its own keys 4 g + i come from its row's lanes.
+template <int DP, bool EXACT, bool STREAM> struct OnePass : Pass<float, float, DP, EXACT, STREAM> {
+    using Base = Pass<float, float, DP, EXACT, STREAM>;
+    using Base::kQuads;
+    using Base::kSteps;
+    static constexpr int kMine = 1;
+
+    struct State {
+        float m, l;
+        f32x4 o[kQuads];
+        __device__ void clear()
+        {
+            m = -HUGE_VALF;
+            l = 0.0f;
+#pragma unroll
+            for (int j = 0; j < kQuads; ++j) o[j] = f32x4{0, 0, 0, 0};
+        }
+        // over a row, whose lanes have a key each (every row has the same)
+        __device__ float sum() const
+        {
+            float x = l;
+            x += turn<8>(x);
+            x += turn<4>(x);
+            x += turn<2>(x);
+            return x + turn<1>(x);
+        }
+    };
+
+    __device__ static int key(int i, int r, int g) { return r; }
+
+    // (every row's lanes take the one head)
+    __device__ static void load_query(const Params &p, const float *q, bool used, int g, typename Base::Query &out)
+    {
+        Base::load_query(p, q, true, g, out);
+    }
+
+    __device__ static void scores(const Params &p, const typename Base::Keys &x, const typename Base::Query &q, int g,
+                                  float (&s)[1])
+    {
+        f32x4 sum = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            const bool inside = EXACT || (4 * i + g) * 4 < p.d;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] = __builtin_fmaf(inside ? x[i][e] : 0.0f, q[i][e], sum[e]);
+        }
+        s[0] = sum_groups((sum[0] + sum[1]) + (sum[2] + sum[3]));
+    }
+
+    __device__ static void weigh(float (&s)[1], float scale, bool all, uint32_t in, State &st)
+    {
+        const bool counts = all || (in & 1);
+        float top = counts ? s[0] : -HUGE_VALF;
+        top = fmaxf(top, turn<8>(top));
+        top = fmaxf(top, turn<4>(top));
+        top = fmaxf(top, turn<2>(top));
+        top = fmaxf(top, turn<1>(top)) * scale;
+        if (__builtin_amdgcn_ballot_w64(top > st.m) != 0) {
+            const float m = fmaxf(st.m, top), f = rescale(st.m, m);
+            st.l *= f;
+#pragma unroll
+            for (int j = 0; j < kQuads; ++j) st.o[j] *= f;
+            st.m = m;
+        }
+        const float m = st.m == -HUGE_VALF ? 0.0f : st.m;
+        s[0] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0], scale, -m));
+        st.l += counts ? s[0] : 0.0f;
+        s[0] = counts ? s[0] : Base::kLeast;
+    }
+
+    __device__ static void outputs(const typename Base::Values &x, const float (&s)[1], State &st)
+    {
+        // key 4 g + i's weight to lane i of row g, and from there to the row
+        const int lane = threadIdx.x & 63;
+        const float mine = __shfl(s[0], (lane / 16 * 4 + lane) % 16);
+        const float w[4] = {spread<0>(mine), spread<1>(mine), spread<2>(mine), spread<3>(mine)};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < kQuads; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) st.o[j][e] = __builtin_fmaf(w[i], x[i][j][e], st.o[j][e]);
+    }
+
+    template <int PAD> __device__ static void store(const State &st, float f, float (*o)[PAD], int heads, int r, int g)
+    {
+#pragma unroll
+        for (int j = 0; j < kQuads; ++j) {
+            f32x4 x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = sum_groups(st.o[j][e]) * f;
+            if (g == 0) *reinterpret_cast<f32x4 *>(&o[0][64 * j + 4 * r]) = x;
+        }
+    }
 };
 
 // Where the keys of a tile lie, in two steps so that the table's entries can
@@ -547,11 +696,10 @@ struct Part {
 // context that lies in one run is finished here; the parts of the others go
 // to the workspace (slot 0: a context begun by an earlier workgroup, slot 1:
 // one that a later workgroup goes on with) for k_join.
-template <class T, class CT, int DP, bool WHOLE, bool EXACT, bool STREAM>
+template <class P, class T, class CT, int DP, bool WHOLE, bool EXACT>
 __global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Params p)
 {
-    using P = Pass<T, CT, DP, EXACT, STREAM>;
-    constexpr int kKeys = P::kKeys, NT = P::kTiles, kPad = DP + 4;
+    constexpr int kKeys = P::kKeys, kPad = DP + 4;
     __shared__ float s_o[kWaves][kTileHeads][kPad];
     __shared__ float s_m[kWaves][kTileHeads], s_l[kWaves][kTileHeads], s_top[kTileHeads];
     __shared__ int64_t s_sum[kWaves];
@@ -644,11 +792,8 @@ __global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Param
         const bool whole = n == sp.n;
         const int32_t *row = p.table + b * p.table_stride;
 
-        State<NT> st;
-        st.m = -HUGE_VALF;
-        st.l = 0.0f;
-#pragma unroll
-        for (int e = 0; e < NT; ++e) st.o[e] = f32x4{0, 0, 0, 0};
+        typename P::State st;
+        st.clear();
         if (sp.len > 0) {
             typename P::Query q;
             P::load_query(p, static_cast<const T *>(p.q) + b * p.q_row + (q0 + (r < heads ? r : 0)) * p.q_head,
@@ -687,15 +832,15 @@ __global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Param
                 uint32_t in = 0;
                 if (!all) {
 #pragma unroll
-                    for (int i = 0; i < kKeys / 4; ++i) {
-                        const int j = k0 + i / 4 * 16 + 4 * g + i % 4;
+                    for (int i = 0; i < P::kMine; ++i) {
+                        const int j = k0 + P::key(i, r, g);
                         if (j >= sp.first_key && j < sp.len) in |= 1u << i;
                     }
                 }
-                float s[kKeys / 4];
+                float s[P::kMine];
                 P::scores(p, keys, q, g, s);
                 if (more) P::load_keys(p, rows, r, g, keys);
-                weigh<P::kShift>(s, scale, all, in, P::kLeast, st);
+                P::weigh(s, scale, all, in, st);
                 P::outputs(values, s, st);
                 if (more) {
                     P::load_values(p, rows, r, g, values);
@@ -709,21 +854,14 @@ __global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Param
         // Join the waves.  Two barriers a context: what the next one writes
         // before its first is not read after this one's second, but for
         // s_bad, which takes turns.
-        const float l = sum_groups(st.l);
+        const float l = st.sum();
         if (g == 0) s_m[wave][r] = st.m;
         __syncthreads();
         float top = s_m[0][r];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
         const float f = rescale(st.m, top);
-        if (r < heads) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int e = 0; e < NT; e += 4)
-                    *reinterpret_cast<f32x4 *>(&s_o[wave][r][P::dim(g, i, e)]) =
-                        f32x4{st.o[e][i], st.o[e + 1][i], st.o[e + 2][i], st.o[e + 3][i]} * f;
-        }
+        P::store(st, f, s_o[wave], heads, r, g);
         if (g == 0) {
             s_l[wave][r] = l * f;
             if (wave == 0) s_top[r] = top;
@@ -843,17 +981,25 @@ template <class T, int SHIFT, int W> __global__ __launch_bounds__(kBlock) void k
     }
 }
 
-template <class T, class CT, int DP, bool STREAM> void launch_attend(const Params &p, dim3 grid, hipStream_t s)
+template <template <bool, bool> class P, class T, class CT, int DP>
+void launch_attend(const Params &p, bool stream, dim3 grid, hipStream_t s)
 {
     // 16 slots of a page at offsets of 24-bit products
     const bool whole = p.page_size % 16 == 0 && p.slot_stride * (int64_t)sizeof(CT) < 1 << 24;
-    if (whole && p.d == DP)
-        hipLaunchKernelGGL((k_attend<T, CT, DP, true, true, STREAM>), grid, dim3(kBlock), 0, s, p);
+    if (whole && p.d == DP && stream)
+        hipLaunchKernelGGL((k_attend<P<true, true>, T, CT, DP, true, true>), grid, dim3(kBlock), 0, s, p);
+    else if (whole && p.d == DP)
+        hipLaunchKernelGGL((k_attend<P<true, false>, T, CT, DP, true, true>), grid, dim3(kBlock), 0, s, p);
     else if (whole)
-        hipLaunchKernelGGL((k_attend<T, CT, DP, true, false, STREAM>), grid, dim3(kBlock), 0, s, p);
+        hipLaunchKernelGGL((k_attend<P<false, false>, T, CT, DP, true, false>), grid, dim3(kBlock), 0, s, p);
     else
-        hipLaunchKernelGGL((k_attend<T, CT, DP, false, false, STREAM>), grid, dim3(kBlock), 0, s, p);
+        hipLaunchKernelGGL((k_attend<P<false, false>, T, CT, DP, false, false>), grid, dim3(kBlock), 0, s, p);
 }
+
+template <class T, class CT, int DP> struct Passes {
+    template <bool EXACT, bool STREAM> using ByColumn = Pass<T, CT, DP, EXACT, STREAM>;
+    template <bool EXACT, bool STREAM> using One = OnePass<DP, EXACT, STREAM>;
+};
 
 template <class T, class CT, int DP> dsim_status launch(Params &p, hipStream_t s)
 {
@@ -876,12 +1022,21 @@ template <class T, class CT, int DP> dsim_status launch(Params &p, hipStream_t s
     // read past it: a batch of 64 up to 4,096 tokens (538 MB) 98.6 us, with
     // plain loads 108; 131,072 tokens x 4 (2.1 GB) 348 and 383.  What it may
     // keep is not: 8,000 tokens (33 MB) read again 17.4 us, streamed 19.4.
+    // Nor are rows of other lengths than 64, 128 and 256, whose lines are
+    // touched more than once (heads of 80: 97 us, with plain loads 76), nor
+    // pages of other sizes than multiples of 16 (heads of 64: 61 and 63).
     const double row = 2.0 * p.d * sizeof(CT) * p.n_heads, cached = row * (double)p.n_pages * p.page_size;
     const double asked = row * (double)p.n_seq * (double)most;
-    if ((asked < cached ? asked : cached) > 256e6)
-        launch_attend<T, CT, DP, true>(p, grid, s);
-    else
-        launch_attend<T, CT, DP, false>(p, grid, s);
+    const bool stream = (asked < cached ? asked : cached) > 256e6;
+    using Kinds = Passes<T, CT, DP>;
+    if constexpr (sizeof(T) == 4) {
+        if (p.group == 1)
+            launch_attend<Kinds::template One, T, CT, DP>(p, stream, grid, s);
+        else
+            launch_attend<Kinds::template ByColumn, T, CT, DP>(p, stream, grid, s);
+    } else {
+        launch_attend<Kinds::template ByColumn, T, CT, DP>(p, stream, grid, s);
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return hip_fail(e, "paged attention launch");
     if (p.direct) return DSIM_OK;
