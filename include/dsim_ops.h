@@ -45,8 +45,8 @@ extern "C" {
  * h * head_stride  (strides in elements; the same for k and v).  Position t
  * of sequence s lies in page block_table[s * table_stride + t / page_size],
  * slot t % page_size.  Entries of the table behind a sequence's last page
- * are never read.  The rows must lie apart, nested in some order of the
- * three strides; the stride of a dimension of one is ignored.
+ * are never read.  Rows that are written must lie apart, nested in some
+ * order of the three strides; the stride of a dimension of one is ignored.
  *   dtype:     DSIM_F32, DSIM_F16, DSIM_BF16 or DSIM_E4M3
  *   k_scale, v_scale: device arrays of n_heads or NULL (1): an e4m3 element
  *              of head h stands for scale[h] times its value.  Only with
@@ -164,7 +164,8 @@ DSIM_API dsim_status dsim_paged_attention(const dsim_kv_cache *cache, int32_t dt
  *             logits_stride and out_stride elements apart (>= vocab, or any
  *             with n_rows = 1).  out may be logits (with the same stride);
  *             it must not overlap otherwise.
- * vocab 1..2^30, n_rows 0..2^20, history_width below 2^30.
+ * vocab 1..2^30, n_rows 0..2^20, history_width below 2^30; n_rows * vocab
+ * below 2^35 (DSIM_ERANGE may be returned beyond: split the call).
  */
 typedef struct {
     const void *logits;

@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <string>
 
 #include "dsim_ops.h"
@@ -262,7 +263,7 @@ void paged_attention(PyObject *const *a)
     c.type_is("out", out, q.scalar_type());
     c.check("out", out, {n, heads, cache.head_dim});
     const int32_t *len = c.vector<int32_t>("seq_len", a[3], at::kInt, n, false);
-    const double scale = PyFloat_AsDouble(a[5]);
+    const double scale = a[5] == Py_None ? 1.0 / std::sqrt((double)cache.head_dim) : PyFloat_AsDouble(a[5]);
     const long window = PyLong_AsLong(a[6]);
     if (PyErr_Occurred()) throw PythonError();
     if (window < 0 || window > INT32_MAX) refuse("window", "must be in [0, 2^31)");

@@ -43,7 +43,8 @@ static bool apart(int64_t d, int m, const int64_t *n, const int64_t *stride)
     return true;
 }
 
-static dsim_status check_cache(const dsim_kv_cache *c)
+// written: the rows must lie apart
+static dsim_status check_cache(const dsim_kv_cache *c, bool written)
 {
     if (!c) return fail(DSIM_EINVAL, "cache is NULL");
     if (c->dtype < DSIM_F32 || c->dtype > DSIM_E4M3) return fail(DSIM_EINVAL, "unknown cache dtype %d", c->dtype);
@@ -63,7 +64,7 @@ static dsim_status check_cache(const dsim_kv_cache *c)
         !stride_ok(c->head_stride, c->n_heads, es))
         return fail(DSIM_EINVAL, "cache strides must be >= 0 and multiples of 16 bytes");
     const int64_t n[3] = {c->n_pages, c->page_size, c->n_heads}, strides[3] = {c->page_stride, c->slot_stride, c->head_stride};
-    if (!apart(c->head_dim, 3, n, strides)) return fail(DSIM_EINVAL, "rows of the cache overlap");
+    if (written && !apart(c->head_dim, 3, n, strides)) return fail(DSIM_EINVAL, "rows of the cache overlap");
     if ((c->n_pages > 0 && (!c->k || !c->v)) || !aligned16(c->k) || !aligned16(c->v))
         return fail(DSIM_EINVAL, "k and v must not be NULL and must be 16-byte aligned");
     if ((c->k_scale || c->v_scale) && c->dtype != DSIM_E4M3)
@@ -105,7 +106,7 @@ dsim_status dsim_kv_append(const dsim_kv_cache *cache, int64_t n_tok, int32_t dt
                            const int32_t *seq, const int32_t *pos, const float *rope, int64_t n_rope, int32_t rot_dim,
                            int32_t interleaved, int32_t *status, void *hip_stream)
 {
-    dsim_status st = check_cache(cache);
+    dsim_status st = check_cache(cache, true);
     if (st) return st;
     if ((st = check_dtype(dtype, cache))) return st;
     if (n_tok < 0 || n_tok > INT32_MAX) return fail(DSIM_ERANGE, "n_tok must be 0..2^31 - 1");
@@ -158,7 +159,7 @@ dsim_status dsim_paged_attention(const dsim_kv_cache *cache, int32_t dtype, cons
                                  int32_t n_q_heads, const int32_t *seq_len, float scale, int32_t window, float *lse,
                                  int32_t *status, void *workspace, size_t ws_bytes, void *hip_stream)
 {
-    dsim_status st = check_cache(cache);
+    dsim_status st = check_cache(cache, false);
     if (st) return st;
     if ((st = check_dtype(dtype, cache))) return st;
     if (n_q_heads < 1 || n_q_heads > kMaxHeads || n_q_heads % cache->n_heads)

@@ -86,6 +86,26 @@ def alloc_paged_attention_workspace(n_q_heads, n_heads, head_dim, device="cuda")
                        device=device)
 
 
+def _workspace(q, cache, stream):
+    """A workspace for one call, its memory not handed out again before
+    `stream` has passed the call."""
+    import torch
+    if not torch.is_tensor(q):
+        raise ValueError("q must be a torch tensor")
+    if not isinstance(cache, dict) or not torch.is_tensor(cache.get("k")):
+        raise ValueError("cache must be a dict of torch tensors")
+    if q.dim() != 3 or cache["k"].dim() != 4:
+        raise ValueError("q must have shape (sequences, query heads, head_dim), not %s" % (tuple(q.shape),))
+    need = dsim_paged_attention_workspace(q.shape[1], cache["k"].shape[2], q.shape[2])
+    if need == 0:
+        raise ValueError("q must have a multiple of the cache's heads, heads of a size that the operator takes")
+    workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    if stream is not None and q.is_cuda:
+        workspace.record_stream(stream if hasattr(stream, "cuda_stream")
+                                else torch.cuda.ExternalStream(stream, device=q.device))
+    return workspace
+
+
 def dsim_paged_attention(q, cache, block_table, seq_len, out, scale=None, window=0, workspace=None, lse=None,
                          status=None, stream=None):
     """q, out: (sequences, query heads, head_dim); seq_len: int32
@@ -93,15 +113,8 @@ def dsim_paged_attention(q, cache, block_table, seq_len, out, scale=None, window
     lse: fp32 (sequences, query heads) or None; status: int32 (sequences,) or
     None; workspace: uint8 of at least dsim_paged_attention_workspace(...)
     bytes (None: one is allocated with torch for this call)."""
-    if scale is None:
-        scale = q.shape[-1] ** -0.5
     if workspace is None:
-        workspace = alloc_paged_attention_workspace(q.shape[1], cache["k"].shape[2], q.shape[2], device=q.device)
-        if stream is not None and q.is_cuda:
-            # its memory may be handed out again only after that stream's work
-            import torch
-            workspace.record_stream(stream if hasattr(stream, "cuda_stream")
-                                    else torch.cuda.ExternalStream(stream, device=q.device))
+        workspace = _workspace(q, cache, stream)
     (_native or lib()).paged_attention(q, cache, block_table, seq_len, out, scale, window, workspace, lse, status,
                                        stream)
 

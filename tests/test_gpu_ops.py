@@ -501,6 +501,24 @@ def test_attend_no_pages():
                              torch.zeros(0, dtype=torch.int32, device="cuda"), out[:0])
 
 
+def test_attend_expanded_cache():
+    """Cache heads that are one head's rows, read again (a stride of 0)."""
+    g = gen(14)
+    table, pages = deal(g, [70, 9], 16)
+    keys, values = cache_like(g, pages, 16, 1, 64, BF16)
+    q, lens = randn(g, 2, 8, 64).bfloat16(), torch.tensor([70, 9], dtype=torch.int32)
+    cache = dict(k=to_gpu(keys).expand(-1, -1, 4, -1), v=to_gpu(values).expand(-1, -1, 4, -1))
+    out = torch.empty(2, 8, 64, dtype=BF16, device="cuda")
+    ops.dsim_paged_attention(q.cuda(), cache, table.cuda(), lens.cuda(), out)
+    ref, _, bound = plain.attend(q, keys.expand(-1, -1, 4, -1), values.expand(-1, -1, 4, -1), table.clamp(min=0), lens,
+                                 0.125)
+    assert torch.all((out.cpu().double() - ref).abs() <= bound + (ref.abs() + bound) * 2.0 ** -8)
+    rows = torch.zeros(1, 4, 64, dtype=BF16, device="cuda")
+    one = torch.zeros(1, dtype=torch.int32, device="cuda")
+    with pytest.raises(ops.DsimError):   # but not written
+        ops.dsim_kv_append(cache, table.cuda(), rows, rows, one, one)
+
+
 def test_attend_strided_rows():
     """q and out as parts of wider tensors."""
     g = gen(4)

@@ -90,6 +90,8 @@ def test_cache_refused(L, i):
     c, r = cache(**over), rows()
     rc = L.dsim_kv_append(C.byref(c), 4, 2, C.byref(r), C.byref(r), None, None, 0, FAKE, FAKE, None, 0, 0, 0, None, None)
     assert rc < 0 and word in dsim.dsim_last_error(), dsim.dsim_last_error()
+    if word == "overlap" and "table_stride" not in over:
+        return   # rows that are only read may
     rc = L.dsim_paged_attention(C.byref(c), 2, C.byref(r), C.byref(r), 4, FAKE, 1.0, 0, None, None, FAKE, 1 << 40, None)
     assert rc < 0 and word in dsim.dsim_last_error(), dsim.dsim_last_error()
 
@@ -265,6 +267,11 @@ def test_attention_binding():
     bad("shape", lse=z(3, 3, dtype=F32))
     bad("contiguous", lse=z(4, 3, dtype=F32).t())
     bad("dtype", status=z(3))
+    bad("required", q=None)
+    bad("torch tensor", q=None, workspace=None)
+    bad("shape", q=z(3, 4), workspace=None)
+    bad("dict", cache=None, workspace=None)
+    bad("heads", q=z(3, 3, 64), workspace=None)
     with pytest.raises(TypeError):
         ops.dsim_paged_attention(z(3, 4, 64), dict(k=z(4, 16, 2, 64), v=z(4, 16, 2, 64)), z(3, 2, dtype=I32),
                                  z(3, dtype=I32), z(3, 4, 64), scale="x", workspace=z(9, dtype=torch.uint8))
