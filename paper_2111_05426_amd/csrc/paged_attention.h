@@ -905,8 +905,8 @@ __global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Param
     if (tid == 0 && !p.by_context && !p.direct) p.cut[blockIdx.x] = cut;
 }
 
-// Joins the parts of the contexts that are cut.  W = 1: a wave takes a head
-// of a context; W = 4: four waves take a quarter of its outputs.  Their
+// Joins the parts of the contexts that are cut.  W waves take a head of a
+// context, or its share where the grid has several layers.  Their
 // threads are `ways` rows, row w taking four elements each of the parts w,
 // w + ways, ...  The first of those are on their way before the weights they
 // get are known.
@@ -925,7 +925,7 @@ template <class T, int SHIFT, int W> __global__ __launch_bounds__(kBlock) void k
     if (n == 0) return;
     const bool used = h < p.part_heads && q0 + h < (q0 / p.group + 1) * p.group;   // (a last tile may have fewer heads)
     auto part = [&](int i) { return Part::of(p, i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)); };
-    const int quads = p.d / 4 / W, ways = kThreads / quads, way = tid / quads;
+    const int quads = p.d / 4 / (int)gridDim.z, ways = kThreads / quads, way = tid / quads;
     const int d0 = 4 * (tid - way * quads + (int)blockIdx.z * quads);
     const int count = used && way < ways ? n : 0;
     auto output = [&](int i) { return *reinterpret_cast<const f32x4 *>(part(i).o + h * p.d + d0); };
@@ -1040,10 +1040,15 @@ template <class T, class CT, int DP> dsim_status launch(Params &p, hipStream_t s
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return hip_fail(e, "paged attention launch");
     if (p.direct) return DSIM_OK;
-    // few contexts have many parts each
+    // Few heads have many parts each, and waves to spare.  32 query and 8
+    // cache heads of 128, 8,000 tokens, by a wave a head, four waves, four
+    // workgroups (us, both launches): 1 sequence 21.8, 18.4, 17.7; 4: 35.5,
+    // 32.1, 32.3; 8: 56.8, 55.5, 58.9; 16: 97.8, 96.8, 107; with 2,500 tokens
+    // 32 sequences 66.5 and 69.5 by a wave and by four.
     const unsigned x = (unsigned)(p.by_context ? contexts : p.grid), heads = (unsigned)p.part_heads;
-    if (contexts * 32 <= p.grid)
-        hipLaunchKernelGGL((k_join<T, P::kShift, 4>), dim3(x, heads, 4), block, 0, s, p);
+    const int64_t joins = (int64_t)p.n_seq * p.n_q_heads;
+    if (joins <= p.grid)
+        hipLaunchKernelGGL((k_join<T, P::kShift, 4>), dim3(x, heads, joins * 4 <= p.grid ? 4 : 1), block, 0, s, p);
     else
         hipLaunchKernelGGL((k_join<T, P::kShift, 1>), dim3(x, (heads + 3) / 4), block, 0, s, p);
     e = hipGetLastError();
