@@ -87,7 +87,8 @@ typedef struct {
  * +-448 stored as +-448 (infinities too) and NaN as NaN.
  *   dtype:  type of k, v, q and q_out: that of the cache, or DSIM_F16 /
  *           DSIM_BF16 with an e4m3 cache
- *   q, q_out: both NULL, or rows of n_q_heads heads; q_out may be q
+ *   q, q_out: both NULL, or rows of n_q_heads heads; q_out may be q (with
+ *           its strides)
  *   rope:   NULL with rot_dim = 0 (nothing is rotated); rot_dim a multiple
  *           of 8, at most head_dim
  *   status: device array [n_tok] or NULL: 0 or DSIM_ST_* bits.  A flagged
@@ -114,7 +115,7 @@ DSIM_API dsim_status dsim_kv_append(const dsim_kv_cache *cache, int64_t n_tok, i
  * result is rounded once to out's type.
  *   q, out: one row per sequence of n_q_heads heads, both of `dtype`: the
  *           cache's type, or DSIM_F16 / DSIM_BF16 with an e4m3 cache;
- *           out must not overlap q
+ *           out may be q (with its strides); it must not overlap otherwise
  *   seq_len: device array [n_seq].  0: out is 0 and lse -inf.  Negative: the
  *           sequence's rows of out, lse and status are left as they were.
  *   lse:    device array [n_seq][n_q_heads] fp32, or NULL

@@ -87,6 +87,15 @@ static dsim_status check_apart(const char *name, const dsim_rows *r, int64_t n, 
     return apart(d, 2, size, stride) ? DSIM_OK : fail(DSIM_EINVAL, "rows of %s overlap", name);
 }
 
+// `out` that begins where `in` does must be the same rows
+static dsim_status check_in_place(const char *out_name, const dsim_rows *in, const dsim_rows *out, int64_t n, int32_t heads)
+{
+    if (in->data == out->data && ((n > 1 && in->row_stride != out->row_stride) ||
+                                  (heads > 1 && in->head_stride != out->head_stride)))
+        return fail(DSIM_EINVAL, "in place, %s must have the strides of q", out_name);
+    return DSIM_OK;
+}
+
 static dsim_status check_dtype(int32_t dtype, const dsim_kv_cache *c)
 {
     if (dtype != DSIM_F32 && dtype != DSIM_F16 && dtype != DSIM_BF16) return fail(DSIM_EINVAL, "unknown dtype %d", dtype);
@@ -123,7 +132,8 @@ dsim_status dsim_kv_append(const dsim_kv_cache *cache, int64_t n_tok, int32_t dt
     if ((st = check_rows("k", k, n_tok, cache->n_heads, es)) || (st = check_rows("v", v, n_tok, cache->n_heads, es)))
         return st;
     if (q && ((st = check_rows("q", q, n_tok, n_q_heads, es)) || (st = check_rows("q_out", q_out, n_tok, n_q_heads, es)) ||
-              (st = check_apart("q_out", q_out, n_tok, n_q_heads, cache->head_dim))))
+              (st = check_apart("q_out", q_out, n_tok, n_q_heads, cache->head_dim)) ||
+              (st = check_in_place("q_out", q, q_out, n_tok, n_q_heads))))
         return st;
     if (!seq || !pos) return fail(DSIM_EINVAL, "seq and pos must not be NULL");
     AppendArgs a{};
@@ -169,7 +179,8 @@ dsim_status dsim_paged_attention(const dsim_kv_cache *cache, int32_t dtype, cons
     if (cache->n_seq == 0) return DSIM_OK;
     const int es = elem_size(dtype);
     if ((st = check_rows("q", q, cache->n_seq, n_q_heads, es)) || (st = check_rows("out", out, cache->n_seq, n_q_heads, es)) ||
-        (st = check_apart("out", out, cache->n_seq, n_q_heads, cache->head_dim)))
+        (st = check_apart("out", out, cache->n_seq, n_q_heads, cache->head_dim)) ||
+        (st = check_in_place("out", q, out, cache->n_seq, n_q_heads)))
         return st;
     if (!seq_len) return fail(DSIM_EINVAL, "seq_len is NULL");
     const size_t need = attend_workspace(n_q_heads, cache->n_heads, cache->head_dim);

@@ -805,6 +805,7 @@ __global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Param
         typename P::State st;
         st.clear();
         if (sp.len > 0) {
+            // (in registers before an output of theirs is written: out may be q)
             typename P::Query q;
             P::load_query(p, static_cast<const T *>(p.q) + b * p.q_row + (q0 + (r < heads ? r : 0)) * p.q_head,
                           r < heads, g, q);

@@ -108,7 +108,7 @@ def _workspace(q, cache, stream):
 
 def dsim_paged_attention(q, cache, block_table, seq_len, out, scale=None, window=0, workspace=None, lse=None,
                          status=None, stream=None):
-    """q, out: (sequences, query heads, head_dim); seq_len: int32
+    """q, out: (sequences, query heads, head_dim), out may be q; seq_len: int32
     (sequences,), the new token included; scale: None for head_dim^-0.5;
     lse: fp32 (sequences, query heads) or None; status: int32 (sequences,) or
     None; workspace: uint8 of at least dsim_paged_attention_workspace(...)

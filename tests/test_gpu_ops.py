@@ -316,6 +316,23 @@ def test_attend_long(dtype, cache):
     check_attend(dtype, cache, 2, 1, 64, 5, lens, seed=7)
 
 
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("width", [None, 600])   # a workgroup per context; cut contexts
+def test_attend_in_place(dtype, cache, width):
+    lens = [5, 0, 300, -1, 77] + ([] if width is None else [9000, 2000])
+    g = gen(8)
+    table, pages = deal(g, lens, 16, width)
+    keys, values = cache_like(g, pages, 16, 2, 64, F32 if cache == E4M3 else cache, "head")
+    dev = dict(k=to_gpu(keys.to(cache)), v=to_gpu(values.to(cache)))
+    q = randn(g, len(lens), 34, 64).to(dtype).cuda()
+    seq_len = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    ws = ops.alloc_paged_attention_workspace(34, 2, 64)
+    out = q.clone()
+    ops.dsim_paged_attention(q, dev, table.cuda(), seq_len, out, workspace=ws)
+    ops.dsim_paged_attention(q, dev, table.cuda(), seq_len, q, workspace=ws)
+    assert plain.same(q.cpu(), out.cpu()) and torch.all(out[1] == 0)
+
+
 def test_attend_many_sequences():
     g = gen(5)
     lens = torch.randint(-1, 60, (700,), generator=g).tolist()

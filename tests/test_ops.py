@@ -119,6 +119,8 @@ def test_append_refused(L):
     call("come together", q=rows())
     call("n_q_heads", q=rows(), q_out=rows(), heads=0)
     call("q_out", q=rows(row_stride=512), q_out=rows(row_stride=192), heads=4)
+    call("in place", q=rows(row_stride=512), q_out=rows(), heads=4)
+    call("in place", q=rows(row_stride=512), q_out=rows(row_stride=512, head_stride=128), heads=4)
     call("k must", k=None)
     call("v", v=rows(data=FAKE + 2))
     call("16 bytes", k=rows(head_stride=68))
@@ -148,6 +150,8 @@ def test_attention_refused(L):
     call(-1, "out", out=rows(data=0))
     call(-1, "overlap", out=rows(row_stride=0))
     call(-1, "overlap", out=rows(row_stride=128))
+    call(-1, "in place", out=rows(row_stride=1024))
+    call(-1, "in place", q=rows(row_stride=512), out=rows(row_stride=512, head_stride=128))
     call(-1, "seq_len", lens=None)
     need = L.dsim_paged_attention_workspace(4, 2, 64)
     assert need > 0
