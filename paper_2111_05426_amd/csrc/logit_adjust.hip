@@ -7,6 +7,16 @@
 // numbers: the order of the atomics does not matter) and passes over the
 // slice, so the row's counts never reach memory.  Every workgroup of a row
 // reads the whole history, from L2 after the first.
+//
+// On MI355X, 512 rows of 50,257 in fp16, histories up to 1,024, 300 biases and
+// a mask (108 MB) take 30 us, 3.6 TB/s; 64 rows of 131,072 in bf16, histories
+// up to 8,192, 16 biases and a mask (36 MB) 15.6; one row 3.6.  Memory bounds
+// the bare pass (18.6 us of the 30, 5.9 of the 15.6); the rest is a chain of
+// short phases between barriers that the few workgroups of a CU hide only in
+// part: counting 4 and 6 us, mask 2.5, biases 3.  (Penalties applied by the
+// threads that hold the history's tokens, each token claimed once by an atomic
+// bit, take 4 us more; one pass of shared memory for counts and biases
+// together, and slices of 4,096, nothing less.)
 #include "numeric.h"
 #include "ops.h"
 
@@ -43,18 +53,21 @@ __device__ inline void tokens(const int32_t *h, int32_t i, int32_t n, int32_t (&
 // first biases; one wait for memory, not four in a row, is what a workgroup
 // takes beside its share of the bandwidth.
 template <class T, int SLICE, int BLOCK>
-__global__ __launch_bounds__(BLOCK) void k_logits(dsim_logits a, int32_t slices)
+__global__ __launch_bounds__(BLOCK) void k_logits(dsim_logits a, int32_t slices, bool by_xcd)
 {
     constexpr int N = 16 / sizeof(T), kLoads = SLICE / (N * BLOCK), kAhead = 1;
     static_assert(SLICE % (N * BLOCK) == 0, "whole vectors");
     // first the history's counts, then the biases' places
     __shared__ uint32_t s_of[SLICE];
-    const int64_t b = blockIdx.x / slices;
+    // workgroups go to the eight XCDs in turn
+    const int32_t i = by_xcd ? blockIdx.x / 8 : blockIdx.x;
+    const int64_t b = by_xcd ? (int64_t)(i / slices) * 8 + blockIdx.x % 8 : i / slices;
+    if (b >= a.n_rows) return;
     const int tid = threadIdx.x;
     const T *in = static_cast<const T *>(a.logits) + b * a.logits_stride;
     T *out = static_cast<T *>(a.out) + b * a.out_stride;
     // slices begin at 16-byte aligned addresses, the first at or before the row
-    const int32_t lo = (int32_t)(blockIdx.x % slices) * SLICE - (int32_t)((uintptr_t)in / sizeof(T) % N);
+    const int32_t lo = (i % slices) * SLICE - (int32_t)((uintptr_t)in / sizeof(T) % N);
     const bool counting = a.history != nullptr, biased = a.n_bias > 0;
 
     vec<T, N> x[kLoads];
@@ -196,15 +209,24 @@ __global__ __launch_bounds__(BLOCK) void k_logits(dsim_logits a, int32_t slices)
 template <class T, int SLICE, int BLOCK> dsim_status launch(const dsim_logits &a, hipStream_t s)
 {
     constexpr int N = 16 / sizeof(T);
-    const int32_t slices = (int32_t)(((int64_t)a.vocab + N - 1 + SLICE - 1) / SLICE);   // (a row may begin inside a vector)
-    const int64_t blocks = a.n_rows * slices;
+    // a row may begin inside a vector
+    const bool aligned = (uintptr_t)a.logits % 16 == 0 && (a.n_rows == 1 || a.logits_stride % N == 0);
+    const int32_t slices = (int32_t)(((int64_t)a.vocab + (aligned ? 0 : N - 1) + SLICE - 1) / SLICE);
+    // The slices of a row on one XCD, whose L2 its history and biases then enter
+    // once, if that leaves none of the eight with much more to do: 128 rows of
+    // 131,072, histories up to 8,192, 23.6 us (in order 25.5), 512 of 50,257
+    // 29.9 (31.0); 9 rows 8.1 (7.9).
+    const bool by_xcd = a.n_rows >= 16;
+    const int64_t blocks = (by_xcd ? (a.n_rows + 7) / 8 * 8 : a.n_rows) * slices;
     if (blocks >= ((int64_t)1 << 32) / BLOCK) return fail(DSIM_ERANGE, "logits: n_rows * vocab is too large for one call");
-    hipLaunchKernelGGL((k_logits<T, SLICE, BLOCK>), dim3((unsigned)blocks), dim3(BLOCK), 0, s, a, slices);
+    hipLaunchKernelGGL((k_logits<T, SLICE, BLOCK>), dim3((unsigned)blocks), dim3(BLOCK), 0, s, a, slices, by_xcd);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? DSIM_OK : hip_fail(e, "logits launch");
 }
 
-// Few rows: slices small enough to give every CU one.
+// Few rows: slices small enough to give every CU one.  50,257 in fp16, 300
+// biases, a mask: 1 row 5.4 us (with the large slices 6.7), 32 rows 6.5 (7.4),
+// 128 rows 12.9 (12.3), 512 33.4 (30.3).
 template <class T> dsim_status launch(const dsim_logits &a, hipStream_t s)
 {
     return a.n_rows * ((a.vocab + 8191) / 8192) < 256 ? launch<T, 2048, 256>(a, s) : launch<T, 8192, 512>(a, s);
