@@ -16,7 +16,7 @@
 // part: counting 4 and 6 us, mask 2.5, biases 3.  (Penalties applied by the
 // threads that hold the history's tokens, each token claimed once by an atomic
 // bit, take 4 us more; one pass of shared memory for counts and biases
-// together, and slices of 4,096, nothing less.)
+// together, and slices of 4,096, gain nothing.)
 #include "numeric.h"
 #include "ops.h"
 

@@ -15,8 +15,14 @@ constexpr int kCus = 256;
 // elements, all resident at once.
 constexpr int per_cu(int dp, int size) { return dp <= 128 || size == 1 ? 2 : 1; }
 constexpr int kMaxGrid = kCus * 2;
-constexpr int kMinTiles = 4;      // a tile for every wave
-constexpr int kExtra = 8;         // what a context costs beside its tiles, in tiles
+// Of a run, a tile for every wave: what it begins of a context costs little
+// where workgroups are left over (one sequence of 2,048 tokens, 8 cache heads
+// of 128: 13.3 us, with runs of at least kExtra more 15.6).
+constexpr int kMinTiles = 4;
+// What a context costs beside its tiles, in tiles.  bf16, 64 sequences of up to
+// 2,000 tokens with 8 cache heads of 128: 59.6 us (5: 58.7, 12: 62.6, 24:
+// 67.3); e4m3 36.2 (40.6, 36.8, 39.5); fp32, 256 of 1,900 642 (640, 625, 631).
+constexpr int kExtra = 8;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // How the elements of a (query, cache) type pair go through the matrix
@@ -751,7 +757,7 @@ __global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Param
         total = uniform(total) * units;
         constexpr int kRuns = kCus * per_cu(DP, sizeof(CT));   // the grid
         const int64_t even = (total + kRuns - 1) / kRuns;
-        run = even > kExtra + kMinTiles ? even : kExtra + kMinTiles;
+        run = even > kMinTiles ? even : kMinTiles;
         const int64_t begin = blockIdx.x * run;
         if (begin >= total) {
             if (tid == 0 && !p.by_context) p.cut[blockIdx.x] = make_int4(0, 0, 0, 0);
@@ -1018,15 +1024,19 @@ template <class T, class CT, int DP> dsim_status launch(Params &p, hipStream_t s
     const int64_t contexts = (int64_t)p.n_seq * p.n_heads * p.tiles_of_heads;
     p.grid = kCus * per_cu(DP, sizeof(CT));
     // Contexts that cannot be long (the block table has no room, or the window
-    // is short) take a workgroup each and need neither the cut nor the join:
-    // up to 32 tiles (fp32, whose products take longer than its loads: 16).
-    // bf16, 8 cache heads of 128, up to 512 tokens: one sequence 11.0 us (cut
-    // 15.2), 256 67.6 (71.1); up to 2,048: one 25.6 (15.6), 64 63.4 (64.3).
-    // fp32, 12 heads of 80, up to 256 tokens: one 13.9 (18.1), 256 96 (94);
-    // up to 512: one 20.8 (18.3), 256 149 (141).
+    // is short) take a workgroup each and need neither the cut nor the join.
+    // Where that leaves CUs idle, fewer tiles are worth the join the longer a
+    // tile takes (us, a workgroup each and cut): bf16, 8 cache heads of 128,
+    // 1 sequence of 512 tokens 11.0 and 13.3, of 768 13.4 and 13.2, of 1,000
+    // 15.9 and 13.3; 4 of one head of 256, 384 tokens 15.3 and 16.0, 512 17.6
+    // and 16.0; fp32, 8 heads of 128, 256 tokens 12.8 and 14.0, 384 16.0 and
+    // 13.9.  64 sequences, 8 heads of 128: bf16, 1,000 tokens 48.1 and 50.5;
+    // fp32, 512 tokens 51.5 and 53.7; but 1 to 1,000 71 and 63, for one long
+    // context is all that is left in the end.
     int64_t most = (int64_t)p.table_width * p.page_size;
     if (p.window > 0 && (int64_t)p.window + P::kKeys < most) most = (int64_t)p.window + P::kKeys;
-    p.direct = most <= (sizeof(CT) == 4 ? 16 : 32) * P::kKeys && contexts < 1 << 24;
+    const int tiles = contexts >= kCus || DP <= 64 ? 32 : DP <= 128 ? (sizeof(CT) == 4 ? 16 : 24) : 12;
+    p.direct = most <= tiles * P::kKeys && contexts < 1 << 24;
     p.by_context = !p.direct && contexts <= p.grid;
     const dim3 grid((unsigned)(p.direct ? contexts : p.grid)), block(kBlock);
     // What the last-level cache (256 MB) cannot keep until the next step is
