@@ -226,10 +226,17 @@ template <class T, int SLICE, int BLOCK> dsim_status launch(const dsim_logits &a
 
 // Few rows: slices small enough to give every CU one.  50,257 in fp16, 300
 // biases, a mask: 1 row 5.4 us (with the large slices 6.7), 32 rows 6.5 (7.4),
-// 128 rows 12.9 (12.3), 512 33.4 (30.3).
+// 128 rows 12.9 (12.3), 512 33.4 (30.3).  But a long history takes longer than
+// the slice, and more threads read it sooner: large slices again, with 1,024
+// threads, as many as find room at once.  50,257 in fp16, 16 biases, a mask: 1
+// row with a history of 32,768 10.1 us (small slices 18.9), 32 rows 11.0
+// (22.3), 16 with one of 4,096 6.7 (7.0), 64 (448 slices) with 8,192 in fp32
+// 11.9 (512 threads 13.0).
 template <class T> dsim_status launch(const dsim_logits &a, hipStream_t s)
 {
-    return a.n_rows * ((a.vocab + 8191) / 8192) < 256 ? launch<T, 2048, 256>(a, s) : launch<T, 8192, 512>(a, s);
+    const int64_t large = a.n_rows * ((a.vocab + 8191) / 8192);
+    if (large <= 512 && a.history && a.history_width >= 4096) return launch<T, 8192, 1024>(a, s);
+    return large < 256 ? launch<T, 2048, 256>(a, s) : launch<T, 8192, 512>(a, s);
 }
 
 }  // namespace

@@ -609,6 +609,13 @@ def test_logits_parts(parts):
             check_logits(x, {k: v for k, v in a.items() if k != drop})
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("n,vocab,width", [(21, 9000, 60), (16, 8192, 5000), (70, 33000, 30), (40, 12345, 4096), (3, 40, 9000)])
+def test_logits_rows_and_histories(dtype, n, vocab, width):
+    """Slices of every size, rows dealt over the XCDs with some left over."""
+    check_logits(*logits_case(n, n, vocab, dtype, width, 9, True))
+
+
 def test_logits_special_values():
     x, a = logits_case(5, 3, 1000, F32, 400, 20, True)
     x[:, ::5] = -math.inf
