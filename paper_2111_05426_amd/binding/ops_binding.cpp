@@ -6,6 +6,7 @@
 // attributes at 0.1 to 0.3 us each; here it takes about what the launches do.
 #include <Python.h>
 
+#include <ATen/core/grad_mode.h>
 #include <c10/hip/HIPStream.h>
 #include <hip/hip_runtime.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -65,6 +66,9 @@ class Call {
         if (!THPVariable_Check(o)) refuse(name, "must be a torch tensor");
         const at::Tensor &t = THPVariable_Unpack(o);
         if (t.layout() != at::kStrided || t.is_neg()) refuse(name, "must be a plain strided tensor");
+        // (what autograd recorded of it would end here without a word)
+        if (t.requires_grad() && at::GradMode::is_enabled())
+            refuse(name, "requires a gradient, which the operator has not: detach it or call under torch.no_grad()");
         return &t;
     }
 

@@ -281,6 +281,22 @@ def test_attention_binding():
                                  z(3, dtype=I32), z(3, 4, 64), scale="x", workspace=z(9, dtype=torch.uint8))
 
 
+def test_tensors_that_require_a_gradient():
+    """No operator has a backward pass: refused while gradients are recorded."""
+    q, cache = torch.zeros(3, 4, 64, dtype=F16, requires_grad=True), append_args()["cache"]
+    args = dict(q=q * 1, cache=cache, block_table=torch.zeros(3, 2, dtype=I32), seq_len=torch.zeros(3, dtype=I32),
+                out=torch.zeros(3, 4, 64, dtype=F16), workspace=torch.zeros(9, dtype=torch.uint8))
+    k, x = torch.zeros(5, 2, 64, dtype=F16, requires_grad=True), torch.zeros(2, 100, requires_grad=True)
+    for what, fn, kw in (("q", ops.dsim_paged_attention, args), ("k", ops.dsim_kv_append, append_args(k=k)),
+                         ("logits", ops.dsim_logit_adjust, dict(logits=x, out=torch.zeros(2, 100))),
+                         ("out", ops.dsim_logit_adjust, dict(logits=x.detach(), out=x))):
+        refused(what + " requires a gradient", fn, **kw)
+        with torch.no_grad():
+            refused("GPU", fn, **kw)
+        with torch.inference_mode():
+            refused("GPU", fn, **kw)
+
+
 def test_logits_binding():
     z = lambda *s, dtype=F32: torch.zeros(*s, dtype=dtype)   # noqa: E731
 
