@@ -55,7 +55,7 @@ __device__ inline Place place_of(const AppendArgs &a, int64_t t)
 
 // j / n for mul = ceil(2^32 / n), 0 for n = 1; exact for j < 2^26, n <= 64 (a
 // call's chunks a token: 2^17, a row's: 64)
-__device__ inline int divide(int j, uint32_t mul) { return mul ? (int)__umulhi((uint32_t)j, mul) : j; }
+__device__ inline uint32_t divide(uint32_t j, uint32_t mul) { return mul ? __umulhi(j, mul) : j; }
 
 // T: type of the new rows; CT: of the cache; VEC: elements per load.  A
 // thread takes one chunk of VEC elements, or, where pairs (i, i + R/2) are
@@ -75,14 +75,15 @@ template <class T, class CT, int VEC> __global__ __launch_bounds__(kMaxBlock) vo
         for (int i = threadIdx.x; i < n_q + n_k + n_v; i += blockDim.x) {
             if (i >= n_q + n_k) {   // a value: copied
                 if (p.status) continue;
-                const int j = i - n_q - n_k, h = divide(j, mul_value), e = (j - h * per_value) * VEC;
+                const uint32_t j = i - n_q - n_k, h = divide(j, mul_value), e = (j - __umul24(h, per_value)) * VEC;
                 V x = load_row<T, VEC>(a.v.data, t * a.v.row_stride + h * a.v.head_stride + e);
                 if (a.c.v_scale) x /= a.c.v_scale[h];
                 store_row<CT, VEC>(a.c.v, p.at + h * a.c.head_stride + e, x);
                 continue;
             }
             const bool query = i < n_q;
-            const int j = query ? i : i - n_q, h = divide(j, mul_head), c = j - h * per_head;
+            const uint32_t j = query ? i : i - n_q, h = divide(j, mul_head);
+            const int c = j - __umul24(h, per_head);
             const dsim_rows &src = query ? a.q : a.k;
             const int64_t from = t * src.row_stride + h * src.head_stride;
             const int64_t to = query ? t * a.q_out.row_stride + h * a.q_out.head_stride
@@ -135,10 +136,14 @@ template <class T, class CT, int VEC> void launch(const AppendArgs &a, hipStream
     // 512 (bf16, 32 query and 8 cache heads of 128: 256 tokens 4.1 us, with
     // 128 threads 5.4).  Many: fewer and busier threads, so that fewer
     // workgroups start (24,588 tokens 114 us, with 512 threads 173, both
-    // with plain stores).
+    // with plain stores); one wave where a token has few chunks, or an e4m3
+    // cache needs more arithmetic for each (8,192 tokens, by one wave and
+    // two: bf16, 12 query and 2 cache heads of 64 11.7 and 13.2 us, 12 and 12
+    // 17.4 and 16.7; in e4m3 17.6 and 18.2; 32 and 8 of 128 33.3 and 32.5).
     const int n_rot = a.interleaved ? a.rot_dim / VEC : a.rot_dim / 2 / VEC, rest = (a.c.head_dim - a.rot_dim) / VEC;
     const int64_t chunks = (int64_t)(a.n_q_heads + a.c.n_heads) * (n_rot + rest) + (int64_t)a.c.n_heads * (a.c.head_dim / VEC);
-    const int64_t most = a.n_tok < 1024 ? kMaxBlock : 128, rounds = (chunks + most - 1) / most;
+    const int64_t few = sizeof(CT) == 1 ? 320 : 128;
+    const int64_t most = a.n_tok < 1024 ? kMaxBlock : chunks <= few ? 64 : 128, rounds = (chunks + most - 1) / most;
     const int block = (int)((chunks + 64 * rounds - 1) / (64 * rounds)) * 64;
     const dim3 grid((unsigned)(a.n_tok < (1 << 20) ? a.n_tok : (1 << 20)));
     const auto mul = [](int n) { return n > 1 ? (uint32_t)((((uint64_t)1 << 32) + n - 1) / n) : 0u; };

@@ -38,7 +38,7 @@ template <class T, int N> __device__ inline vec<T, N> from_f32(vec<float, N> x)
         static_assert(N % 4 == 0, "whole words");
         vec<uint32_t, N / 4> w;
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = x[i] > 448.0f ? 448.0f : x[i] < -448.0f ? -448.0f : x[i];
+        for (int i = 0; i < N; ++i) x[i] = x[i] != x[i] ? x[i] : __builtin_amdgcn_fmed3f(x[i], -448.0f, 448.0f);
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) {
             int p = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i], x[4 * i + 1], 0, false);

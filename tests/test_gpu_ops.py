@@ -125,6 +125,13 @@ def test_append_many_tokens():
     check_append(F16, F16, 1, 1, 16, 16, [3000, 1, 2000], rot=16)
 
 
+@pytest.mark.parametrize("dtype,cache", [(F32, F32), (BF16, BF16), (F16, E4M3)])
+@pytest.mark.parametrize("heads,kv,d,rot,interleaved", [(12, 12, 64, 48, True), (12, 2, 64, 64, False), (32, 8, 128, 128, False)])
+def test_append_prompts(dtype, cache, heads, kv, d, rot, interleaved):
+    """A wave a token and two."""
+    check_append(dtype, cache, heads, kv, d, 32, [700, 1, 500], rot=rot, interleaved=interleaved, scales=cache == E4M3)
+
+
 def test_append_more_tokens_than_workgroups():
     n = (1 << 20) + 5
     g = torch.Generator(device="cuda").manual_seed(1)
