@@ -129,7 +129,10 @@ DSIM_API dsim_status dsim_kv_append(const dsim_kv_cache *cache, int64_t n_tok, i
  *           refuses).
  * The work of all sequences is laid end to end and cut into equal parts, so
  * that one long context among short ones is spread over the GPU; contexts
- * that a cut goes through are joined by a second launch.  n_seq <= 2^20.
+ * that a cut goes through are joined by a second launch.  Where the block
+ * table or the window keeps every context short (at most 1,024 keys, fewer
+ * for long heads), each is one workgroup's and there is no second launch.
+ * n_seq <= 2^20.
  */
 DSIM_API size_t dsim_paged_attention_workspace(int32_t n_q_heads, int32_t n_heads, int32_t head_dim);
 DSIM_API dsim_status dsim_paged_attention(const dsim_kv_cache *cache, int32_t dtype, const dsim_rows *q,
