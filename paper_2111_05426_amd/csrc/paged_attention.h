@@ -1049,12 +1049,15 @@ template <class T, class CT, int DP> dsim_status launch(Params &p, hipStream_t s
     // 1 sequence of 512 tokens 11.0 and 13.3, of 768 13.4 and 13.2, of 1,000
     // 15.9 and 13.3; 4 of one head of 256, 384 tokens 15.3 and 16.0, 512 17.6
     // and 16.0; fp32, 8 heads of 128, 256 tokens 12.8 and 14.0, 384 16.0 and
-    // 13.9.  64 sequences, 8 heads of 128: bf16, 1,000 tokens 48.1 and 50.5;
-    // fp32, 512 tokens 51.5 and 53.7; but 1 to 1,000 71 and 63, for one long
-    // context is all that is left in the end.
+    // 13.9.  Many contexts: 8 heads of 128 in bf16, a window of 1,000, 16
+    // sequences 19.0 and 21.7, 64 45.5 and 51.2, in e4m3 24.8 and 32.7; fp32,
+    // a window of 500, 64 48.2 and 54.1, but up to 1,000 tokens of any number
+    // 71 and 63, for one long context is all that is left in the end; 16 heads
+    // of 256, one workgroup a CU, bf16, a window of 1,000 193 and 183.
     int64_t most = (int64_t)p.table_width * p.page_size;
-    if (p.window > 0 && (int64_t)p.window + P::kKeys < most) most = (int64_t)p.window + P::kKeys;
-    const int tiles = contexts >= kCus || DP <= 64 ? 32 : DP <= 128 ? (sizeof(CT) == 4 ? 16 : 24) : 12;
+    if (p.window > 0 && p.window < most) most = p.window;
+    const bool many = contexts >= kCus / 2 && per_cu(DP, sizeof(CT)) > 1;
+    const int tiles = DP <= 64 || many ? 32 : DP <= 128 ? (sizeof(CT) == 4 ? 16 : 24) : 12;
     p.direct = most <= tiles * P::kKeys && contexts < 1 << 24;
     p.by_context = !p.direct && contexts <= p.grid;
     const dim3 grid((unsigned)(p.direct ? contexts : p.grid)), block(kBlock);
