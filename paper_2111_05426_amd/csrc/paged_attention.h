@@ -191,11 +191,11 @@ template <int NT> struct Columns {
     __device__ float sum() const { return sum_groups(l); }
 };
 
-// The running maximum takes in the products s; returns them as weights, 2^SHIFT
-// for one at the maximum.  scale > 0: base-2 logarithms per unit of s.  `in`:
+// The running maximum takes in the products s; returns them as weights, 1 for
+// one at the maximum.  scale > 0: base-2 logarithms per unit of s.  `in`:
 // bit i says whether s[i] counts (looked at unless `all`); one that does not
 // becomes the weight `least` and adds nothing to the sum.
-template <int SHIFT, int N, int NT>
+template <int N, int NT>
 __device__ inline void weigh(float (&s)[N], float scale, bool all, uint32_t in, float least, Columns<NT> &st)
 {
     if (!all) {
@@ -214,7 +214,7 @@ __device__ inline void weigh(float (&s)[N], float scale, bool all, uint32_t in, 
         for (int e = 0; e < NT; ++e) st.o[e] *= f;
         st.m = m;
     }
-    const float m = st.m == -HUGE_VALF ? 0.0f : st.m - SHIFT;
+    const float m = st.m == -HUGE_VALF ? 0.0f : st.m;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -m));
@@ -252,7 +252,7 @@ template <class P, int DP, int KEYS> struct ByColumns {
 
     __device__ static void weigh(float (&s)[kMine], float scale, bool all, uint32_t in, State &st)
     {
-        attend::weigh<P::kShift>(s, scale, all, in, P::kLeast, st);
+        attend::weigh(s, scale, all, in, P::kLeast, st);
     }
 
     // the outputs times f to shared memory, a row per head
@@ -276,12 +276,9 @@ struct Pass : ByColumns<Pass<T, CT, DP, EXACT, STREAM>, DP, 32> {
     static constexpr int kChunk = 16 / sizeof(CT);            // elements per 16-byte load of a key
     static constexpr int kSteps = DP / (4 * kChunk);          // loads of a key per lane
     static constexpr int kParts = kChunk / 8;                 // products per load
-    // fp16 ends at 2^-24: weights from 2^15 down keep a long tail of small
-    // ones, which together may weigh as much as the largest
-    static constexpr int kShift = __is_same(T, f16) ? 15 : 0;
     // of a key that does not count: not 0, so that the attended value that
     // stands in its place may be infinite
-    static constexpr float kLeast = __is_same(T, f16) ? 0x1p-24f : 0x1p-100f;
+    static constexpr float kLeast = 0x1p-100f;
     using Query = vec<T, 8>[kSteps * kParts];
 
     using Keys = u32x4[2][kSteps];
@@ -337,51 +334,50 @@ struct Pass : ByColumns<Pass<T, CT, DP, EXACT, STREAM>, DP, 32> {
     }
 
     // two of the four e4m3 of a word, exactly
-    template <bool HIGH> __device__ static vec<T, 2> widen2(uint32_t w)
+    template <class U, bool HIGH> __device__ static vec<U, 2> widen2(uint32_t w)
     {
-        if constexpr (__is_same(T, f16))
-            return __builtin_bit_cast(vec<T, 2>, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH));
+        if constexpr (__is_same(U, f16))
+            return __builtin_bit_cast(vec<U, 2>, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH));
         else
-            return __builtin_bit_cast(vec<T, 2>, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HIGH));
+            return __builtin_bit_cast(vec<U, 2>, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HIGH));
     }
 
     __device__ static vec<T, 8> widen8(uint32_t lo, uint32_t hi)
     {
-        const vec<T, 2> a = widen2<false>(lo), b = widen2<true>(lo), c = widen2<false>(hi), d = widen2<true>(hi);
+        const vec<T, 2> a = widen2<T, false>(lo), b = widen2<T, true>(lo), c = widen2<T, false>(hi), d = widen2<T, true>(hi);
         return {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
     }
 
-    // A weight as the sum of two numbers of T: with one the output would carry
-    // an error as large as its own rounding.  The first is cut off, the
-    // second is never 0 (at least the type's smallest that the products keep,
-    // 2^-39 of the largest weight in fp16), so that an infinite value times
-    // both is that infinity.
-    __device__ static void split(const float (&s)[8], vec<T, 8> &hi, vec<T, 8> &lo)
+    // Weights as the sums of three bf16 numbers of 8 bits, which hold fp32's 24
+    // exactly and its range.  (Two, 16 bits, put the outputs five times as far
+    // from the formula's as fp32 sums do.)  For values that may be infinite no
+    // part is 0 unless the weight is, so that the three products' sum is that
+    // infinity: fp32's smallest normal number stands in, below which weights
+    // are 0 themselves.
+    __device__ static void split(const float (&s)[8], vec<bf16, 8> (&w)[3])
     {
-        vec<float, 8> rest;
-        if constexpr (__is_same(T, bf16)) {
-            vec<uint32_t, 4> w;
+        uint32_t part[3][8];
+        const auto rest = [](uint32_t x) {
+            return __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, x) - __builtin_bit_cast(float, x & 0xffff0000u));
+        };
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t bits = __builtin_bit_cast(uint32_t, s[i]);
-                rest[i] = fmaxf(s[i] - __builtin_bit_cast(float, bits & 0xffff0000u), 0x1p-126f);
+        for (int i = 0; i < 8; ++i) {
+            part[0][i] = __builtin_bit_cast(uint32_t, s[i]);
+            part[1][i] = rest(part[0][i]);
+            part[2][i] = rest(part[1][i]);
+            if constexpr (!k8) {
+                const uint32_t least = min(part[0][i], 0x00800000u);   // (as whole numbers: none is negative)
+                part[1][i] = max(part[1][i], least);
+                part[2][i] = max(part[2][i], least);
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                w[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, s[2 * i + 1]), __builtin_bit_cast(uint32_t, s[2 * i]),
-                                             0x07060302);
-            hi = __builtin_bit_cast(vec<T, 8>, w);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                const auto two = __builtin_amdgcn_cvt_pkrtz(s[i], s[i + 1]);
-                hi[i] = (T)two[0];
-                hi[i + 1] = (T)two[1];
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) rest[i] = fmaxf(s[i] - (float)hi[i], 0x1p-24f);
         }
-        lo = __builtin_convertvector(rest, vec<T, 8>);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            vec<uint32_t, 4> x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_perm(part[k][2 * i + 1], part[k][2 * i], 0x07060302);
+            w[k] = __builtin_bit_cast(vec<bf16, 8>, x);
+        }
     }
 
     // products of the lane's keys 16 t + 4 g + i with query head r
@@ -402,37 +398,52 @@ struct Pass : ByColumns<Pass<T, CT, DP, EXACT, STREAM>, DP, 32> {
             for (int i = 0; i < 4; ++i) s[4 * t + i] = acc[t][i];
     }
 
-    // the values of those keys, times their weights
+    // The values of those keys, times their weights.  bf16 and e4m3 values are
+    // bf16 numbers, their products' operands as they are (64 sequences of up
+    // to 4,096, bf16, 32 and 8 heads of 128: 98.8 us; with fp32 operands 102;
+    // 128 of up to 8,192 in e4m3 202 and 273).  fp16 values are not, and fp16
+    // weights would end at 2^-39 of the largest: both as fp32 (64 sequences of
+    // up to 4,096 106 us; the values in two bf16 parts and five products 105,
+    // but 256 of up to 300 with 12 heads of 64 40 us for 37).
     __device__ static void outputs(const Values &x, const float (&s)[8], Columns<DP / 16> &st)
     {
-        vec<T, 8> hi, lo;
-        split(s, hi, lo);
-        vec<T, kE> row[8];
+        if constexpr (__is_same(CT, f16)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) row[i] = to_t(x[i]);
-        constexpr int kTogether = 4;
+            for (int i = 0; i < 8; ++i) {
+                const vec<float, kE> row = to_f32<f16, kE>(x[i]);
 #pragma unroll
-        for (int e0 = 0; e0 < kE; e0 += kTogether) {
-            vec<T, 8> a[kTogether];
+                for (int e = 0; e < kE; ++e) st.o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(row[e], s[i], st.o[e], 0, 0, 0);
+            }
+        } else {
+            vec<bf16, 8> w[3];
+            split(s, w);
+            vec<bf16, kE> row[8];
 #pragma unroll
-            for (int e = 0; e < kTogether; ++e)
+            for (int i = 0; i < 8; ++i) row[i] = to_bf16(x[i]);
+            constexpr int kTogether = 4;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) a[e][i] = row[i][e0 + e];
+            for (int e0 = 0; e0 < kE; e0 += kTogether) {
+                vec<bf16, 8> a[kTogether];
 #pragma unroll
-            for (int e = 0; e < kTogether; ++e) st.o[e0 + e] = Mfma<T>::mul(a[e], hi, st.o[e0 + e]);
+                for (int e = 0; e < kTogether; ++e)
 #pragma unroll
-            for (int e = 0; e < kTogether; ++e) st.o[e0 + e] = Mfma<T>::mul(a[e], lo, st.o[e0 + e]);
+                    for (int i = 0; i < 8; ++i) a[e][i] = row[i][e0 + e];
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+#pragma unroll
+                    for (int e = 0; e < kTogether; ++e) st.o[e0 + e] = Mfma<bf16>::mul(a[e], w[k], st.o[e0 + e]);
+            }
         }
     }
 
-    __device__ static vec<T, kE> to_t(vec<CT, kE> x)
+    __device__ static vec<bf16, kE> to_bf16(vec<CT, kE> x)
     {
         if constexpr (k8) {
             const auto w = __builtin_bit_cast(vec<uint32_t, kE / 4>, x);
-            vec<T, kE> y;
+            vec<bf16, kE> y;
 #pragma unroll
             for (int i = 0; i < kE / 4; ++i) {
-                const vec<T, 2> a = widen2<false>(w[i]), b = widen2<true>(w[i]);
+                const vec<bf16, 2> a = widen2<bf16, false>(w[i]), b = widen2<bf16, true>(w[i]);
                 y[4 * i] = a[0];
                 y[4 * i + 1] = a[1];
                 y[4 * i + 2] = b[0];
@@ -451,7 +462,7 @@ struct Pass : ByColumns<Pass<T, CT, DP, EXACT, STREAM>, DP, 32> {
 // fp32: the same with products of four reduction indices, 16 keys a tile.
 template <int DP, bool EXACT, bool STREAM>
 struct Pass<float, float, DP, EXACT, STREAM> : ByColumns<Pass<float, float, DP, EXACT, STREAM>, DP, 16> {
-    static constexpr int kKeys = 16, kSteps = DP / 16, kQuads = DP / 64, kShift = 0;
+    static constexpr int kKeys = 16, kSteps = DP / 16, kQuads = DP / 64;
     using Query = f32x4[kSteps];
 
     using Keys = f32x4[kSteps];
@@ -703,12 +714,11 @@ __device__ inline void write_row(const Params &p, int b, int head, int d, f32x4 
     *reinterpret_cast<vec<T, 4> *>(static_cast<T *>(p.out) + b * p.out_row + head * p.out_head + d) = from_f32<T, 4>(x);
 }
 
-template <int SHIFT>
 __device__ inline void write_lse(const Params &p, int b, int head, float m, float l, bool empty, int32_t bad)
 {
     if (p.lse)
         p.lse[(int64_t)b * p.n_q_heads + head] =
-            bad ? __builtin_nanf("") : empty ? -HUGE_VALF : (m + (__builtin_log2f(l) - SHIFT)) * kLn2;
+            bad ? __builtin_nanf("") : empty ? -HUGE_VALF : (m + __builtin_log2f(l)) * kLn2;
 }
 
 // A part of a context: d outputs of each head, then the heads' maxima and
@@ -921,7 +931,7 @@ __global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Param
             o *= vs;
             if (whole) {
                 write_row<T>(p, b, q0 + h, d, o, sum, sp.len == 0, bad);
-                if (d == 0) write_lse<P::kShift>(p, b, q0 + h, s_top[h], sum, sp.len == 0, bad);
+                if (d == 0) write_lse(p, b, q0 + h, s_top[h], sum, sp.len == 0, bad);
             } else {
                 *reinterpret_cast<f32x4 *>(part.o + h * p.d + d) = o;
                 if (d == 0) {
@@ -946,7 +956,7 @@ __global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Param
 // threads are `ways` rows, row w taking four elements each of the parts w,
 // w + ways, ...  The first of those are on their way before the weights they
 // get are known.
-template <class T, int SHIFT, int W> __global__ __launch_bounds__(kBlock) void k_join(Params p)
+template <class T, int W> __global__ __launch_bounds__(kBlock) void k_join(Params p)
 {
     constexpr int kThreads = 64 * W, kHeads = kBlock / kThreads, kAhead = 8;
     __shared__ float s_m[kWaves], s_l[kWaves];
@@ -1012,7 +1022,7 @@ template <class T, int SHIFT, int W> __global__ __launch_bounds__(kBlock) void k
         write_row<T>(p, b, q0 + h, d0, o, l, false, bad);
     }
     if (tid == 0 && blockIdx.z == 0) {
-        write_lse<SHIFT>(p, b, q0 + h, m, l, false, bad);
+        write_lse(p, b, q0 + h, m, l, false, bad);
         if (p.status) p.status[b] = bad;
     }
 }
@@ -1091,9 +1101,9 @@ template <class T, class CT, int DP> dsim_status launch(Params &p, hipStream_t s
     const unsigned x = (unsigned)(p.by_context ? contexts : p.grid), heads = (unsigned)p.part_heads;
     const int64_t joins = (int64_t)p.n_seq * p.n_q_heads;
     if (joins <= p.grid)
-        hipLaunchKernelGGL((k_join<T, P::kShift, 4>), dim3(x, heads, joins * 4 <= p.grid ? 4 : 1), block, 0, s, p);
+        hipLaunchKernelGGL((k_join<T, 4>), dim3(x, heads, joins * 4 <= p.grid ? 4 : 1), block, 0, s, p);
     else
-        hipLaunchKernelGGL((k_join<T, P::kShift, 1>), dim3(x, (heads + 3) / 4), block, 0, s, p);
+        hipLaunchKernelGGL((k_join<T, 1>), dim3(x, (heads + 3) / 4), block, 0, s, p);
     e = hipGetLastError();
     return e == hipSuccess ? DSIM_OK : hip_fail(e, "paged attention join launch");
 }

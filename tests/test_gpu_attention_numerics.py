@@ -1,0 +1,112 @@
+"""What the paged attention's numbers are good for: weights with fp32's bits
+and range whatever the cache's type, infinities and NaN as in the formula,
+and errors of the size that fp32 arithmetic has (attention_bounds.py)."""
+import math
+
+import pytest
+import torch
+
+import attention_bounds as bounds
+from paper_2111_05426_amd import ops
+from test_gpu_ops import BF16, E4M3, F16, F32, TYPES, cache_like, deal, gen, gpu, randn, to_gpu  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+WIDTHS = [None, 200]   # a workgroup per context; a block table with room for 3,200 tokens: cut and joined
+
+
+def attend(q, keys, values, table, lens, scale, window=0, **scales):
+    """(out, lse) of the operator for tensors on the host."""
+    out = torch.full(q.shape, 9.0, dtype=q.dtype, device="cuda")
+    lse = torch.full(q.shape[:2], 9.0, device="cuda")
+    cache = dict(k=to_gpu(keys), v=to_gpu(values), **{n: to_gpu(x) for n, x in scales.items()})
+    ws = ops.alloc_paged_attention_workspace(q.shape[1], keys.shape[2], q.shape[2])
+    ws.fill_(255)
+    ops.dsim_paged_attention(q.cuda(), cache, table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), out,
+                             scale=scale, window=window, workspace=ws, lse=lse)
+    return out.cpu(), lse.cpu()
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("heads,kv,d", [(4, 4, 64), (8, 2, 128), (6, 2, 80), (4, 1, 256), (3, 3, 16)])
+@pytest.mark.parametrize("window", [0, 700])
+def test_errors_are_those_of_fp32(dtype, cache, heads, kv, d, window):
+    g = gen(d + heads)
+    lens = [1, 30, 250, 0, 1500]
+    table, pages = deal(g, lens, 16)
+    keys, values = (x.to(cache) for x in cache_like(g, pages, 16, kv, d, F32 if cache == E4M3 else cache))
+    q = (2 * randn(g, len(lens), heads, d)).to(dtype)
+    scales = {n + "_scale": 0.25 + torch.rand(kv, generator=g) for n in "kv"} if cache == E4M3 else {}
+    ref, ref_lse, room, lse_room = bounds.attend(q, keys, values, table.clamp(min=0), lens, d ** -0.5, window, **scales)
+    out, lse = attend(q, keys, values, table, lens, d ** -0.5, window, **scales)
+    print("of the room: %.2f" % bounds.off(out, ref, room) if dtype == F32 else "")
+    assert bounds.within(out, ref, room)
+    some = torch.tensor(lens) > 0
+    assert torch.all((lse.double() - ref_lse)[some].abs() <= lse_room[some]) and torch.all(lse[3] == -math.inf)
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("kv", [1, 4])   # four query heads
+@pytest.mark.parametrize("width", WIDTHS)
+def test_weights_keep_their_bits(dtype, cache, kv, width):
+    """Two keys of values 1 and -1 whose weights nearly cancel: out = tanh(a /
+    2), a the difference of their scores, one product of powers of two and a
+    query's element.  The second weight exp(-a) is off by at most 2^-23 (an exponential next to 1,
+    its argument exact but for 2^-24 of a), the sums 1 +- w by 2^-24 each, so
+    out by 2^-22.  A weight of 16 bits is off by up to 2^-17."""
+    n, d = 64, 16
+    g = gen(1)
+    q = torch.zeros(n, 4, d)
+    q[..., 0] = (64 + torch.arange(n * 4)).view(n, 4) * 2.0 ** -9
+    keys, values = torch.zeros(n, 16, kv, d), torch.zeros(n, 16, kv, d)
+    keys[:, 1, :, 0], values[:, 0], values[:, 1] = -2.0 ** -5, 1.0, -1.0
+    q, keys, values = q.to(dtype), keys.to(cache), values.to(cache)
+    table = torch.full((n, width or 2), -1, dtype=torch.int32)
+    table[:, 0] = torch.randperm(n, generator=g)
+    scale = 2.0 ** -4
+    out, _ = attend(q, keys, values, table, [2] * n, scale)
+    ref = torch.tanh(q[..., :1].double() * 2.0 ** -5 * scale / 2).expand(n, 4, d)
+    assert bool(torch.all((out.double() - ref).abs() <= 2.0 ** -22 + ref.abs() * bounds.HALF_STEP[dtype] + bounds.LEAST[dtype]))
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("n", [20, 900, 3000])
+@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("kv", [1, 2])   # two query heads
+def test_far_keys_add_what_they_weigh(dtype, cache, n, width, kv):
+    """One key with small values far above many with large ones, which weigh
+    2^-50 to 2^-60 of it: nothing, and no more, comes from them."""
+    g, d = gen(n), 64
+    table, pages = deal(g, [n], 16, width)
+    keys, values = (torch.zeros(pages, 16, kv, d) for _ in range(2))
+    spot = table[0, 0].long(), 3
+    keys[..., 0] = -torch.randint(50, 61, (pages, 16, kv), generator=g).float()
+    values[:] = 256.0
+    keys[spot], values[spot] = 0.0, 2.0 ** -9
+    q = torch.zeros(1, 2, d)
+    q[..., 0] = 1.0
+    q, keys, values = q.to(dtype), keys.to(cache), values.to(cache)
+    ref, _, room, _ = bounds.attend(q, keys, values, table.clamp(min=0), [n], math.log(2.0))
+    out, _ = attend(q, keys, values, table, [n], math.log(2.0))
+    assert room.max() < 2.0 ** -23 and bounds.within(out, ref, room)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("below", [0, 12, 30, 60])
+@pytest.mark.parametrize("n,where", [(200, 0), (200, 70), (200, 199), (3000, 1717)])
+@pytest.mark.parametrize("kv", [1, 2])
+def test_infinite_values_of_small_weights(dtype, below, n, where, kv):
+    """An infinite value whose key's score lies far below the others' is
+    infinite in the output as long as fp32 has the weight."""
+    g, d = gen(n + where), 64
+    table, pages = deal(g, [n], 16, 200 if n > 1000 else None)
+    keys, values = torch.zeros(pages, 16, kv, d), randn(g, pages, 16, kv, d)
+    spot = table[0, where // 16].long(), where % 16
+    keys[spot[0], spot[1], :, 0] = -float(below)
+    values[spot[0], spot[1], :, 5], values[spot[0], spot[1], :, 9] = math.inf, -math.inf
+    q = torch.zeros(1, 2, d)
+    q[..., 0] = 1.0
+    out, _ = attend(q.to(dtype), keys.to(dtype), values.to(dtype), table, [n], 1.0)
+    assert torch.all(out[..., 5] == math.inf) and torch.all(out[..., 9] == -math.inf)
+    rest = [i for i in range(d) if i not in (5, 9)]
+    assert torch.all(out[..., rest].isfinite())
