@@ -194,9 +194,9 @@ template <int NT> struct Columns {
 // The running maximum takes in the products s; returns them as weights, 1 for
 // one at the maximum.  scale > 0: base-2 logarithms per unit of s.  `in`:
 // bit i says whether s[i] counts (looked at unless `all`); one that does not
-// becomes the weight `least` and adds nothing to the sum.
+// becomes the weight 0.
 template <int N, int NT>
-__device__ inline void weigh(float (&s)[N], float scale, bool all, uint32_t in, float least, Columns<NT> &st)
+__device__ inline void weigh(float (&s)[N], float scale, bool all, uint32_t in, Columns<NT> &st)
 {
     if (!all) {
 #pragma unroll
@@ -218,11 +218,7 @@ __device__ inline void weigh(float (&s)[N], float scale, bool all, uint32_t in, 
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -m));
-        st.l += s[i];
-    }
-    if (!all) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) s[i] = in >> i & 1 ? s[i] : least;
+        st.l += s[i];   // (exp2(-inf) = 0 for those that do not count)
     }
 }
 
@@ -252,7 +248,7 @@ template <class P, int DP, int KEYS> struct ByColumns {
 
     __device__ static void weigh(float (&s)[kMine], float scale, bool all, uint32_t in, State &st)
     {
-        attend::weigh(s, scale, all, in, P::kLeast, st);
+        attend::weigh(s, scale, all, in, st);
     }
 
     // the outputs times f to shared memory, a row per head
@@ -276,9 +272,6 @@ struct Pass : ByColumns<Pass<T, CT, DP, EXACT, STREAM>, DP, 32> {
     static constexpr int kChunk = 16 / sizeof(CT);            // elements per 16-byte load of a key
     static constexpr int kSteps = DP / (4 * kChunk);          // loads of a key per lane
     static constexpr int kParts = kChunk / 8;                 // products per load
-    // of a key that does not count: not 0, so that the attended value that
-    // stands in its place may be infinite
-    static constexpr float kLeast = 0x1p-100f;
     using Query = vec<T, 8>[kSteps * kParts];
 
     using Keys = u32x4[2][kSteps];
@@ -380,6 +373,16 @@ struct Pass : ByColumns<Pass<T, CT, DP, EXACT, STREAM>, DP, 32> {
         }
     }
 
+    // The values of keys that do not count become 0: what stands in their
+    // place, the nearest attended key's, may be infinite, and times the weight
+    // 0 NaN.
+    __device__ static void drop(Values &x, uint32_t in, int g)
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (!(in >> i & 1)) x[i] = vec<CT, kE>(0);
+    }
+
     // products of the lane's keys 16 t + 4 g + i with query head r
     __device__ static void scores(const Params &p, const Keys &x, const Query &q, int g, float (&s)[8])
     {
@@ -467,7 +470,6 @@ struct Pass<float, float, DP, EXACT, STREAM> : ByColumns<Pass<float, float, DP, 
 
     using Keys = f32x4[kSteps];
     using Values = f32x4[4][kQuads];
-    static constexpr float kLeast = 0x1p-100f;
 
     __device__ static void load_query(const Params &p, const float *q, bool used, int g, Query &out)
     {
@@ -500,6 +502,15 @@ struct Pass<float, float, DP, EXACT, STREAM> : ByColumns<Pass<float, float, DP, 
                 x[i][j] = read<STREAM, f32x4>(val + (EXACT || at < p.d ? at : 0));
             }
         }
+    }
+
+    __device__ static void drop(Values &x, uint32_t in, int g)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < kQuads; ++j)
+                if (!(in >> i & 1)) x[i][j] = f32x4{0, 0, 0, 0};
     }
 
     __device__ static void scores(const Params &p, const Keys &x, const Query &q, int g, float (&s)[4])
@@ -603,8 +614,14 @@ template <int DP, bool EXACT, bool STREAM> struct OnePass : Pass<float, float, D
         }
         const float m = st.m == -HUGE_VALF ? 0.0f : st.m;
         s[0] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0], scale, -m));
-        st.l += counts ? s[0] : 0.0f;
-        s[0] = counts ? s[0] : Base::kLeast;
+        s[0] = counts ? s[0] : 0.0f;
+        st.l += s[0];
+    }
+
+    // (`in` is key r's, the values are those of keys 4 g + i)
+    __device__ static void drop(typename Base::Values &x, uint32_t in, int g)
+    {
+        Base::drop(x, (uint32_t)(__builtin_amdgcn_ballot_w64(in & 1) >> (4 * g)) & 15, g);
     }
 
     __device__ static void outputs(const typename Base::Values &x, const float (&s)[1], State &st)
@@ -887,6 +904,7 @@ __global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Param
                 P::scores(p, keys, q, g, s);
                 if (more) P::load_keys(p, rows, r, g, keys);
                 P::weigh(s, scale, all, in, st);
+                if (!all) P::drop(values, in, g);
                 P::outputs(values, s, st);
                 if (more) {
                     P::load_values(p, rows, r, g, values);

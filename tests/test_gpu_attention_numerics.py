@@ -110,3 +110,60 @@ def test_infinite_values_of_small_weights(dtype, below, n, where, kv):
     assert torch.all(out[..., 5] == math.inf) and torch.all(out[..., 9] == -math.inf)
     rest = [i for i in range(d) if i not in (5, 9)]
     assert torch.all(out[..., rest].isfinite())
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("n", [1, 40, 3000])
+@pytest.mark.parametrize("kv", [1, 2])
+def test_scores_of_minus_infinity(dtype, n, kv):
+    """Keys of score -inf weigh nothing; where there are no others the
+    fraction is 0 / 0."""
+    g, d = gen(n), 64
+    table, pages = deal(g, [n, n + 1], 16, 200 if n > 1000 else None)
+    keys, values = torch.zeros(pages, 16, kv, d), randn(g, pages, 16, kv, d)
+    keys[..., 0] = -math.inf
+    keys[table[1, 0].long(), 0, :, 0] = 1.0
+    q = torch.zeros(2, 2, d)
+    q[..., 0] = 1.0
+    q, keys, values = q.to(dtype), keys.to(dtype), values.to(dtype)
+    out, lse = attend(q, keys, values, table, [n, n + 1], 1.0)
+    assert torch.all(out[0].isnan()) and torch.all(lse[0] == -math.inf)
+    first = values[table[1, 0].long(), 0].expand(2, d) if kv == 1 else values[table[1, 0].long(), 0]
+    assert torch.equal(out[1], first) and torch.all((lse[1] - 1.0).abs() <= 2.0 ** -21)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,window", [(1, 0), (33, 0), (65, 0), (65, 49), (3001, 0), (3009, 2993)])
+@pytest.mark.parametrize("kv", [1, 2])
+def test_keys_outside_add_nothing(dtype, n, window, kv):
+    """The keys of a tile behind a sequence's end and before its window are not
+    the nearest attended key again, not even a little: its value is 2^60, its
+    weight 2^-110, every other value 0.  The weight's argument of 110 is off by
+    2^-24 of itself for its product with the scale and 2^-24 for the scale, the
+    weight by 2 ln 2 of that, 110 times 2^-22.5 in all."""
+    g, d = gen(n), 64
+    table, pages = deal(g, [n], 16, 200 if n > 1000 else None)
+    keys, values = (torch.zeros(pages, 16, kv, d) for _ in range(2))
+    last = (n - 1) if window == 0 else n - window   # next to the keys that do not count
+    if n > 1:
+        keys[table[0, last // 16].long(), last % 16, :, 0] = -110.0
+    values[table[0, last // 16].long(), last % 16] = 2.0 ** 60
+    q = torch.zeros(1, 2, d)
+    q[..., 0] = 1.0
+    q, keys, values = q.to(dtype), keys.to(dtype), values.to(dtype)
+    ref, _, _, _ = bounds.attend(q, keys, values, table.clamp(min=0), [n], math.log(2.0), window)
+    out, _ = attend(q, keys, values, table, [n], math.log(2.0), window)
+    assert torch.all((out.double() / ref - 1).abs() <= 110 * 2.0 ** -22.5 + 2.0 ** -22 + bounds.HALF_STEP[dtype])
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("n,window", [(1, 0), (33, 0), (65, 49), (3001, 2985)])
+@pytest.mark.parametrize("kv", [1, 2])
+def test_infinite_values_next_to_keys_outside(dtype, n, window, kv):
+    """The first and last attended keys, infinite ones: infinite, not NaN."""
+    g, d = gen(n), 64
+    table, pages = deal(g, [n], 16, 200 if n > 1000 else None)
+    keys, values = randn(g, pages, 16, kv, d), randn(g, pages, 16, kv, d)
+    for at, sign in ((n - 1, 1.0), (max(0, n - window) if window else 0, 1.0)):
+        values[table[0, at // 16].long(), at % 16, :, 7] = sign * math.inf
+    out, _ = attend(randn(g, 1, 2, d).to(dtype), keys.to(dtype), values.to(dtype), table, [n], 0.125, window)
+    assert torch.all(out[..., 7] == math.inf) and torch.all(out[..., :7].isfinite())
