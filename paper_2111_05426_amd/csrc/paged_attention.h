@@ -192,7 +192,7 @@ template <int NT> struct Columns {
 };
 
 // The running maximum takes in the products s; returns them as weights, 1 for
-// one at the maximum.  scale > 0: base-2 logarithms per unit of s.  `in`:
+// one at the maximum.  scale >= 0: base-2 logarithms per unit of s.  `in`:
 // bit i says whether s[i] counts (looked at unless `all`); one that does not
 // becomes the weight 0.
 template <int N, int NT>
@@ -216,10 +216,13 @@ __device__ inline void weigh(float (&s)[N], float scale, bool all, uint32_t in, 
     }
     const float m = st.m == -HUGE_VALF ? 0.0f : st.m;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -m));
-        st.l += s[i];   // (exp2(-inf) = 0 for those that do not count)
+    for (int i = 0; i < N; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -m));
+    if (!all) {   // (a scale of 0 times -inf is NaN)
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] = in >> i & 1 ? s[i] : 0.0f;
     }
+#pragma unroll
+    for (int i = 0; i < N; ++i) st.l += s[i];
 }
 
 // Keys and values; STREAM: they are read once and leave the caches soon.
@@ -861,8 +864,7 @@ __global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Param
             typename P::Query q;
             P::load_query(p, static_cast<const T *>(p.q) + b * p.q_row + (q0 + (r < heads ? r : 0)) * p.q_head,
                           r < heads, g, q);
-            // (not 0, which times the -inf of a key that does not count were NaN)
-            const float scale = fmaxf(fabsf(p.scale) * (p.k_scale ? p.k_scale[kv] : 1.0f), 0x1p-120f);
+            const float scale = fabsf(p.scale) * (p.k_scale ? p.k_scale[kv] : 1.0f);
             const CT *kb = static_cast<const CT *>(p.k) + kv * p.head_stride;
             const CT *vb = static_cast<const CT *>(p.v) + kv * p.head_stride;
             // The next tile's keys are on their way as soon as the scores are

@@ -167,3 +167,21 @@ def test_infinite_values_next_to_keys_outside(dtype, n, window, kv):
         values[table[0, at // 16].long(), at % 16, :, 7] = sign * math.inf
     out, _ = attend(randn(g, 1, 2, d).to(dtype), keys.to(dtype), values.to(dtype), table, [n], 0.125, window)
     assert torch.all(out[..., 7] == math.inf) and torch.all(out[..., :7].isfinite())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("scale", [0.0, -0.0, 2.0 ** -126])
+@pytest.mark.parametrize("n", [5, 40, 3001])
+@pytest.mark.parametrize("kv", [1, 2])
+def test_tiny_scales_of_large_products(dtype, scale, n, kv):
+    """Products of up to 2^126: with a scale of 0 every key weighs the same."""
+    g, d = gen(n), 64
+    table, pages = deal(g, [n], 16, 200 if n > 1000 else None)
+    keys, values = torch.zeros(pages, 16, kv, d), randn(g, pages, 16, kv, d)
+    keys[..., 0] = torch.randint(-1, 2, (pages, 16, kv), generator=g) * 2.0 ** 63
+    q = torch.zeros(1, 2, d)
+    q[..., 0] = 2.0 ** 63
+    q, keys, values = q.to(dtype), keys.to(dtype), values.to(dtype)
+    ref, ref_lse, room, lse_room = bounds.attend(q, keys, values, table.clamp(min=0), [n], scale)
+    out, lse = attend(q, keys, values, table, [n], scale)
+    assert bounds.within(out, ref, room) and torch.all((lse.double() - ref_lse).abs() <= lse_room)
