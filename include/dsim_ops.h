@@ -116,6 +116,7 @@ DSIM_API dsim_status dsim_kv_append(const dsim_kv_cache *cache, int64_t n_tok, i
  *   q, out: one row per sequence of n_q_heads heads, both of `dtype`: the
  *           cache's type, or DSIM_F16 / DSIM_BF16 with an e4m3 cache;
  *           out may be q (with its strides); it must not overlap otherwise
+ *   scale:  in [-2^126, 2^126]
  *   seq_len: device array [n_seq].  0: out is 0 and lse -inf.  Negative: the
  *           sequence's rows of out, lse and status are left as they were.
  *   lse:    device array [n_seq][n_q_heads] fp32, or NULL

@@ -174,7 +174,8 @@ dsim_status dsim_paged_attention(const dsim_kv_cache *cache, int32_t dtype, cons
     if ((st = check_dtype(dtype, cache))) return st;
     if (n_q_heads < 1 || n_q_heads > kMaxHeads || n_q_heads % cache->n_heads)
         return fail(DSIM_ERANGE, "n_q_heads must be a multiple of n_heads (%d) and at most %d", cache->n_heads, kMaxHeads);
-    if (!std::isfinite(scale)) return fail(DSIM_EINVAL, "scale must be finite");
+    // (times log2 e it has to be finite too)
+    if (!(std::fabs(scale) <= 0x1p126f)) return fail(DSIM_EINVAL, "scale must be in [-2^126, 2^126]");
     if (window < 0) return fail(DSIM_EINVAL, "window must be >= 0");
     if (cache->n_seq == 0) return DSIM_OK;
     const int es = elem_size(dtype);
