@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/core/grad_mode.h>
+#include <c10/core/AutogradState.h>
 #include <c10/hip/HIPStream.h>
 #include <hip/hip_runtime.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -69,8 +70,14 @@ class Call {
         // (what autograd recorded of it would end here without a word)
         if (t.requires_grad() && at::GradMode::is_enabled())
             refuse(name, "requires a gradient, which the operator has not: detach it or call under torch.no_grad()");
+        if (t._fw_grad(0).defined() && c10::AutogradState::get_tls_state().get_fw_grad_mode())
+            refuse(name, "carries a tangent, which the operator has not: take its primal");
         return &t;
     }
+
+    // A tensor that the call writes: one that an earlier operation saved for
+    // its backward pass is then known to have changed.
+    void writes(const at::Tensor &t) { written_[n_written_++] = &t; }
 
     // The tensor's shape (kAny entries free), the last dimension contiguous
     // (all of it if `whole`), on a GPU and on the others' device.
@@ -92,12 +99,14 @@ class Call {
             refuse(name, "must be on " + device_.str() + " with " + first_ + ", not on " + t.device().str());
     }
 
-    template <class T> T *vector(const char *name, PyObject *o, at::ScalarType type, int64_t n, bool optional = true)
+    template <class T>
+    T *vector(const char *name, PyObject *o, at::ScalarType type, int64_t n, bool optional = true, bool written = false)
     {
         const at::Tensor *t = get(name, o, optional);
         if (!t) return nullptr;
         type_is(name, *t, type);
         check(name, *t, {n}, true);
+        if (written) writes(*t);
         return static_cast<T *>(data(*t));
     }
 
@@ -145,6 +154,8 @@ class Call {
             }
             throw PythonError();
         }
+        for (int i = 0; i < n_written_; ++i)   // (tensors of inference mode keep no versions)
+            if (!written_[i]->is_inference()) written_[i]->unsafeGetTensorImpl()->bump_version();
     }
 
   private:
@@ -157,6 +168,8 @@ class Call {
     const char *fn_, *first_ = nullptr;
     PyObject *stream_;
     c10::Device device_{c10::kCPU};
+    const at::Tensor *written_[4];   // (the most that a call writes)
+    int n_written_ = 0;
 };
 
 PyObject *item(PyObject *dict, const char *key)
@@ -175,7 +188,7 @@ void element_type(const char *name, const at::Tensor &t, bool cache)
     }
 }
 
-dsim_kv_cache cache_of(Call &c, PyObject *cache, PyObject *table)
+dsim_kv_cache cache_of(Call &c, PyObject *cache, PyObject *table, bool written)
 {
     if (!PyDict_Check(cache)) refuse("cache", "must be a dict");
     const at::Tensor &k = *c.get("cache['k']", item(cache, "k")), &v = *c.get("cache['v']", item(cache, "v"));
@@ -186,6 +199,10 @@ dsim_kv_cache cache_of(Call &c, PyObject *cache, PyObject *table)
     c.check("cache['v']", v, {n[0], n[1], n[2], n[3]});
     for (int i = 0; i < 4; ++i)
         if (n[i] > 1 && v.strides()[i] != s[i]) refuse("cache['v']", "must have the strides of cache['k']");
+    if (written) {
+        c.writes(k);
+        c.writes(v);
+    }
     const at::Tensor &t = *c.get("block_table", table);
     c.type_is("block_table", t, at::kInt);
     c.check("block_table", t, {kAny, kAny});
@@ -215,7 +232,7 @@ dsim_kv_cache cache_of(Call &c, PyObject *cache, PyObject *table)
 void kv_append(PyObject *const *a)
 {
     Call c("dsim_kv_append", a[11]);
-    const dsim_kv_cache cache = cache_of(c, a[0], a[1]);
+    const dsim_kv_cache cache = cache_of(c, a[0], a[1], true);
     const at::Tensor &k = *c.get("k", a[2]), &v = *c.get("v", a[3]);
     element_type("k", k, false);
     c.check("k", k, {kAny, cache.n_heads, cache.head_dim});
@@ -244,8 +261,9 @@ void kv_append(PyObject *const *a)
         c.check("q_out", *q_out, {n, heads, cache.head_dim});
         qr = c.rows(*q);
         qo = c.rows(*q_out);
+        c.writes(*q_out);
     }
-    int32_t *status = c.vector<int32_t>("status", a[10], at::kInt, n);
+    int32_t *status = c.vector<int32_t>("status", a[10], at::kInt, n, true, true);
     c.run([&](void *stream) {
         return dsim_kv_append(&cache, n, dtype_of(k), &kr, &vr, q ? &qr : nullptr, q ? &qo : nullptr, (int32_t)heads, seq,
                               pos, rope ? static_cast<const float *>(c.data(*rope)) : nullptr, rope ? rope->size(0) : 0,
@@ -257,7 +275,7 @@ void kv_append(PyObject *const *a)
 void paged_attention(PyObject *const *a)
 {
     Call c("dsim_paged_attention", a[10]);
-    const dsim_kv_cache cache = cache_of(c, a[1], a[2]);
+    const dsim_kv_cache cache = cache_of(c, a[1], a[2], false);
     const int64_t n = cache.n_seq;
     const at::Tensor &q = *c.get("q", a[0]), &out = *c.get("out", a[4]);
     element_type("q", q, false);
@@ -278,8 +296,11 @@ void paged_attention(PyObject *const *a)
         c.type_is("lse", *lse, at::kFloat);
         c.check("lse", *lse, {n, heads}, true);
     }
-    int32_t *status = c.vector<int32_t>("status", a[9], at::kInt, n);
+    int32_t *status = c.vector<int32_t>("status", a[9], at::kInt, n, true, true);
     const dsim_rows qr = c.rows(q), o = c.rows(out);
+    c.writes(out);
+    c.writes(ws);
+    if (lse) c.writes(*lse);
     c.run([&](void *stream) {
         return dsim_paged_attention(&cache, dtype_of(q), &qr, &o, (int32_t)heads, len, (float)scale, (int32_t)window,
                                     lse ? static_cast<float *>(c.data(*lse)) : nullptr, status, c.data(ws),
@@ -302,6 +323,7 @@ void logit_adjust(PyObject *const *a)
     dsim_logits s{};
     s.logits = c.data(x);
     s.out = c.data(y);
+    c.writes(y);
     s.logits_stride = x.stride(0);
     s.out_stride = y.stride(0);
     s.n_rows = n;

@@ -24,9 +24,11 @@ Every call runs on the device of its tensors, on `stream` (a torch stream or
 a raw handle; None: that device's current stream), where its tensors must be
 ready.  Like the rest of the binding the calls raise ValueError for tensors
 that do not match what the library reads or writes, before any launch, and
-DsimError where the library refuses.  None has a backward pass: a tensor that
-requires a gradient is refused while gradients are recorded.  The checks and the call are host C++
-(binding/ops_binding.cpp, built as _ops.so); there is no fallback.
+DsimError where the library refuses.  None has a derivative: a tensor that
+requires a gradient is refused while gradients are recorded, and one that
+carries a tangent; what a call writes counts as changed in place.  The checks
+and the call are host C++ (binding/ops_binding.cpp, built as _ops.so); there
+is no fallback.
 """
 from . import dsim
 from .dsim import DsimError  # noqa: F401  (what the calls raise)
