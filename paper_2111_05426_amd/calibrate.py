@@ -52,7 +52,8 @@ the GPT models that the simulator studies and fits
     t = launch_s + bytes / mem_bytes_per_s
 
 by non-negative least squares on relative error, bytes being what the op
-cannot do without.
+cannot do without.  What a call reads comes from memory, not from the
+last-level cache: it is timed on copies of its tensors in turn.
 """
 import argparse
 import json
@@ -206,6 +207,7 @@ DECODE_SHAPES = [(1, 128, 12, 64), (1, 4096, 12, 64), (16, 1024, 12, 64), (64, 1
                  (1, 2048, 12, 128), (1, 65536, 12, 128), (32, 2048, 12, 128), (128, 2048, 12, 128),
                  (512, 1024, 12, 128)]
 DECODE_VOCAB, DECODE_PAGE = 50257, 16
+LAST_LEVEL_CACHE = 256 << 20   # bytes of MI355X's
 
 
 def fit_roofline(nbytes, seconds):
@@ -215,59 +217,91 @@ def fit_roofline(nbytes, seconds):
     return (launch, 1.0 / per_byte if per_byte > 0.0 else float("inf")), worst
 
 
-def _timed(call, reps, warmup):
-    """Seconds per call of `reps` back-to-back ones."""
+def _copies(nbytes, reps):
+    """How many copies of a call's tensors `reps` calls take in turn so that
+    none finds its own in the last-level cache: two caches' worth of others
+    between one use and the next, or a copy for every call."""
+    return max(1, min(reps, 1 - (-2 * LAST_LEVEL_CACHE // nbytes)))
+
+
+def _timed(calls, reps, warmup, device="cuda"):
+    """Seconds per call of `reps` back-to-back ones, taken in turn; what they
+    read is not in the last-level cache, as in a step whose weights and other
+    layers' caches go through it between one layer's call and its next."""
     import torch
-    for _ in range(warmup):
-        call()
+    for i in range(warmup):
+        calls[i % len(calls)]()
+    torch.zeros(2 * LAST_LEVEL_CACHE, dtype=torch.uint8, device=device)
     torch.cuda.synchronize()
     e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     e0.record()
-    for _ in range(reps):
-        call()
+    for i in range(reps):
+        calls[i % len(calls)]()
     e1.record()
     torch.cuda.synchronize()
     return e0.elapsed_time(e1) * 1e-3 / reps
 
 
-def measure_decode(shapes=DECODE_SHAPES, dtype="fp16", reps=20, warmup=3):
+def _decode_calls(batch, context, heads, d, dt, reps, gen, device):
+    """A single-token step's operators on one shape: (op, bytes, calls) each,
+    the calls on tensors of their own."""
+    import torch
+    from . import ops
+    e = torch.tensor([], dtype=dt).element_size()
+
+    def randn(*shape):
+        return torch.randn(*shape, device=device, generator=gen).to(dt)
+
+    width = -(-context // DECODE_PAGE)
+    nbytes = {"append": batch * (6 * heads * d * e + 12) + d * 4,
+              "attention": 2 * batch * heads * d * e * (context + 1) + 4 * batch * (width + 1),
+              "logits": batch * (2 * DECODE_VOCAB * e + 4 * context + 8)}
+    n = {op: _copies(b, reps) for op, b in nbytes.items()}
+    pages = n["attention"] * batch * width
+    cache = {name: randn(pages, heads, DECODE_PAGE, d).transpose(1, 2) for name in ("k", "v")}
+    tables = torch.randperm(pages, device=device, generator=gen).to(torch.int32).view(-1, batch, width)
+    seq = torch.arange(batch, dtype=torch.int32, device=device)
+    length = torch.full((batch,), context, dtype=torch.int32, device=device)
+    rope = ops.rope_table(context, d, device=device)
+    ws = ops.alloc_paged_attention_workspace(heads, heads, d, device=device)
+    penalty = torch.full((batch,), 1.1, device=device)
+    qkv = randn(n["append"], batch, 3 * heads, d)
+    turned = torch.empty(n["append"], batch, heads, d, dtype=dt, device=device)
+    queries = randn(n["attention"], batch, heads, d)
+    out = torch.empty_like(queries)
+    logits = randn(n["logits"], batch, DECODE_VOCAB)
+    adjusted = torch.empty_like(logits)
+    tokens = torch.randint(0, DECODE_VOCAB, (n["logits"], batch, context), device=device, generator=gen, dtype=torch.int32)
+
+    def append(i):
+        (q, k, v), o = qkv[i].split(heads, dim=1), turned[i]
+        # (no two calls write one slot, as long as there are more slots than calls)
+        table, last = tables[i % len(tables)], length - 1 - i // len(tables) % context
+        return lambda: ops.dsim_kv_append(cache, table, k, v, seq, last, rope=rope, q=q, q_out=o)
+
+    def attention(i):
+        q, table, o = queries[i], tables[i], out[i]
+        return lambda: ops.dsim_paged_attention(q, cache, table, length, o, workspace=ws)
+
+    def adjust(i):
+        x, y, history = logits[i], adjusted[i], tokens[i]
+        return lambda: ops.dsim_logit_adjust(x, y, history=history, history_len=length, repetition=penalty)
+
+    return [(op, nbytes[op], [call(i) for i in range(n[op])])
+            for op, call in (("append", append), ("attention", attention), ("logits", adjust))]
+
+
+def measure_decode(shapes=DECODE_SHAPES, dtype="fp16", reps=20, warmup=3, device="cuda"):
     """Seconds per call of a single-token step's operators; rows of (op,
     batch, context, heads, head size, bytes, seconds)."""
     import torch
-    from . import ops
     dt = {"fp16": torch.float16, "bf16": torch.bfloat16, "fp32": torch.float32}[dtype]
-    e = torch.tensor([], dtype=dt).element_size()
-    gen = torch.Generator(device="cuda").manual_seed(0)
-
-    def randn(*shape):
-        return torch.randn(*shape, device="cuda", generator=gen).to(dt)
-
+    gen = torch.Generator(device=device).manual_seed(0)
     rows = []
-    for batch, context, heads, d in shapes:
-        width = -(-context // DECODE_PAGE)
-        cache = {n: randn(batch * width, heads, DECODE_PAGE, d).transpose(1, 2) for n in ("k", "v")}
-        table = torch.randperm(batch * width, device="cuda", generator=gen).to(torch.int32).view(batch, width)
-        seq = torch.arange(batch, dtype=torch.int32, device="cuda")
-        length = torch.full((batch,), context, dtype=torch.int32, device="cuda")
-        last = length - 1
-        rope = ops.rope_table(context, d)
-        qkv = randn(batch, 3 * heads, d)
-        q, k, v = qkv.split(heads, dim=1)
-        q_out, out = torch.empty_like(q), torch.empty_like(q)
-        ws = ops.alloc_paged_attention_workspace(heads, heads, d)
-        logits, adjusted = randn(batch, DECODE_VOCAB), torch.empty(batch, DECODE_VOCAB, dtype=dt, device="cuda")
-        tokens = torch.randint(0, DECODE_VOCAB, (batch, context), device="cuda", generator=gen, dtype=torch.int32)
-        penalty = torch.full((batch,), 1.1, device="cuda")
-        for op, nbytes, call in (
-                ("append", batch * (6 * heads * d * e + 12) + d * 4,
-                 lambda: ops.dsim_kv_append(cache, table, k, v, seq, last, rope=rope, q=q, q_out=q_out)),
-                ("attention", 2 * batch * heads * d * e * (context + 1) + 4 * batch * (width + 1),
-                 lambda: ops.dsim_paged_attention(q_out, cache, table, length, out, workspace=ws)),
-                ("logits", batch * (2 * DECODE_VOCAB * e + 4 * context + 8),
-                 lambda: ops.dsim_logit_adjust(logits, adjusted, history=tokens, history_len=length,
-                                               repetition=penalty))):
-            rows.append((op, batch, context, heads, d, nbytes, _timed(call, reps, warmup)))
-        del cache, logits, adjusted, tokens
+    for shape in shapes:
+        for op, nbytes, calls in _decode_calls(*shape, dt, reps, gen, device):
+            rows.append((op, *shape, nbytes, _timed(calls, reps, warmup, device)))
+        del calls
     return rows
 
 
