@@ -8,7 +8,9 @@ choices) and packed-fp32 instructions disabled.  The binding (_ops.so) is
 host C++ against torch's headers, linked to libdsim.so beside it.
 """
 import glob
+import importlib.util
 import os
+import shutil
 import subprocess
 import sys
 import sysconfig
@@ -53,14 +55,29 @@ def _build_library(hipcc, verbose):
     os.replace(LIB + ".tmp", LIB)
 
 
+def _torch_root():
+    """torch's folder, or None; torch itself is not imported."""
+    spec = importlib.util.find_spec("torch")
+    return os.path.dirname(spec.origin) if spec and spec.origin else None
+
+
 def _build_binding(verbose):
-    import torch
-    root = os.path.dirname(os.path.abspath(torch.__file__))
+    """The operators' binding; without torch's headers or a C++ compiler it is
+    left out, and the operators' Python calls raise ImportError."""
+    root, cxx = _torch_root(), os.environ.get("CXX", "g++")
+    lacks = ("torch's headers" if not root or not os.path.isdir(os.path.join(root, "include", "torch")) else
+             "a C++ compiler (%s)" % cxx if not shutil.which(cxx.split()[0]) else None)
+    if os.path.exists(BINDING):
+        os.remove(BINDING)   # (one of another library's)
+    if lacks:
+        print("the operators' Python binding is not built: it needs %s" % lacks, file=sys.stderr)
+        return
     rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
-    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
-           "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", "-I", INCLUDE, "-isystem", os.path.join(root, "include"),
-           "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
-           "-isystem", os.path.join(rocm, "include"), "-isystem", sysconfig.get_paths()["include"]]
+    cmd = cxx.split() + ["-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
+                         "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", "-I", INCLUDE,
+                         "-isystem", os.path.join(root, "include"),
+                         "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+                         "-isystem", os.path.join(rocm, "include"), "-isystem", sysconfig.get_paths()["include"]]
     cmd += binding_sources() + ["-o", BINDING + ".tmp", "-L", HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN",
                                 "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
                                 "-lc10_hip"]
