@@ -131,6 +131,13 @@ class Call {
         if (stream_ == Py_None) {
             stream = c10::hip::getCurrentHIPStream((c10::DeviceIndex)device).stream();
         } else {
+            if (!PyLong_Check(stream_)) {
+                PyObject *of = PyObject_GetAttrString(stream_, "device_index");
+                const long index = of ? PyLong_AsLong(of) : device;
+                Py_XDECREF(of);
+                PyErr_Clear();   // (another library's stream need not say)
+                if (index != device) refuse("stream", "must be on " + device_.str() + " with " + first_);
+            }
             PyObject *h = PyLong_Check(stream_) ? Py_NewRef_(stream_) : PyObject_GetAttrString(stream_, "cuda_stream");
             if (!h) throw PythonError();
             stream = PyLong_AsVoidPtr(h);
