@@ -185,3 +185,64 @@ def test_tiny_scales_of_large_products(dtype, scale, n, kv):
     ref, ref_lse, room, lse_room = bounds.attend(q, keys, values, table.clamp(min=0), [n], scale)
     out, lse = attend(q, keys, values, table, [n], scale)
     assert bounds.within(out, ref, room) and torch.all((lse.double() - ref_lse).abs() <= lse_room)
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("group", [1, 2])
+def test_streamed_cache(dtype, cache, d, group):
+    """A few sequences in a cache larger than the last-level cache under block
+    tables with room for all of it: keys and values are read past the caches."""
+    kv, slots, lens = 4, 16, [1, 50, 3000, 0, 700]
+    size = torch.tensor([], dtype=cache).element_size()
+    pages = 320_000_000 // (2 * slots * kv * d * size)
+    g = gen(d + group)
+    big = ops.alloc_kv_cache(pages, slots, kv, d, cache)
+    near, count = deal(g, lens, slots)   # the same pages numbered from 0
+    used = torch.randperm(pages, generator=g)[:count]
+    keys, values = (x.to(cache) for x in cache_like(g, count, slots, kv, d, F32 if cache == E4M3 else cache, "slot"))
+    for c, x in ((big["k"], keys), (big["v"], values)):
+        if cache == E4M3:
+            c.view(torch.uint8)[used.cuda()] = x.view(torch.uint8).cuda()
+        else:
+            c[used.cuda()] = x.cuda()
+    table = torch.zeros(len(lens), pages, dtype=torch.int32)
+    table[:, :near.shape[1]] = torch.where(near < 0, -1, used[near.clamp(min=0).long()]).to(torch.int32)
+    q = (2 * randn(g, len(lens), kv * group, d)).to(dtype)
+    out = torch.empty(q.shape, dtype=dtype, device="cuda")
+    ops.dsim_paged_attention(q.cuda(), big, table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), out)
+    ref, _, room, _ = bounds.attend(q, keys, values, near.clamp(min=0), lens, d ** -0.5)
+    assert bounds.within(out.cpu(), ref, room)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("scale", [0.0, -0.2, 3.0])
+@pytest.mark.parametrize("kv", [2, 4])
+def test_scales_of_cut_contexts(dtype, scale, kv):
+    g, d, lens = gen(kv), 64, [40, 2500, 0, 300]
+    table, pages = deal(g, lens, 16, 200)
+    keys, values = cache_like(g, pages, 16, kv, d, dtype)
+    q = randn(g, len(lens), 4, d).to(dtype)
+    ref, ref_lse, room, lse_room = bounds.attend(q, keys, values, table.clamp(min=0), lens, scale)
+    out, lse = attend(q, keys, values, table, lens, scale)
+    some = torch.tensor(lens) > 0
+    assert bounds.within(out, ref, room) and torch.all((lse.double() - ref_lse)[some].abs() <= lse_room[some])
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("n_seq", [3, 300])   # joined by context, by workgroup
+def test_strided_rows_of_cut_contexts(dtype, n_seq):
+    """q and out as parts of wider tensors, written by the join."""
+    g, d, kv = gen(n_seq), 64, 2
+    lens = [2500, 9, 1700] + [3] * (n_seq - 3)
+    table, pages = deal(g, lens, 16, 200)
+    keys, values = cache_like(g, pages, 16, kv, d, dtype)
+    wide = randn(g, n_seq, 9, 96).to(dtype)
+    q = wide[:, 1:5, 16:80]
+    big = torch.zeros(n_seq, 8, 128, dtype=dtype, device="cuda")
+    ops.dsim_paged_attention(wide.cuda()[:, 1:5, 16:80], dict(k=to_gpu(keys), v=to_gpu(values)), table.cuda(),
+                             torch.tensor(lens, dtype=torch.int32, device="cuda"), big[:, 2:6, 32:96])
+    ref, _, room, _ = bounds.attend(q, keys, values, table.clamp(min=0), lens, 0.125)
+    assert bounds.within(big[:, 2:6, 32:96].cpu(), ref, room)
+    big[:, 2:6, 32:96] = 0
+    assert torch.all(big == 0)
