@@ -168,16 +168,18 @@ __device__ inline float sum_groups(float x)
     return z[0] + z[1];
 }
 
-// What sums held against the maximum `from` count against the maximum `to`.
-// Where there was none (-inf) they are held against 0: zero, or NaN, which
-// has to stay.
-__device__ inline float rescale(float from, float to)
+// What sums held against the maximum `from` count against the maximum `to`,
+// both products of query and key, `scale` base-2 logarithms per unit.  Where
+// there was none (-inf) they are held against 0: zero, or NaN, which has to
+// stay.  (Differences are scaled, not maxima subtracted from scaled products:
+// a scaled maximum above 2^31 is rounded by more than an exponent can be.)
+__device__ inline float rescale(float from, float to, float scale)
 {
-    return from == -HUGE_VALF ? 1.0f : __builtin_amdgcn_exp2f(from - to);
+    return from == -HUGE_VALF ? 1.0f : __builtin_amdgcn_exp2f((from - to) * scale);
 }
 
-// Running state of one wave: for column r (a query head) the maximum m, this
-// lane's share of the sum l, and the output's rows.
+// Running state of one wave: for column r (a query head) the largest product
+// m, this lane's share of the sum l, and the output's rows.
 template <int NT> struct Columns {
     float m, l;
     f32x4 o[NT];
@@ -205,10 +207,10 @@ __device__ inline void weigh(float (&s)[N], float scale, bool all, uint32_t in, 
     float top = s[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) top = fmaxf(top, s[i]);
-    top = max_groups(top) * scale;
+    top = max_groups(top);
     if (__builtin_amdgcn_ballot_w64(top > st.m) != 0) {
         const float m = fmaxf(st.m, top);
-        const float f = rescale(st.m, m);
+        const float f = rescale(st.m, m, scale);
         st.l *= f;
 #pragma unroll
         for (int e = 0; e < NT; ++e) st.o[e] *= f;
@@ -216,7 +218,7 @@ __device__ inline void weigh(float (&s)[N], float scale, bool all, uint32_t in, 
     }
     const float m = st.m == -HUGE_VALF ? 0.0f : st.m;
 #pragma unroll
-    for (int i = 0; i < N; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -m));
+    for (int i = 0; i < N; ++i) s[i] = __builtin_amdgcn_exp2f((s[i] - m) * scale);
     if (!all) {   // (a scale of 0 times -inf is NaN)
 #pragma unroll
         for (int i = 0; i < N; ++i) s[i] = in >> i & 1 ? s[i] : 0.0f;
@@ -607,16 +609,16 @@ template <int DP, bool EXACT, bool STREAM> struct OnePass : Pass<float, float, D
         top = fmaxf(top, turn<8>(top));
         top = fmaxf(top, turn<4>(top));
         top = fmaxf(top, turn<2>(top));
-        top = fmaxf(top, turn<1>(top)) * scale;
+        top = fmaxf(top, turn<1>(top));
         if (__builtin_amdgcn_ballot_w64(top > st.m) != 0) {
-            const float m = fmaxf(st.m, top), f = rescale(st.m, m);
+            const float m = fmaxf(st.m, top), f = rescale(st.m, m, scale);
             st.l *= f;
 #pragma unroll
             for (int j = 0; j < kQuads; ++j) st.o[j] *= f;
             st.m = m;
         }
         const float m = st.m == -HUGE_VALF ? 0.0f : st.m;
-        s[0] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0], scale, -m));
+        s[0] = __builtin_amdgcn_exp2f((s[0] - m) * scale);
         s[0] = counts ? s[0] : 0.0f;
         st.l += s[0];
     }
@@ -734,12 +736,16 @@ __device__ inline void write_row(const Params &p, int b, int head, int d, f32x4 
     *reinterpret_cast<vec<T, 4> *>(static_cast<T *>(p.out) + b * p.out_row + head * p.out_head + d) = from_f32<T, 4>(x);
 }
 
-__device__ inline void write_lse(const Params &p, int b, int head, float m, float l, bool empty, int32_t bad)
+__device__ inline void write_lse(const Params &p, int b, int head, float m, float scale, float l, bool empty, int32_t bad)
 {
     if (p.lse)
         p.lse[(int64_t)b * p.n_q_heads + head] =
-            bad ? __builtin_nanf("") : empty ? -HUGE_VALF : (m + __builtin_log2f(l)) * kLn2;
+            bad ? __builtin_nanf("") : empty ? -HUGE_VALF : (m * scale + __builtin_log2f(l)) * kLn2;
 }
+
+// Base-2 logarithms per unit of the products with a cache head's keys (which
+// are negated for a negative scale).
+__device__ inline float scale_of(const Params &p, int kv) { return fabsf(p.scale) * (p.k_scale ? p.k_scale[kv] : 1.0f); }
 
 // A part of a context: d outputs of each head, then the heads' maxima and
 // sums; 16-byte aligned.
@@ -857,6 +863,7 @@ __global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Param
         const bool whole = n == sp.n;
         const int32_t *row = p.table + b * p.table_stride;
 
+        const float scale = scale_of(p, kv);
         typename P::State st;
         st.clear();
         if (sp.len > 0) {
@@ -864,7 +871,6 @@ __global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Param
             typename P::Query q;
             P::load_query(p, static_cast<const T *>(p.q) + b * p.q_row + (q0 + (r < heads ? r : 0)) * p.q_head,
                           r < heads, g, q);
-            const float scale = fabsf(p.scale) * (p.k_scale ? p.k_scale[kv] : 1.0f);
             const CT *kb = static_cast<const CT *>(p.k) + kv * p.head_stride;
             const CT *vb = static_cast<const CT *>(p.v) + kv * p.head_stride;
             // The next tile's keys are on their way as soon as the scores are
@@ -926,7 +932,7 @@ __global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Param
         float top = s_m[0][r];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
-        const float f = rescale(st.m, top);
+        const float f = rescale(st.m, top, scale);
         P::store(st, f, s_o[wave], heads, r, g);
         if (g == 0) {
             s_l[wave][r] = l * f;
@@ -951,7 +957,7 @@ __global__ __launch_bounds__(kBlock, per_cu(DP, sizeof(CT))) void k_attend(Param
             o *= vs;
             if (whole) {
                 write_row<T>(p, b, q0 + h, d, o, sum, sp.len == 0, bad);
-                if (d == 0) write_lse(p, b, q0 + h, s_top[h], sum, sp.len == 0, bad);
+                if (d == 0) write_lse(p, b, q0 + h, s_top[h], scale, sum, sp.len == 0, bad);
             } else {
                 *reinterpret_cast<f32x4 *>(part.o + h * p.d + d) = o;
                 if (d == 0) {
@@ -990,6 +996,7 @@ template <class T, int W> __global__ __launch_bounds__(kBlock) void k_join(Param
     if (p.by_context && p.seq_len[blockIdx.x / (p.n_heads * p.tiles_of_heads)] < 0) return;
     if (n == 0) return;
     const bool used = h < p.part_heads && q0 + h < (q0 / p.group + 1) * p.group;   // (a last tile may have fewer heads)
+    const float scale = scale_of(p, q0 / p.group);
     auto part = [&](int i) { return Part::of(p, i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)); };
     const int quads = p.d / 4 / (int)gridDim.z, ways = kThreads / quads, way = tid / quads;
     const int d0 = 4 * (tid - way * quads + (int)blockIdx.z * quads);
@@ -1021,15 +1028,15 @@ template <class T, int W> __global__ __launch_bounds__(kBlock) void k_join(Param
         }
     }
     float l = 0.0f;
-    for (int i = tid; used && i < n; i += kThreads) l += rescale(part(i).m[h], m) * part(i).l[h];
+    for (int i = tid; used && i < n; i += kThreads) l += rescale(part(i).m[h], m, scale) * part(i).l[h];
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o);
     f32x4 o = {0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < kAhead; ++j)
-        if (way + j * ways < count) o += rescale(part(way + j * ways).m[h], m) * ahead[j];
+        if (way + j * ways < count) o += rescale(part(way + j * ways).m[h], m, scale) * ahead[j];
 #pragma unroll 4
-    for (int i = way + kAhead * ways; i < count; i += ways) o += rescale(part(i).m[h], m) * output(i);
+    for (int i = way + kAhead * ways; i < count; i += ways) o += rescale(part(i).m[h], m, scale) * output(i);
     s_o[threadIdx.x] = o;
     if (lane == 0) s_l[wave] = l;
     __syncthreads();
@@ -1042,7 +1049,7 @@ template <class T, int W> __global__ __launch_bounds__(kBlock) void k_join(Param
         write_row<T>(p, b, q0 + h, d0, o, l, false, bad);
     }
     if (tid == 0 && blockIdx.z == 0) {
-        write_lse(p, b, q0 + h, m, l, false, bad);
+        write_lse(p, b, q0 + h, m, scale, l, false, bad);
         if (p.status) p.status[b] = bad;
     }
 }

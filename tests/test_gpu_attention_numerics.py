@@ -246,3 +246,29 @@ def test_strided_rows_of_cut_contexts(dtype, n_seq):
     assert bounds.within(big[:, 2:6, 32:96].cpu(), ref, room)
     big[:, 2:6, 32:96] = 0
     assert torch.all(big == 0)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("power", [10, 15, 40])
+@pytest.mark.parametrize("n", [5, 100, 3000])
+@pytest.mark.parametrize("kv", [1, 2])
+def test_large_scores(dtype, power, n, kv):
+    """Scores of up to 2^80: those at the maximum share the whole weight (the
+    others lie 2^6 and more below it), however coarse the maximum itself is."""
+    if dtype == F16 and power > 15:
+        pytest.skip("beyond the type")
+    g, d = gen(n + power), 64
+    table, pages = deal(g, [n], 16, 200 if n > 1000 else None)
+    keys, values = torch.zeros(pages, 16, kv, d), randn(g, pages, 16, kv, d)
+    keys[..., 0] = torch.randint(-4, 5, (pages, 16, kv), generator=g) * 2.0 ** (power - 3)
+    q = torch.zeros(1, 2, d)
+    q[0, :, 0] = torch.tensor([1.0, -0.75]) * 2.0 ** power
+    q, keys, values = q.to(dtype), keys.to(dtype), values.to(dtype)
+    scale = 0.1
+    ref, ref_lse, _, _ = bounds.attend(q, keys, values, table.clamp(min=0), [n], scale)
+    out, lse = attend(q, keys, values, table, [n], scale)
+    # a mean of n values at most: n roundings of sums of them and of the weights'
+    assert bounds.within(out, ref, n * 2.0 ** -23 * values.double().abs().max())
+    # the scaled maximum and the logarithm of the count, at most 12, rounded to
+    # fp32, scaled by ln 2 and added: 2^-24 of each four times
+    assert torch.all((lse.double() - ref_lse).abs() <= (ref_lse.abs() + 2 * 12) * 2.0 ** -22)
