@@ -272,3 +272,59 @@ def test_large_scores(dtype, power, n, kv):
     # the scaled maximum and the logarithm of the count, at most 12, rounded to
     # fp32, scaled by ln 2 and added: 2^-24 of each four times
     assert torch.all((lse.double() - ref_lse).abs() <= (ref_lse.abs() + 2 * 12) * 2.0 ** -22)
+
+
+@pytest.mark.parametrize("dtype,cache", [(F32, F32), (BF16, BF16), (F16, E4M3)])
+@pytest.mark.parametrize("slots,lens", [(16, [160, 3]), (16, [3200, 3199, 1]), (7, [70, 69]), (1000, [3000, 999, 1001]),
+                                        (4096, [4096, 17])])
+def test_contexts_that_fill_the_table(dtype, cache, slots, lens):
+    """Lengths up to the table's last slot, windows as long as contexts, and a
+    table that is a part of a wider one."""
+    g, d, kv = gen(slots + len(lens)), 64, 2
+    width = -(-lens[0] // slots)
+    table, pages = deal(g, lens, slots, width)
+    keys, values = (x.to(cache) for x in cache_like(g, pages, slots, kv, d, F32 if cache == E4M3 else cache))
+    q = (2 * randn(g, len(lens), 4, d)).to(dtype)
+    wide = torch.full((len(lens), width + 4), -9, dtype=torch.int32)
+    wide[:, 1:width + 1] = table
+    dev = dict(k=to_gpu(keys), v=to_gpu(values))
+    for window in (0, lens[0], lens[0] - 1, 2 ** 31 - 1):
+        out = torch.zeros(q.shape, dtype=dtype, device="cuda")
+        status = torch.full((len(lens),), -7, dtype=torch.int32, device="cuda")
+        ops.dsim_paged_attention(q.cuda(), dev, wide.cuda()[:, 1:width + 1],
+                                 torch.tensor(lens, dtype=torch.int32, device="cuda"), out, window=window, status=status)
+        ref, _, room, _ = bounds.attend(q, keys, values, table.clamp(min=0), lens, 0.125, window)
+        assert bounds.within(out.cpu(), ref, room) and not status.any()
+
+
+@pytest.mark.parametrize("heads,kv", [(1024, 1024), (1024, 4), (1000, 8)])
+@pytest.mark.parametrize("width", WIDTHS)
+def test_as_many_heads_as_are_taken(heads, kv, width):
+    g, d, lens = gen(heads), 16, [33, 300]
+    table, pages = deal(g, lens, 16, width)
+    keys, values = cache_like(g, pages, 16, kv, d, BF16)
+    q = (2 * randn(g, 2, heads, d)).bfloat16()
+    ref, ref_lse, room, lse_room = bounds.attend(q, keys, values, table.clamp(min=0), lens, 0.25)
+    out, lse = attend(q, keys, values, table, lens, 0.25)
+    assert bounds.within(out, ref, room) and torch.all((lse.double() - ref_lse).abs() <= lse_room)
+
+
+def test_more_sequences_than_threads():
+    """Most of them left alone, some empty, a few long."""
+    g, d, n = gen(5), 64, 3000
+    lens = [-1] * n
+    for i in range(0, n, 7):
+        lens[i] = 0
+    for i, x in ((0, 900), (13, 2500), (1499, 1), (1500, 3000), (2999, 77)):
+        lens[i] = x
+    table, pages = deal(g, lens, 16, 190)
+    keys, values = cache_like(g, pages, 16, 2, d, BF16)
+    q = (2 * randn(g, n, 4, d)).bfloat16()
+    ref, ref_lse, room, lse_room = bounds.attend(q, keys, values, table.clamp(min=0), lens, 0.125)
+    out, lse = attend(q, keys, values, table, lens, 0.125)
+    lens = torch.tensor(lens)
+    assert torch.all(out[lens < 0] == 9.0) and torch.all(lse[lens < 0] == 9.0)
+    assert torch.all(out[lens == 0] == 0.0) and torch.all(lse[lens == 0] == -math.inf)
+    some = lens > 0
+    assert bounds.within(out[some], ref[some], room[some])
+    assert torch.all((lse.double() - ref_lse)[some].abs() <= lse_room[some])
