@@ -5,8 +5,12 @@
 // written once, and one row of the rotation table: 3 flops per 2 elements
 // moved, so memory bounds it, and latency a call of few tokens.  On MI355X
 // 24,588 tokens of prompts (bf16, 32 query and 8 cache heads of 128, 606 MB)
-// take 108 us, 5.6 TB/s; one token of 12 heads of 64 takes 3.2 us.  (Loading a
-// thread's next chunk before the one at hand is stored costs 14 us more.)
+// take 108 us, 5.6 TB/s; one token of 12 heads of 64 takes the kernel 3.0 us and
+// calls one after another 4.5.  A token's first wait is for its sequence and
+// position, the second for its page, the third for the row (the load stands
+// behind the page's check), the fourth for the row's other half and the
+// rotation.  (Loading a thread's next chunk before the one at hand is stored
+// costs the 24,588 tokens 14 us more.)
 #include "numeric.h"
 #include "ops.h"
 
@@ -137,9 +141,12 @@ template <class T, class CT, int VEC> void launch(const AppendArgs &a, hipStream
     // 128 threads 5.4).  Many: fewer and busier threads, so that fewer
     // workgroups start (24,588 tokens 114 us, with 512 threads 173, both
     // with plain stores); one wave where a token has few chunks, or an e4m3
-    // cache needs more arithmetic for each (8,192 tokens, by one wave and
-    // two: bf16, 12 query and 2 cache heads of 64 11.7 and 13.2 us, 12 and 12
-    // 17.4 and 16.7; in e4m3 17.6 and 18.2; 32 and 8 of 128 33.3 and 32.5).
+    // cache needs more arithmetic for each.  8,192 tokens by one wave and two,
+    // bf16 of 96 chunks 10.9 and 11.9 us, 128 11.9 and 12.4, 192 16.4 and
+    // 15.8, 448 33.7 and 33.7; fp16 neighbours into e4m3 of 192 chunks 12.7 and
+    // 14.3, 288 17.0 and 18.2, 336 20.6 and 21.6, 384 19.9 and 19.9, 480 37.2
+    // and 35.4.  (At 2,048 tokens e4m3 loses from 240 chunks on: 288 7.6 and
+    // 7.0.)
     const int n_rot = a.interleaved ? a.rot_dim / VEC : a.rot_dim / 2 / VEC, rest = (a.c.head_dim - a.rot_dim) / VEC;
     const int64_t chunks = (int64_t)(a.n_q_heads + a.c.n_heads) * (n_rot + rest) + (int64_t)a.c.n_heads * (a.c.head_dim / VEC);
     const int64_t few = sizeof(CT) == 1 ? 320 : 128;

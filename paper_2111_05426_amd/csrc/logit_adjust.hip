@@ -8,10 +8,11 @@
 // slice, so the row's counts never reach memory.  Every workgroup of a row
 // reads the whole history, from L2 after the first.
 //
-// On MI355X, 512 rows of 50,257 in fp16, histories up to 1,024, 300 biases and
-// a mask (108 MB) take 30 us, 3.6 TB/s; 64 rows of 131,072 in bf16, histories
-// up to 8,192, 16 biases and a mask (36 MB) 15.6; one row 3.6.  Memory bounds
-// the bare pass (18.6 us of the 30, 5.9 of the 15.6); the rest is a chain of
+// On MI355X the kernel takes, for 512 rows of 50,257 in fp16, histories up to
+// 1,024, 300 biases and a mask (108 MB) 30 us, 3.6 TB/s; for 64 rows of 131,072
+// in bf16, histories up to 8,192, 16 biases and a mask (36 MB) 14.0; for one
+// row 3.7 (calls one after another 33.7, 15.1 and 3.9).  Memory bounds
+// the bare pass (18.6 us of the 30, 5.9 of the 14.0); the rest is a chain of
 // short phases between barriers that the few workgroups of a CU hide only in
 // part: counting 4 and 6 us, mask 2.5, biases 3.  (Penalties applied by the
 // threads that hold the history's tokens, each token claimed once by an atomic

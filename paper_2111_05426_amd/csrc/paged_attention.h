@@ -6,16 +6,19 @@
 // byte in bf16; the card's balance is over 150), and what has to be kept up is
 // loads in flight: 16 bytes a lane, a tile's keys requested again as soon as
 // their scores are known, its values as soon as the outputs are.  One pass:
-// the maximum and the sum run along in fp32.  Matrix instructions make the
-// products cheap (35 to 45% of the vector issue slots are left busy by
-// addresses, exponentials and the widening of e4m3); a sequence's keys take
-// part in them straight from the loads, with nothing in shared memory.
-// On MI355X (us, both launches): bf16, 32 query and 8 cache heads of 128, 64
-// sequences of up to 4,096 tokens (538 MB) 98.7, 5.45 TB/s; 64 query heads, 4
-// of 131,072 (2.1 GB) 330, 6.5 TB/s; e4m3, 128 of up to 8,192 (1.14 GB) 193,
-// 5.9 TB/s; fp32, 16 sequences, 12 heads of 80, window 1,000 (100 MB) 28.5,
-// 3.5 TB/s; fp16, one of 97 tokens, 12 heads of 64, 5.7.  Reads alone, in
-// pieces of 4 to 64 KB, reach 6.0 to 6.5 TB/s.
+// the maximum and the sum run along in fp32, and weights keep fp32's bits.
+// Matrix instructions make the products cheap; addresses, exponentials, the
+// weights' parts and the widening of e4m3 take a fifth of the vector issue
+// slots with bf16, 43% with e4m3.  A sequence's keys take part in the products
+// straight from the loads, with nothing in shared memory.
+// On MI355X (us a call, both launches, calls one after another on several
+// copies of the tensors): bf16, 32 query and 8 cache heads of 128, 64 sequences
+// of up to 4,096 tokens (538 MB) 98.7, 5.45 TB/s; 64 query heads, 4 of 131,072
+// (2.1 GB) 330, 6.5 TB/s; e4m3, 128 of up to 8,192 (1.14 GB) 196, 5.8 TB/s;
+// fp32, 16 sequences, 12 heads of 80, window 1,000 (100 MB) 27.9, 3.6 TB/s;
+// fp16, one of 97 tokens, 12 heads of 64, 6.1.  Reads alone, in pieces of 4 to
+// 64 KB, reach 6.0 to 6.5 TB/s.  Figures beside the rules below are of calls
+// captured into a graph, on two copies in turn: up to 5% above or below.
 #pragma once
 
 #include "numeric.h"
@@ -236,8 +239,8 @@ template <bool STREAM, class V> __device__ inline V read(const void *p)
 // Whether rows of d elements, more than DP / 2 of them (but for the smallest
 // DP) and padded to DP, reach beyond element `at`: the same for all lanes.
 // What none of them needs is neither loaded nor multiplied (fp32, 64
-// sequences, 12 cache heads of 176, 48 query heads, window 450: 121 us; with
-// all of the padding 138; 12 of 80, window 1,000: 105 and 110).
+// sequences, 12 cache heads of 176, 48 query heads, window 450: 116 us; with
+// all of the padding 118; 12 of 80, window 1,000: 105 and 112).
 template <int DP, bool EXACT> __device__ inline bool needed(const Params &p, int at)
 {
     return EXACT || at <= (DP > 64 ? DP / 2 : 0) || at < p.d;
@@ -549,8 +552,8 @@ struct Pass<float, float, DP, EXACT, STREAM> : ByColumns<Pass<float, float, DP, 
 
 // fp32, a cache head with one query head: fifteen of the matrix instructions'
 // sixteen columns would be empty, and in fp32 they are slow enough to show
-// (16 sequences of 12 heads of 80, window 1,000: 35.3 us, this way 29.3; 256
-// of up to 64 tokens 51 and 42; 64 of up to 4,096 the same), so the products
+// (16 sequences of 12 heads of 80, window 1,000: 30.8 us, this way 26.9; 256
+// of up to 64 tokens 42.5 and 35.2; 64 of up to 4,096 193 and 188), so the products
 // are ordinary ones.  Keys and values lie as above; a lane sums its
 // chunks of key r's product, the groups' sums are added, and the weights of
 // its own keys 4 g + i come from its row's lanes.
@@ -1099,9 +1102,9 @@ template <class T, class CT, int DP> dsim_status launch(Params &p, hipStream_t s
     p.by_context = !p.direct && contexts <= p.grid;
     const dim3 grid((unsigned)(p.direct ? contexts : p.grid)), block(kBlock);
     // What the last-level cache (256 MB) cannot keep until the next step is
-    // read past it: a batch of 64 up to 4,096 tokens (538 MB) 98.6 us, with
-    // plain loads 108; 131,072 tokens x 4 (2.1 GB) 348 and 383.  What it may
-    // keep is not: 8,000 tokens (33 MB) read again 17.4 us, streamed 19.4.
+    // read past it: a batch of 64 up to 4,096 tokens (538 MB) 99 us, with
+    // plain loads 108; 131,072 tokens x 4 (2.1 GB) 345 and 381.  What it may
+    // keep is not: 8,000 tokens (33 MB) read again 18.7 us, streamed 20.0.
     // Nor are rows of other lengths than 64, 128 and 256, whose lines are
     // touched more than once (heads of 80: 97 us, with plain loads 76), nor
     // pages of other sizes than multiples of 16 (heads of 64: 61 and 63).
