@@ -1,5 +1,5 @@
 // kv_append.hip -- new keys and values rotated and written into a paged
-// cache, queries rotated on the way (dsim_kv_append).
+// cache, queries rotated on the way (dsim_kv_append, dsim_kv_append_axes).
 //
 // A token is (n_q_heads + 2 n_heads) rows of head_dim elements read once and
 // written once, and one row of the rotation table: 3 flops per 2 elements
@@ -11,6 +11,7 @@
 // behind the page's check), the fourth for the row's other half and the
 // rotation.  (Loading a thread's next chunk before the one at hand is stored
 // costs the 24,588 tokens 14 us more.)
+#include "multi_ops.h"
 #include "numeric.h"
 #include "ops.h"
 
@@ -36,18 +37,27 @@ struct Place {
     int64_t at;
     int32_t status, pos;
     bool skip;
+    int32_t axis[DSIM_MAX_AXES];   // positions of the rotation, where it has its own
 };
 
-__device__ inline Place place_of(const AppendArgs &a, int64_t t)
+template <bool AXES> __device__ inline Place place_of(const AppendArgs &a, const AxesArgs &x, int64_t t)
 {
-    Place p{0, 0, 0, false};
+    Place p{0, 0, 0, false, {}};
     const int32_t s = a.seq[t];
     p.pos = a.pos[t];
     p.skip = s < 0;
     if (p.skip) return p;
     if (s >= a.c.n_seq) p.status |= DSIM_ST_BAD_SEQUENCE;
-    if (p.pos < 0 || (int64_t)p.pos >= (int64_t)a.c.table_width * a.c.page_size || (a.rope && p.pos >= a.n_rope))
+    if (p.pos < 0 || (int64_t)p.pos >= (int64_t)a.c.table_width * a.c.page_size || (!AXES && a.rope && p.pos >= a.n_rope))
         p.status |= DSIM_ST_BAD_POSITION;
+    if constexpr (AXES) {
+#pragma unroll
+        for (int i = 0; i < DSIM_MAX_AXES; ++i) {
+            const int32_t at = i < x.n_axes ? x.pos[t * x.n_axes + i] : 0;
+            if (at < 0 || (i < x.n_axes && at >= a.n_rope)) p.status |= DSIM_ST_BAD_POSITION;
+            p.axis[i] = at;
+        }
+    }
     if (p.status) return p;
     const int32_t page = a.c.block_table[s * a.c.table_stride + p.pos / a.c.page_size];
     if (page < 0 || page >= a.c.n_pages)
@@ -61,10 +71,53 @@ __device__ inline Place place_of(const AppendArgs &a, int64_t t)
 // call's chunks a token: 2^17, a row's: 64)
 __device__ inline uint32_t divide(uint32_t j, uint32_t mul) { return mul ? __umulhi(j, mul) : j; }
 
+// Cosines and sines of pairs e .. e + N - 1, which with positions on several
+// axes need not lie in one row of the table.
+template <bool AXES, int N>
+__device__ inline void angles(const AppendArgs &a, const AxesArgs &x, const Place &p, const float *cs, int e,
+                              vec<float, N> &c, vec<float, N> &s)
+{
+    using V = vec<float, N>;
+    const int half = a.rot_dim / 2;
+    if constexpr (AXES) {
+        const auto row = [&](int pair) {
+            int at = p.axis[0];
+#pragma unroll
+            for (int i = 1; i < DSIM_MAX_AXES; ++i) at = pair >= x.end[i - 1] ? p.axis[i] : at;
+            return a.rope + (int64_t)at * a.rot_dim;
+        };
+        const float *r = row(e), *last = row(e + N - 1);
+        c = *reinterpret_cast<const V *>(r + e);
+        s = *reinterpret_cast<const V *>(r + half + e);
+        if (r != last) {   // (a section ends inside, or both ends happen to be of different rows)
+#pragma unroll
+            for (int k = 1; k < N; ++k) {
+                const float *at = row(e + k);
+                c[k] = at[e + k];
+                s[k] = at[half + e + k];
+            }
+        } else {
+            // sections between that begin and end inside
+#pragma unroll
+            for (int k = 1; k < N - 1; ++k) {
+                const float *at = row(e + k);
+                if (at != r) {
+                    c[k] = at[e + k];
+                    s[k] = at[half + e + k];
+                }
+            }
+        }
+    } else {
+        c = *reinterpret_cast<const V *>(cs + e);
+        s = *reinterpret_cast<const V *>(cs + half + e);
+    }
+}
+
 // T: type of the new rows; CT: of the cache; VEC: elements per load.  A
 // thread takes one chunk of VEC elements, or, where pairs (i, i + R/2) are
 // rotated, one chunk of each half.
-template <class T, class CT, int VEC> __global__ __launch_bounds__(kMaxBlock) void k_append(AppendArgs a, uint32_t mul_head, uint32_t mul_value)
+template <class T, class CT, int VEC, bool AXES>
+__global__ __launch_bounds__(kMaxBlock) void k_append(AppendArgs a, AxesArgs axes, uint32_t mul_head, uint32_t mul_value)
 {
     using V = vec<float, VEC>;
     const int d = a.c.head_dim, rot = a.rot_dim;
@@ -72,7 +125,7 @@ template <class T, class CT, int VEC> __global__ __launch_bounds__(kMaxBlock) vo
     const int per_head = n_rot + (d - rot) / VEC, per_value = d / VEC;
     const int n_q = a.n_q_heads * per_head, n_k = a.c.n_heads * per_head, n_v = a.c.n_heads * per_value;
     for (int64_t t = blockIdx.x; t < a.n_tok; t += gridDim.x) {
-        const Place p = place_of(a, t);
+        const Place p = place_of<AXES>(a, axes, t);
         if (threadIdx.x == 0 && a.status) a.status[t] = p.status;
         if (p.skip) continue;
         const float *cs = a.rope ? a.rope + (p.status ? 0 : (int64_t)p.pos * rot) : nullptr;
@@ -105,13 +158,14 @@ template <class T, class CT, int VEC> __global__ __launch_bounds__(kMaxBlock) vo
             V x = load_row<T, VEC>(src.data, from + e), y;
             if (two) {
                 y = load_row<T, VEC>(src.data, from + e2);
-                const V cosv = *reinterpret_cast<const V *>(cs + e), sinv = *reinterpret_cast<const V *>(cs + rot / 2 + e);
+                V cosv, sinv;
+                angles<AXES, VEC>(a, axes, p, cs, e, cosv, sinv);
                 const V z = x * cosv - y * sinv;
                 y = y * cosv + x * sinv;
                 x = z;
             } else if (turned) {
-                using H = vec<float, VEC / 2>;
-                const H co = *reinterpret_cast<const H *>(cs + e / 2), si = *reinterpret_cast<const H *>(cs + (rot + e) / 2);
+                vec<float, VEC / 2> co, si;
+                angles<AXES, VEC / 2>(a, axes, p, cs, e / 2, co, si);
 #pragma unroll
                 for (int k = 0; k < VEC; k += 2) {
                     const float z = x[k] * co[k / 2] - x[k + 1] * si[k / 2];
@@ -134,7 +188,7 @@ template <class T, class CT, int VEC> __global__ __launch_bounds__(kMaxBlock) vo
     }
 }
 
-template <class T, class CT, int VEC> void launch(const AppendArgs &a, hipStream_t s)
+template <class T, class CT, int VEC, bool AXES> void launch(const AppendArgs &a, const AxesArgs &x, hipStream_t s)
 {
     // A workgroup takes a token.  Few tokens: a thread for every chunk, up to
     // 512 (bf16, 32 query and 8 cache heads of 128: 256 tokens 4.1 us, with
@@ -154,39 +208,43 @@ template <class T, class CT, int VEC> void launch(const AppendArgs &a, hipStream
     const int block = (int)((chunks + 64 * rounds - 1) / (64 * rounds)) * 64;
     const dim3 grid((unsigned)(a.n_tok < (1 << 20) ? a.n_tok : (1 << 20)));
     const auto mul = [](int n) { return n > 1 ? (uint32_t)((((uint64_t)1 << 32) + n - 1) / n) : 0u; };
-    hipLaunchKernelGGL((k_append<T, CT, VEC>), grid, dim3(block), 0, s, a, mul(n_rot + rest), mul(a.c.head_dim / VEC));
+    hipLaunchKernelGGL((k_append<T, CT, VEC, AXES>), grid, dim3(block), 0, s, a, x, mul(n_rot + rest), mul(a.c.head_dim / VEC));
 }
 
-template <class T, class CT> void launch(const AppendArgs &a, hipStream_t s)
+template <class T, class CT, bool AXES> void launch(const AppendArgs &a, const AxesArgs &x, hipStream_t s)
 {
     // chunks of 16 bytes of T; 4 elements where a half of the rotated part
     // is no whole number of 8
     if constexpr (sizeof(T) == 4) {
-        launch<T, CT, 4>(a, s);
+        launch<T, CT, 4, AXES>(a, x, s);
     } else {
         if (a.rot_dim % 16)
-            launch<T, CT, 4>(a, s);
+            launch<T, CT, 4, AXES>(a, x, s);
         else
-            launch<T, CT, 8>(a, s);
+            launch<T, CT, 8, AXES>(a, x, s);
     }
+}
+
+template <bool AXES> dsim_status launch_any(const AppendArgs &a, const AxesArgs &x, hipStream_t s)
+{
+    if (a.dtype == DSIM_F32)
+        launch<float, float, AXES>(a, x, s);
+    else if (a.dtype == DSIM_F16 && a.c.dtype == DSIM_F16)
+        launch<f16, f16, AXES>(a, x, s);
+    else if (a.dtype == DSIM_BF16 && a.c.dtype == DSIM_BF16)
+        launch<bf16, bf16, AXES>(a, x, s);
+    else if (a.dtype == DSIM_F16)
+        launch<f16, e4m3, AXES>(a, x, s);
+    else
+        launch<bf16, e4m3, AXES>(a, x, s);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? DSIM_OK : hip_fail(e, "append launch");
 }
 
 }  // namespace
 
-dsim_status launch_append(const AppendArgs &a, hipStream_t s)
-{
-    if (a.dtype == DSIM_F32)
-        launch<float, float>(a, s);
-    else if (a.dtype == DSIM_F16 && a.c.dtype == DSIM_F16)
-        launch<f16, f16>(a, s);
-    else if (a.dtype == DSIM_BF16 && a.c.dtype == DSIM_BF16)
-        launch<bf16, bf16>(a, s);
-    else if (a.dtype == DSIM_F16)
-        launch<f16, e4m3>(a, s);
-    else
-        launch<bf16, e4m3>(a, s);
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? DSIM_OK : hip_fail(e, "append launch");
-}
+dsim_status launch_append(const AppendArgs &a, hipStream_t s) { return launch_any<false>(a, AxesArgs{}, s); }
+
+dsim_status launch_append_axes(const AppendArgs &a, const AxesArgs &x, hipStream_t s) { return launch_any<true>(a, x, s); }
 
 }  // namespace dsim

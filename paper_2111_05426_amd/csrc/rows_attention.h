@@ -1,0 +1,887 @@
+// rows_attention.h -- the kernels of dsim_prompt_attention and
+// dsim_tree_attention: attention of many rows (query tokens times the query
+// heads of one cache head) over paged keys and values.
+#pragma once
+
+#include <type_traits>
+
+#include "multi_ops.h"
+#include "numeric.h"
+
+namespace dsim {
+namespace rows {
+
+constexpr int kWaves = 4;
+constexpr int kBlock = 64 * kWaves;
+constexpr int kCus = 256;
+constexpr int kMaxGrid = 2 * kCus;
+constexpr int kPlan = 1024;          // threads of the plan
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// What a block of rows costs beside its tiles, in tiles.
+constexpr int kExtra = 4;
+constexpr int kMinTiles = 4;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+struct Params {
+    const void *k, *v, *q;
+    void *out;
+    const float *k_scale, *v_scale, *slopes;
+    const int32_t *table, *start, *len, *prefix_len, *first_key, *depth;
+    const uint32_t *mask;
+    float *lse;
+    int32_t *status;
+    int64_t n_pages, page_stride, slot_stride, head_stride, table_stride, q_row, q_head, out_row, out_head, mask_stride;
+    int64_t n_tok, max_blocks;
+    // the plan, in the workspace
+    int64_t *cost;        // [max_blocks + 1] sums of the blocks' costs, one head's
+    int2 *span;           // [max_blocks] keys of a block
+    int32_t *first;       // [n_seq + 1] sequences' first blocks
+    int4 *cut;            // [kMaxGrid]
+    float *part;
+    float scale, cap;     // scale: natural units
+    int32_t n_seq, n_heads, d, page_size, table_width, window, mask_words;
+    int32_t group, n_q_heads, rows;   // rows of a block
+    bool tree, direct;
+    uint32_t page_mul, page_shift, group_mul, group_shift;   // t / n = t * mul >> shift, 0 <= t < 2^31
+};
+
+__device__ inline int32_t divide(int32_t t, uint32_t mul, uint32_t shift)
+{
+    return (int32_t)((uint64_t)(uint32_t)t * mul >> shift);
+}
+
+// A sequence of the call.
+struct Seq {
+    int32_t start, n, len;   // first token, tokens, length as given
+    int32_t keys;            // all of them (none if bad)
+    int32_t bad;             // its rows are NaN
+    int32_t status;
+};
+
+__device__ inline Seq seq_of(const Params &p, int s)
+{
+    Seq x;
+    x.start = p.start[s];
+    x.len = p.len[s];
+    const int32_t end = p.start[s + 1];
+    x.n = 0;
+    x.keys = 0;
+    x.bad = x.status = 0;
+    if (x.len < 0) return x;
+    if (x.start < 0 || end < x.start || end > p.n_tok) {
+        x.status = DSIM_ST_BAD_POSITION;
+        return x;
+    }
+    x.n = end - x.start;
+    const int64_t keys = p.tree ? (int64_t)x.len + x.n : x.len;
+    if (keys > (int64_t)p.table_width * p.page_size || (p.tree ? x.n > 32 * (int64_t)p.mask_words : x.n > x.len))
+        x.bad = x.status = DSIM_ST_BAD_POSITION;
+    else
+        x.keys = (int32_t)keys;
+    return x;
+}
+
+__device__ inline int32_t blocks_of(const Params &p, const Seq &x)
+{
+    return (int32_t)(((int64_t)x.n * p.group + p.rows - 1) / p.rows);
+}
+
+// The keys that a token may attend to but for the mask of a tree: lo <= j <
+// hi; position: that of the token.
+struct Range {
+    int32_t lo, hi, position;
+};
+
+__device__ inline Range range_of(const Params &p, const Seq &x, int32_t i, int32_t prefix, int32_t first_key, int32_t depth)
+{
+    Range r;
+    if (p.tree) {
+        r.position = (int32_t)min((int64_t)x.len + max(depth, 0), (int64_t)INT32_MAX);
+        r.hi = x.len;
+        r.lo = p.window > 0 ? max(r.position - p.window + 1, 0) : 0;
+    } else {
+        r.position = x.len - x.n + i;
+        r.hi = min(max(r.position + 1, prefix), x.len);
+        r.lo = max(p.window > 0 ? max(r.position - p.window + 1, 0) : 0, first_key);
+    }
+    if (x.bad || r.lo >= r.hi) r.lo = r.hi = 0;
+    return r;
+}
+
+__device__ inline Range range_of(const Params &p, const Seq &x, int s, int32_t i)
+{
+    const int32_t t = x.start + i;
+    return range_of(p, x, i, p.prefix_len ? p.prefix_len[s] : 0, p.first_key ? max(p.first_key[t], 0) : 0,
+                    p.depth ? p.depth[t] : 0);
+}
+
+// The keys that some token of tokens i0 to i1 attends to lie in [x, y).
+__device__ inline int2 span_of(const Params &p, const Seq &x, int s, int32_t i0, int32_t i1)
+{
+    if (x.bad) return make_int2(0, 0);
+    if (p.tree) return make_int2(p.window > 0 ? min(max(x.len - p.window + 1, 0), x.len) : 0, x.keys);
+    int lo = INT32_MAX, hi = 0;
+    if (p.first_key) {
+        for (int32_t i = i0; i <= i1; ++i) {
+            const Range r = range_of(p, x, s, i);
+            if (r.lo >= r.hi) continue;
+            lo = min(lo, r.lo);
+            hi = max(hi, r.hi);
+        }
+    } else {   // both grow with the token
+        lo = range_of(p, x, s, i0).lo;
+        hi = range_of(p, x, s, i1).hi;
+    }
+    return lo < hi ? make_int2(lo, hi) : make_int2(0, 0);
+}
+
+template <int KT> __device__ inline int32_t tiles_of(int2 span)
+{
+    return max((span.y + KT - 1) / KT - span.x / KT, 1);
+}
+
+// Sum of x over the workgroup's threads before this one, and the total.
+template <int THREADS> __device__ inline int64_t scan(int64_t x, int64_t *s, int64_t &total)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t incl = x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t y = __shfl_up(incl, o);
+        if (lane >= o) incl += y;
+    }
+    if (lane == 63) s[wave] = incl;
+    __syncthreads();
+    int64_t before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+        if (w < wave) before += s[w];
+        total += s[w];
+    }
+    __syncthreads();
+    return before + incl - x;
+}
+
+// The largest i < n with a(i) <= x, where a does not descend and a(0) <= x:
+// 64 probes at a time, the same for all lanes.
+template <class A> __device__ inline int32_t find(A a, int32_t n, int64_t x)
+{
+    const int lane = threadIdx.x & 63;
+    int32_t lo = 0;
+    while (n > 1) {
+        const int32_t step = (n + 63) / 64, i = lo + lane * step;
+        const bool le = lane * step < n && a(i) <= x;
+        const int last = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(le));   // (lane 0's is)
+        n = min(step, n - last * step);
+        lo += last * step;
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// Blocks of rows, their keys and what they cost, and the sequences' status.
+template <int KT> __global__ __launch_bounds__(kPlan) void k_plan(Params p)
+{
+    __shared__ int64_t s_sum[kPlan / 64];
+    int64_t before = 0, total;
+    for (int s0 = 0; s0 < p.n_seq; s0 += kPlan) {
+        const int s = s0 + threadIdx.x;
+        Seq x{};
+        int64_t n = 0;
+        if (s < p.n_seq) {
+            x = seq_of(p, s);
+            n = blocks_of(p, x);
+        }
+        const int64_t at = before + scan<kPlan>(n, s_sum, total);
+        // (more rows than tokens: starts that descend; what does not fit is refused)
+        if (s < p.n_seq) {
+            p.first[s] = (int32_t)min(at, p.max_blocks);
+            if (at + n > p.max_blocks) x.status = DSIM_ST_BAD_POSITION;
+            if (p.status && x.len >= 0) p.status[s] = x.status;
+        }
+        before += total;
+    }
+    const int32_t n = (int32_t)min(before, p.max_blocks);
+    if (threadIdx.x == 0) p.first[p.n_seq] = n;
+    __syncthreads();
+    before = 0;
+    for (int32_t b0 = 0; b0 < n; b0 += kPlan) {
+        const int32_t b = b0 + threadIdx.x;
+        int64_t cost = 0;
+        if (b < n) {
+            int lo = 0, hi = p.n_seq;   // the last sequence that begins at b or before
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2;
+                (p.first[mid] <= b ? lo : hi) = mid;
+            }
+            const Seq x = seq_of(p, lo);
+            const int32_t r0 = (b - p.first[lo]) * p.rows, r1 = min(r0 + p.rows, x.n * p.group);
+            const int2 span = span_of(p, x, lo, r0 / p.group, (r1 - 1) / p.group);
+            p.span[b] = span;
+            cost = tiles_of<KT>(span) + kExtra;
+        }
+        const int64_t at = before + scan<kPlan>(cost, s_sum, total);
+        if (b < n) p.cost[b] = at;
+        before += total;
+    }
+    if (threadIdx.x == 0) p.cost[n] = before;
+}
+
+// 16 bytes of T hold nothing but numbers
+template <class T> __device__ inline bool finite(u32x4 x)
+{
+    constexpr uint32_t top = __is_same(T, f16) ? 0x7c00u : 0x7f80u;
+    bool ok = true;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (sizeof(T) == 4)
+            ok &= (x[i] & 0x7f800000u) != 0x7f800000u;
+        else
+            ok &= (x[i] & top) != top && (x[i] & top << 16) != top << 16;
+    }
+    return ok;
+}
+
+// eight e4m3 in fp16 or bf16, exactly
+template <class T, bool HIGH> __device__ inline vec<T, 2> widen2(uint32_t w)
+{
+    if constexpr (__is_same(T, f16))
+        return __builtin_bit_cast(vec<T, 2>, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH));
+    else
+        return __builtin_bit_cast(vec<T, 2>, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HIGH));
+}
+
+template <class T> __device__ inline vec<T, 8> widen8(uint32_t lo, uint32_t hi)
+{
+    const vec<T, 2> a = widen2<T, false>(lo), b = widen2<T, true>(lo), c = widen2<T, false>(hi), d = widen2<T, true>(hi);
+    return {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+__device__ inline vec<float, 2> halves(float x)   // those of lanes r and 32 + r
+{
+    const auto y = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return {__builtin_bit_cast(float, (uint32_t)y[0]), __builtin_bit_cast(float, (uint32_t)y[1])};
+}
+
+// tanh, off by less than 2^-20 of itself (fp32: the library's)
+template <bool EXACT> __device__ inline float tanh_of(float y)
+{
+    if constexpr (EXACT) {
+        return tanhf(y);
+    } else {
+        const float a = fabsf(y), z = y * y;
+        const float big = 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(2.0f * kLog2e * a) + 1.0f);
+        // y - y^3 / 3 + 2 y^5 / 15 - 17 y^7 / 315
+        const float small = a * (1.0f + z * (-0.33333333f + z * (0.13333333f + z * -0.05396825f)));
+        return copysignf(a < 0.2f ? small : big, y);
+    }
+}
+
+// Sums held against the maximum `from`, against `to`: see paged_attention.h.
+__device__ inline float rescale(float from, float to, float scale)
+{
+    return from == -HUGE_VALF ? 1.0f : __builtin_amdgcn_exp2f((from - to) * scale);
+}
+
+// T: type of the queries, CT: of the cache, DP: the head's size padded, WR:
+// blocks of 32 rows in a workgroup.  The four waves are WR x WK: those of a
+// block of rows share out the keys of a tile.
+template <class T, class CT, int DP_, int WR_> struct Shape {
+    static constexpr int DP = DP_, WR = WR_, WK = kWaves / WR;
+    static constexpr bool F32 = sizeof(T) == 4;
+    static constexpr int U = !F32 && WR == 4 ? 2 : 1;          // times 32 keys of a tile for each wave
+    static constexpr int KW = 32 * U, KT = WK * KW, M = 32 * WR;
+    static constexpr int PITCH = DP * sizeof(T);               // of a row in shared memory
+    static constexpr int NC = PITCH / 16;                      // its pieces of 16 bytes
+    static constexpr int IN = DP * sizeof(CT) / 16;            // those of a row of the cache
+    static constexpr int NQ = KT * IN / kBlock;                // that a thread loads, of keys and of values
+    static constexpr int SUMS = 32 * DP * 4 * (WK - 1) * WR;   // outputs of waves that are joined
+    static constexpr int LDS = 2 * KT * PITCH > SUMS ? 2 * KT * PITCH : SUMS;
+    static constexpr int PER_CU = DP <= 128 && LDS <= 76 * 1024 ? 2 : 1;   // workgroups, all resident at once
+    // Offset for the weights' exponents.  fp16 ends at 2^-24: weights up to
+    // 2^14 instead of 1 keep all that are above 2^-38 of the largest.
+    static constexpr float UP = __is_same(T, f16) ? 14.0f : 0.0f;
+    // Whether weights enter the second product as two numbers of T.
+    static constexpr bool SPLIT = !F32 && WR < 4;
+
+    // Pieces of a row are permuted by its number so that the lanes that read
+    // a column meet different banks: 16 rows' pieces of keys (16 bytes a
+    // lane), 4 rows of 64 bytes of values (read transposed).
+    __device__ static int key_piece(int row, int c) { return c ^ (NC == 8 ? row >> 1 & 7 : row & 15); }
+    __device__ static int value_piece(int row, int c)
+    {
+        return F32 ? c : c ^ (NC == 8 ? (row >> 1 & 1) << 2 : (row & 3) << 2);
+    }
+};
+
+template <class T> struct Mfma;
+template <> struct Mfma<f16> {
+    __device__ static f32x16 mul(vec<f16, 8> a, vec<f16, 8> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Mfma<bf16> {
+    __device__ static f32x16 mul(vec<bf16, 8> a, vec<bf16, 8> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+
+// A part of a block: the outputs of its rows, their maxima and sums.
+struct Part {
+    float *o, *m, *l;
+    __device__ static Part of(const Params &p, int64_t slot)
+    {
+        float *o = p.part + slot * p.rows * (p.d + 2), *m = o + (int64_t)p.rows * p.d;
+        return {o, m, m + p.rows};
+    }
+};
+
+template <class T>
+__device__ inline void write_row(const Params &p, int64_t t, int head, int d, f32x4 x, float l)
+{
+    // (a row that attends to a bad page has the sum NaN)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = l == 0.0f ? 0.0f : x[k] / l;
+    *reinterpret_cast<vec<T, 4> *>(static_cast<T *>(p.out) + t * p.out_row + head * p.out_head + d) = from_f32<T, 4>(x);
+}
+
+__device__ inline void write_lse(const Params &p, int64_t t, int head, float m, float scale, float l, float up)
+{
+    if (p.lse) p.lse[t * p.n_q_heads + head] = l == 0.0f ? -HUGE_VALF : (m * scale + (__builtin_log2f(l) - up)) * kLn2;
+}
+
+// The scores' way from a product with a cache head's keys (times the sign of
+// the scale) to a base-2 exponent.
+struct Scores {
+    float in, cap, slope;   // slope: of the row; all in base-2 units
+    float unit;             // base-2 units of what is kept as score
+    bool raw;               // scores are products
+    __device__ static Scores of(const Params &p, int kv, float slope)
+    {
+        Scores s;
+        const float scale = fabsf(p.scale) * (p.k_scale ? p.k_scale[kv] : 1.0f);
+        s.raw = p.cap == 0.0f && !p.slopes;
+        s.in = p.cap > 0.0f ? scale / p.cap : scale * kLog2e;
+        s.cap = p.cap * kLog2e;
+        s.slope = slope * kLog2e;
+        s.unit = s.raw ? s.in : 1.0f;
+        return s;
+    }
+};
+
+template <class T, class CT, int DP, int WR>
+__global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR>::PER_CU)) void k_rows(Params p)
+{
+    using S = Shape<T, CT, DP, WR>;
+    constexpr int WK = S::WK, U = S::U, KT = S::KT, M = S::M;
+    constexpr int OB = DP / 32;   // blocks of 32 outputs
+    constexpr int QV = S::F32 ? DP / 8 : DP / 16;
+    using Q = typename std::conditional<S::F32, f32x4, vec<T, 8>>::type;
+    __shared__ __attribute__((aligned(16))) char s_buf[S::LDS];
+    __shared__ float s_m[kWaves][32], s_l[kWaves][32];
+    __shared__ int32_t s_lo, s_hi;
+    __shared__ uint32_t s_bad[2][KT / 32], s_note[2];
+    char *const s_k = s_buf, *const s_v = s_buf + KT * S::PITCH;
+    const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave - wr * WK;
+
+    // this workgroup's run
+    int s, kv, b;         // sequence, cache head, block of the sequence
+    int32_t c0 = 0;
+    int64_t left = 1, run = 0;
+    int32_t index = blockIdx.x;
+    if (p.direct) {
+        // one block of one head: found among the sequences
+        int32_t block = index / p.n_heads;
+        kv = index - block * p.n_heads;
+        for (s = 0; s < p.n_seq; s += 64) {
+            int32_t n = s + lane < p.n_seq ? blocks_of(p, seq_of(p, s + lane)) : 0, incl = n;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int32_t y = __shfl_up(incl, o);
+                if (lane >= o) incl += y;
+            }
+            const uint64_t behind = __builtin_amdgcn_ballot_w64(block < incl);
+            if (behind) {
+                const int at = __builtin_ctzll(behind);
+                block -= __shfl(incl - n, at);
+                s += at;
+                break;
+            }
+            block -= __shfl(incl, 63);
+        }
+        if (s >= p.n_seq) return;
+        s = __builtin_amdgcn_readfirstlane(s);
+        b = __builtin_amdgcn_readfirstlane(block);
+    } else {
+        // neighbouring runs on one XCD
+        index = (index & 7) * (gridDim.x / 8) + (index >> 3);
+        const int32_t blocks = p.first[p.n_seq];
+        const int64_t total = p.cost[blocks] * p.n_heads, even = (total + gridDim.x - 1) / gridDim.x;
+        run = even > kMinTiles ? even : kMinTiles;
+        const int64_t begin = index * run, end = min(begin + run, total);
+        if (begin >= total) {
+            if (tid == 0) p.cut[index] = make_int4(0, 0, 0, 0);
+            return;
+        }
+        left = end - begin;
+        s = find([&](int32_t i) { return p.cost[p.first[i]] * p.n_heads; }, p.n_seq, begin);
+        const int32_t first = p.first[s], n = p.first[s + 1] - first;
+        const int64_t base = p.cost[first], each = p.cost[first + n] - base, at = begin - base * p.n_heads;
+        kv = (int)(at / each);
+        const int64_t z = at - kv * each;
+        b = find([&](int32_t i) { return p.cost[first + i] - base; }, n, z);
+        c0 = (int32_t)(z - (p.cost[first + b] - base));
+    }
+    int4 cut = make_int4(0, 0, 0, 0);
+
+    for (; left > 0; ++b, c0 = 0) {
+        int2 span;
+        Seq x;
+        int32_t t0 = 0, n = 0, tiles = 0;
+        if (p.direct) {
+            left = 0;
+            x = seq_of(p, s);
+            const int32_t r0 = b * M, r1 = min(r0 + M, x.n * p.group);
+            span = span_of(p, x, s, r0 / p.group, (r1 - 1) / p.group);
+            n = tiles = tiles_of<KT>(span);
+        } else {
+            while (b >= p.first[s + 1] - p.first[s]) {   // the next head, or sequence
+                b = 0;
+                if (p.first[s + 1] == p.first[s] || ++kv == p.n_heads) {
+                    kv = 0;
+                    ++s;
+                }
+            }
+            x = seq_of(p, s);
+            span = p.span[p.first[s] + b];
+            tiles = tiles_of<KT>(span);
+            const int32_t cost = tiles + kExtra, c1 = (int32_t)(cost - c0 < left ? cost : c0 + left);
+            left -= c1 - c0;
+            t0 = max(c0 - kExtra, 0);
+            n = max(c1 - kExtra, 0) - t0;
+            if (n == 0) continue;   // the next run begins the block
+        }
+        const int32_t first_tile = span.x / KT;
+        if (span.y == 0) n = 0;   // (no keys: the rows are written all the same)
+
+        // the lane's row
+        const int32_t total_rows = x.n * p.group, row = b * M + wr * 32 + r;
+        const bool valid = row < total_rows;
+        const int32_t my = min(row, total_rows - 1), i = divide(my, p.group_mul, p.group_shift), h = my - i * p.group;
+        const int32_t t = x.start + i, head = kv * p.group + h;
+        const Range in = range_of(p, x, s, i);
+        const Scores sc = Scores::of(p, kv, p.slopes ? p.slopes[head] : 0.0f);
+        const uint32_t *mask = p.tree ? p.mask + t * p.mask_stride : nullptr;
+        Q q[QV];
+        {
+            const T *from = static_cast<const T *>(p.q) + t * p.q_row + head * p.q_head;
+#pragma unroll
+            for (int k = 0; k < QV; ++k) {
+                const int at = (2 * k + g) * (S::F32 ? 4 : 8);
+                const Q y = at < p.d ? *reinterpret_cast<const Q *>(from + at) : Q(0);
+                q[k] = p.scale < 0.0f ? -y : y;
+            }
+        }
+        __syncthreads();   // (the block before has been written, s_lo and s_hi read)
+        if (tid == 0) {
+            s_lo = 0;
+            s_hi = INT32_MAX;
+            s_note[0] = s_note[1] = 0;
+        }
+        if (tid < KT / 32) s_bad[0][tid] = s_bad[1][tid] = 0;
+        __syncthreads();
+        {
+            int32_t lo = in.lo, hi = in.hi;   // all rows attend to the keys of [largest lo, least hi)
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                lo = max(lo, __shfl_xor(lo, o));
+                hi = min(hi, __shfl_xor(hi, o));
+            }
+            if (lane == 0) {
+                atomicMax(&s_lo, lo);
+                atomicMin(&s_hi, hi);
+            }
+        }
+        __syncthreads();
+        const int32_t all_lo = s_lo, all_hi = s_hi;
+
+        const CT *kb = static_cast<const CT *>(p.k) + kv * p.head_stride;
+        const CT *vb = static_cast<const CT *>(p.v) + kv * p.head_stride;
+        const int32_t *table = p.table + s * p.table_stride;
+        u32x4 kx[S::NQ], vx[S::NQ];
+        uint32_t bad_keys = 0;   // bit q: the page of piece q's key
+        auto load = [&](int32_t k0) {
+#pragma unroll
+            for (int j = 0; j < S::NQ; ++j) {
+                const int piece = j * kBlock + tid, c = piece % S::IN;
+                const int32_t key = min(max(k0 + piece / S::IN, span.x), span.y - 1);
+                const int32_t of = divide(key, p.page_mul, p.page_shift), page = table[of];
+                const bool ok = page >= 0 && page < p.n_pages, used = c * (16 / (int)sizeof(CT)) < p.d;
+                bad_keys = (bad_keys & ~(1u << j)) | (uint32_t)!ok << j;
+                kx[j] = vx[j] = u32x4{0, 0, 0, 0};
+                if (ok && used) {
+                    const int64_t at = page * p.page_stride + (key - of * p.page_size) * p.slot_stride + c * (16 / (int)sizeof(CT));
+                    kx[j] = *reinterpret_cast<const u32x4 *>(kb + at);
+                    vx[j] = *reinterpret_cast<const u32x4 *>(vb + at);
+                }
+            }
+        };
+        // pieces of the tile to shared memory; partial: values that are not
+        // finite are told of
+        auto store = [&](int turn, bool partial) {
+            bool odd = false;
+#pragma unroll
+            for (int j = 0; j < S::NQ; ++j) {
+                const int piece = j * kBlock + tid, key = piece / S::IN, c = piece % S::IN;
+                if (bad_keys >> j & 1) {
+                    atomicOr(&s_bad[turn][key / 32], 1u << key % 32);
+                    atomicOr(&s_note[turn], 1u);
+                }
+                if constexpr (sizeof(CT) == 1) {
+                    const auto kk = __builtin_bit_cast(vec<uint32_t, 4>, kx[j]), vv = __builtin_bit_cast(vec<uint32_t, 4>, vx[j]);
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const vec<T, 8> a = widen8<T>(kk[2 * half], kk[2 * half + 1]), v = widen8<T>(vv[2 * half], vv[2 * half + 1]);
+                        *reinterpret_cast<vec<T, 8> *>(s_k + key * S::PITCH + S::key_piece(key, 2 * c + half) * 16) = a;
+                        *reinterpret_cast<vec<T, 8> *>(s_v + key * S::PITCH + S::value_piece(key, 2 * c + half) * 16) = v;
+                        if (partial) odd |= !finite<T>(__builtin_bit_cast(u32x4, v));
+                    }
+                } else {
+                    *reinterpret_cast<u32x4 *>(s_k + key * S::PITCH + S::key_piece(key, c) * 16) = kx[j];
+                    *reinterpret_cast<u32x4 *>(s_v + key * S::PITCH + S::value_piece(key, c) * 16) = vx[j];
+                    if (partial) odd |= !finite<T>(vx[j]);
+                }
+            }
+            if (odd) atomicOr(&s_note[turn], 2u);
+        };
+
+        float m = -HUGE_VALF, l = x.bad ? __builtin_nanf("") : 0.0f;
+        f32x16 o[OB];
+#pragma unroll
+        for (int e = 0; e < OB; ++e) o[e] = f32x16(0.0f);
+
+        if (n > 0) load((first_tile + t0) * KT);
+        for (int32_t tile = t0; tile < t0 + n; ++tile) {
+            const int turn = tile & 1;
+            const int32_t k0 = (first_tile + tile) * KT;
+            const bool partial = !(k0 >= all_lo && k0 + KT <= all_hi);
+            __syncthreads();   // the tile before has been read
+            store(turn, partial);
+            if (tid == 0) s_note[turn ^ 1] = 0;
+            if (tid < KT / 32) s_bad[turn ^ 1][tid] = 0;
+            __syncthreads();
+            if (tile + 1 < t0 + n) load(k0 + KT);
+            const uint32_t note = s_note[turn];
+
+            // scores of the wave's keys (rows) and rows (columns)
+            f32x16 sx[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) sx[u] = f32x16(0.0f);
+#pragma unroll
+            for (int k = 0; k < QV; ++k) {
+                if (k * (S::F32 ? 8 : 16) >= p.d) break;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int key = wk * S::KW + 32 * u + r;
+                    const Q a = *reinterpret_cast<const Q *>(s_k + key * S::PITCH + S::key_piece(key, 2 * k + g) * 16);
+                    if constexpr (S::F32) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sx[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], q[k][e], sx[u], 0, 0, 0);
+                    } else {
+                        sx[u] = Mfma<T>::mul(a, q[k], sx[u]);
+                    }
+                }
+            }
+            // element i of a lane's: key 8 (i / 4) + 4 g + i % 4 of 32
+            uint32_t in32[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int32_t kw = k0 + wk * S::KW + 32 * u;
+                if (!sc.raw) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float y = sx[u][e] * sc.in;
+                        if (p.cap > 0.0f) y = tanh_of<S::F32>(y) * sc.cap;
+                        sx[u][e] = y;
+                    }
+                    if (p.slopes) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            int32_t at = kw + 8 * (e / 4) + 4 * g + e % 4;
+                            if (p.tree && at >= x.len)
+                                at = (int32_t)min((int64_t)x.len + max(p.depth[x.start + min(at - x.len, x.n - 1)], 0), (int64_t)INT32_MAX);
+                            sx[u][e] -= sc.slope * (float)abs(in.position - at);
+                        }
+                    }
+                }
+                in32[u] = ~0u;
+                if (partial) {
+                    const int32_t lo = min(max(in.lo - kw, 0), 32), hi = min(max(in.hi - kw, 0), 32);
+                    in32[u] = (uint32_t)((1ull << hi) - 1) & ~(uint32_t)((1ull << lo) - 1);
+                    if (p.tree && kw + 32 > x.len && kw < x.keys) {
+                        // bits of the nodes from the first of these keys on
+                        const int32_t node = kw - x.len, w = max(node, 0) >> 5;
+                        uint64_t bits = mask[w];
+                        if (w + 1 < p.mask_words) bits |= (uint64_t)mask[w + 1] << 32;
+                        uint32_t word = node < 0 ? (uint32_t)(bits << -node) : (uint32_t)(bits >> (node & 31));
+                        const int32_t end = x.keys - kw;   // > 0
+                        if (end < 32) word &= (1u << end) - 1;
+                        in32[u] |= word;
+                    }
+                    const uint32_t mine = in32[u] >> 4 * g;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        sx[u][e] = mine >> (8 * (e / 4) + e % 4) & 1 ? sx[u][e] : -HUGE_VALF;
+                }
+                if (note & 1) {
+                    if (in32[u] & s_bad[turn][(wk * S::KW + 32 * u) / 32]) {
+                        l = __builtin_nanf("");
+                        if (valid && p.status) atomicOr(&p.status[s], DSIM_ST_BAD_PAGE);
+                    }
+                }
+            }
+            // weights against the running maximum
+            float top = sx[0][0];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, sx[u][e]);
+            {
+                const auto y = halves(top);
+                top = fmaxf(y[0], y[1]);
+            }
+            if (__builtin_amdgcn_ballot_w64(top > m) != 0) {
+                const float to = fmaxf(m, top), f = rescale(m, to, sc.unit);
+                l *= f;
+#pragma unroll
+                for (int e = 0; e < OB; ++e) o[e] *= f;
+                m = to;
+            }
+            const float base = m == -HUGE_VALF ? 0.0f : m;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sx[u][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sx[u][e] - base, sc.unit, S::UP));
+                if (partial) {   // (a scale of 0 times -inf is NaN)
+                    const uint32_t mine = in32[u] >> 4 * g;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sx[u][e] = mine >> (8 * (e / 4) + e % 4) & 1 ? sx[u][e] : 0.0f;
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) l += sx[u][e];
+            }
+            // outputs (rows) of the rows (columns)
+            if (partial && (note & 2)) {
+                // Values that are not finite, and rows that do not attend to
+                // them: a weight of 0 would make them NaN, so each product
+                // stands alone.
+#pragma unroll 1
+                for (int k = 0; k < 32 * U; ++k) {
+                    float mine = 0.0f;   // the weight, in a lane of the key's half
+                    bool attended = false;
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        if (u == k >> 5) attended = in32[u] >> (k & 31) & 1;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (u == k >> 5 && e == (k >> 3 & 3) * 4 + (k & 3)) mine = sx[u][e];
+                    }
+                    const auto both = halves(mine);
+                    const float w = k >> 2 & 1 ? both[1] : both[0];
+                    const int key = wk * S::KW + k;
+#pragma unroll
+                    for (int d = 0; d < OB; ++d)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int at = (32 * d + 8 * e + 4 * g) * (int)sizeof(T);
+                            const vec<float, 4> v = to_f32<T, 4>(*reinterpret_cast<const vec<T, 4> *>(
+                                s_v + key * S::PITCH + S::value_piece(key, at / 16) * 16 + at % 16));
+                            if (attended)
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) o[d][4 * e + c] = __builtin_fmaf(w, v[c], o[d][4 * e + c]);
+                        }
+                }
+            } else if constexpr (S::F32) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int key = wk * S::KW + 8 * (e / 4) + 4 * g + e % 4;
+#pragma unroll
+                    for (int d = 0; d < OB; ++d) {
+                        if (32 * d >= p.d) break;
+                        const float a = *reinterpret_cast<const float *>(s_v + key * S::PITCH + (32 * d + r) * 4);
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, sx[0][e], o[d], 0, 0, 0);
+                    }
+                }
+            } else {
+                typedef short s16x4 __attribute__((ext_vector_type(4)));
+                using lds4 = __attribute__((address_space(3))) s16x4;
+                const int sub = lane & 15;
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        vec<float, 8> w;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) w[e] = sx[u][8 * half + e];
+                        const vec<T, 8> hi = from_f32<T, 8>(w);
+                        vec<T, 8> lo;
+                        if constexpr (S::SPLIT) lo = from_f32<T, 8>(w - to_f32<T, 8>(hi));
+#pragma unroll
+                        for (int d = 0; d < OB; ++d) {
+                            if (32 * d >= p.d) break;
+                            s16x4 part[2];
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const int key = wk * S::KW + 32 * u + 16 * half + 8 * k + 4 * g + sub / 4;
+                                const int at = 32 * d + 16 * (lane >> 4 & 1) + 4 * (sub & 3), c = at / 8;
+                                part[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                    (lds4 *)(s_v + key * S::PITCH + S::value_piece(key, c) * 16 + at % 8 * 2));
+                            }
+                            typedef short s16x8 __attribute__((ext_vector_type(8)));
+                            const vec<T, 8> a = __builtin_bit_cast(vec<T, 8>, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+                            o[d] = Mfma<T>::mul(a, hi, o[d]);
+                            if constexpr (S::SPLIT) o[d] = Mfma<T>::mul(a, lo, o[d]);
+                        }
+                    }
+            }
+        }
+
+        // the halves' sums, and the waves that share the rows
+        {
+            const auto y = halves(l);
+            l = y[0] + y[1];
+        }
+        if constexpr (WK > 1) {
+            if (g == 0) s_m[wave][r] = m;
+            __syncthreads();   // (and the last tile has been read)
+            float top = m;
+#pragma unroll
+            for (int w = 0; w < WK; ++w) top = fmaxf(top, s_m[wr * WK + w][r]);
+            const float f = rescale(m, top, sc.unit);
+            l *= f;
+            m = top;
+            if (g == 0) s_l[wave][r] = l;
+            float *sums = reinterpret_cast<float *>(s_buf) + (wr * (WK - 1) + wk - 1) * (32 * DP) + lane;
+#pragma unroll
+            for (int e = 0; e < OB; ++e) {
+                o[e] *= f;
+                if (wk > 0)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) sums[(16 * e + k) * 64] = o[e][k];
+            }
+            __syncthreads();
+            if (wk == 0) {
+#pragma unroll
+                for (int w = 1; w < WK; ++w) {
+                    l += s_l[wr * WK + w][r];
+                    const float *from = reinterpret_cast<const float *>(s_buf) + (wr * (WK - 1) + w - 1) * (32 * DP) + lane;
+#pragma unroll
+                    for (int e = 0; e < OB; ++e)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) o[e][k] += from[(16 * e + k) * 64];
+                }
+            }
+        }
+        const bool whole = p.direct || tiles == n || span.y == 0;
+        if (wk == 0 && valid) {
+            const float vs = p.v_scale ? p.v_scale[kv] : 1.0f;
+            const Part part = Part::of(p, 2 * index + (t0 == 0 ? 1 : 0));
+            const int at = wr * 32 + r;
+#pragma unroll
+            for (int e = 0; e < OB; ++e)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int d = 32 * e + 8 * k + 4 * g;
+                    if (d >= p.d) continue;
+                    const f32x4 y = f32x4{o[e][4 * k], o[e][4 * k + 1], o[e][4 * k + 2], o[e][4 * k + 3]} * vs;
+                    if (whole)
+                        write_row<T>(p, t, head, d, y, l);
+                    else
+                        *reinterpret_cast<f32x4 *>(part.o + at * p.d + d) = y;
+                }
+            if (g == 0) {
+                if (whole) {
+                    write_lse(p, t, head, m, sc.unit, l, S::UP);
+                } else {
+                    part.m[at] = m;
+                    part.l[at] = l;
+                }
+            }
+        }
+        if (t0 == 0 && !p.direct)   // parts: this one and the runs' behind
+            cut = make_int4(whole ? 0 : 1 + (int)((tiles - n + run - 1) / run), s, kv, b);
+    }
+    if (tid == 0 && !p.direct) p.cut[index] = cut;
+}
+
+// Joins the parts of a block that a run's end cut: a wave a row, its lanes
+// four outputs each.
+template <class T> __global__ __launch_bounds__(kBlock) void k_join(Params p, float up)
+{
+    const int index = blockIdx.x;
+    const int4 cut = p.cut[index];
+    if (cut.x == 0) return;
+    const int n = cut.x, s = cut.y, kv = cut.z, lane = threadIdx.x & 63;
+    const int at = blockIdx.y * kWaves + (threadIdx.x >> 6);   // row of the block
+    const Seq x = seq_of(p, s);
+    const int32_t row = cut.w * p.rows + at;
+    if (row >= x.n * p.group) return;
+    const int32_t i = divide(row, p.group_mul, p.group_shift), t = x.start + i, head = kv * p.group + row - i * p.group;
+    const Scores sc = Scores::of(p, kv, 0.0f);
+    auto part = [&](int j) { return Part::of(p, j == 0 ? 2 * index + 1 : 2 * (index + j)); };
+    float m = -HUGE_VALF;
+    for (int j = 0; j < n; ++j) m = fmaxf(m, part(j).m[at]);
+    float l = 0.0f;
+    f32x4 o = {0, 0, 0, 0};
+    const int d = 4 * lane;
+    for (int j = 0; j < n; ++j) {
+        const Part y = part(j);
+        const float f = rescale(y.m[at], m, sc.unit);
+        l += y.l[at] * f;
+        if (d < p.d) o += *reinterpret_cast<const f32x4 *>(y.o + (int64_t)at * p.d + d) * f;
+    }
+    if (d < p.d) write_row<T>(p, t, head, d, o, l);
+    if (lane == 0) write_lse(p, t, head, m, sc.unit, l, up);
+}
+
+template <class T, class CT, int DP, int WR> dsim_status launch(Params &p, hipStream_t s)
+{
+    using S = Shape<T, CT, DP, WR>;
+    const auto check = [](const char *what) {
+        const hipError_t e = hipGetLastError();
+        return e == hipSuccess ? DSIM_OK : hip_fail(e, what);
+    };
+    dsim_status st = DSIM_OK;
+    if (!p.direct || p.status) {
+        hipLaunchKernelGGL((k_plan<S::KT>), dim3(1), dim3(kPlan), 0, s, p);
+        if ((st = check("attention plan launch"))) return st;
+    }
+    if (p.direct) {
+        hipLaunchKernelGGL((k_rows<T, CT, DP, WR>), dim3((unsigned)(p.max_blocks * p.n_heads)), dim3(kBlock), 0, s, p);
+        return check("attention launch");
+    }
+    const int grid = kCus * S::PER_CU;
+    hipLaunchKernelGGL((k_rows<T, CT, DP, WR>), dim3(grid), dim3(kBlock), 0, s, p);
+    if ((st = check("attention launch"))) return st;
+    hipLaunchKernelGGL((k_join<T>), dim3(grid, S::M / kWaves), dim3(kBlock), 0, s, p, S::UP);
+    return check("attention join launch");
+}
+
+template <class T, class CT, int DP> dsim_status launch(Params &p, hipStream_t s)
+{
+    if constexpr (!(sizeof(T) == 4 && DP == 256))
+        if (p.rows == 32) return launch<T, CT, DP, 1>(p, s);
+    if (p.rows == 64) return launch<T, CT, DP, 2>(p, s);
+    return launch<T, CT, DP, 4>(p, s);
+}
+
+template <class T, class CT> dsim_status launch(Params &p, hipStream_t s)
+{
+    return p.d <= 64 ? launch<T, CT, 64>(p, s) : p.d <= 128 ? launch<T, CT, 128>(p, s) : launch<T, CT, 256>(p, s);
+}
+
+// by the queries' type, in a translation unit each
+dsim_status launch_f32(Params &p, hipStream_t s);
+dsim_status launch_f16(Params &p, bool e4m3_cache, hipStream_t s);
+dsim_status launch_bf16(Params &p, bool e4m3_cache, hipStream_t s);
+
+}  // namespace rows
+}  // namespace dsim

@@ -1,0 +1,111 @@
+// rows_attention.hip -- dsim_prompt_attention and dsim_tree_attention on the
+// host: their workspace and their launch; the kernels are in
+// rows_attention.h.
+#include "rows_attention.h"
+
+namespace dsim {
+namespace rows {
+
+// Rows of a block: no more than the average sequence has.
+static int rows_of(int64_t n_tok, int32_t n_seq, int32_t group, int32_t head_dim)
+{
+    const int64_t average = n_seq > 0 ? (n_tok * group + n_seq - 1) / n_seq : 0;
+    return average <= 32 && head_dim <= 128 ? 32 : average <= 64 ? 64 : 128;
+}
+
+static int64_t blocks(int64_t n_tok, int32_t n_seq, int32_t group, int rows)
+{
+    return (n_tok * group + rows - 1) / rows + n_seq;
+}
+
+struct Layout {
+    size_t cost, span, first, cut, part, end;
+    Layout(int64_t n_blocks, int32_t n_seq, int rows, int32_t d)
+    {
+        const auto up = [](size_t x) { return (x + 15) / 16 * 16; };
+        cost = 0;
+        span = up(cost + 8 * ((size_t)n_blocks + 1));
+        first = up(span + 8 * (size_t)n_blocks);
+        cut = up(first + 4 * ((size_t)n_seq + 1));
+        part = cut + sizeof(int4) * kMaxGrid;
+        end = part + (size_t)kMaxGrid * 2 * rows * (d + 2) * sizeof(float);
+    }
+};
+
+}  // namespace rows
+
+size_t rows_workspace(int64_t n_tok, int32_t n_seq, int32_t n_q_heads, int32_t n_heads, int32_t head_dim)
+{
+    const int32_t group = n_q_heads / n_heads;
+    const int rows = rows::rows_of(n_tok, n_seq, group, head_dim);
+    return rows::Layout(rows::blocks(n_tok, n_seq, group, rows), n_seq, rows, head_dim).end;
+}
+
+dsim_status launch_rows(const RowsArgs &a, hipStream_t s)
+{
+    using namespace rows;
+    Params p{};
+    p.k = a.c.k;
+    p.v = a.c.v;
+    p.q = a.q.q.data;
+    p.out = a.q.out.data;
+    p.k_scale = a.c.k_scale;
+    p.v_scale = a.c.v_scale;
+    p.slopes = a.q.slopes;
+    p.table = a.c.block_table;
+    p.start = a.q.start;
+    p.len = a.q.len;
+    p.prefix_len = a.prefix_len;
+    p.first_key = a.first_key;
+    p.depth = a.depth;
+    p.mask = a.mask;
+    p.lse = a.q.lse;
+    p.status = a.q.status;
+    p.n_pages = a.c.n_pages;
+    p.page_stride = a.c.page_stride;
+    p.slot_stride = a.c.slot_stride;
+    p.head_stride = a.c.head_stride;
+    p.table_stride = a.c.table_stride;
+    p.q_row = a.q.q.row_stride;
+    p.q_head = a.q.q.head_stride;
+    p.out_row = a.q.out.row_stride;
+    p.out_head = a.q.out.head_stride;
+    p.mask_stride = a.mask_stride;
+    p.mask_words = a.mask_words;
+    p.n_tok = a.q.n_tok;
+    p.scale = a.q.scale;
+    p.cap = a.q.cap;
+    p.n_seq = a.c.n_seq;
+    p.n_heads = a.c.n_heads;
+    p.n_q_heads = a.q.n_q_heads;
+    p.d = a.c.head_dim;
+    p.page_size = a.c.page_size;
+    p.table_width = a.c.table_width;
+    p.window = a.q.window;
+    p.group = a.q.n_q_heads / a.c.n_heads;
+    p.rows = rows_of(p.n_tok, p.n_seq, p.group, p.d);
+    p.max_blocks = blocks(p.n_tok, p.n_seq, p.group, p.rows);
+    p.tree = a.tree;
+    const Layout at(p.max_blocks, p.n_seq, p.rows, p.d);
+    char *ws = static_cast<char *>(a.q.workspace);
+    p.cost = reinterpret_cast<int64_t *>(ws + at.cost);
+    p.span = reinterpret_cast<int2 *>(ws + at.span);
+    p.first = reinterpret_cast<int32_t *>(ws + at.first);
+    p.cut = reinterpret_cast<int4 *>(ws + at.cut);
+    p.part = reinterpret_cast<float *>(ws + at.part);
+    // ceil(2^(31 + l) / n), l = ceil(log2 n): exact for t < 2^31
+    const auto divisor = [](int32_t n, uint32_t &mul, uint32_t &shift) {
+        int l = 0;
+        while ((1 << l) < n) ++l;
+        shift = 31 + l;
+        mul = (uint32_t)((((uint64_t)1 << shift) + n - 1) / n);
+    };
+    divisor(p.page_size, p.page_mul, p.page_shift);
+    divisor(p.group, p.group_mul, p.group_shift);
+    const int64_t most = (int64_t)p.table_width * p.page_size;
+    p.direct = most <= 1024;
+    if (a.q.dtype == DSIM_F32) return rows::launch_f32(p, s);
+    return (a.q.dtype == DSIM_F16 ? rows::launch_f16 : rows::launch_bf16)(p, a.c.dtype == DSIM_E4M3, s);
+}
+
+}  // namespace dsim

@@ -131,3 +131,121 @@ def dsim_logit_adjust(logits, out, history=None, prompt_len=None, history_len=No
     ceil(vocab / 32)), bit t % 32 of word t // 32 set where t is allowed."""
     (_native or lib()).logit_adjust(logits, out, history, prompt_len, history_len, repetition, frequency, presence,
                                     bias_id, bias, mask, stream)
+
+
+# ---------------------------------------------------------------------------
+# A step of several tokens (include/dsim_multi_ops.h)
+# ---------------------------------------------------------------------------
+def dsim_kv_append_axes(cache, block_table, k, v, seq, slot, pos, rope, sections=None, interleaved=False, q=None,
+                        q_out=None, status=None, stream=None):
+    """dsim_kv_append with a token's place in the cache, slot: int32 (tokens,),
+    apart from what it is rotated by, pos: int32 (tokens, axes).  sections: the
+    rotated pairs of each axis, rot_dim / 2 in all (None: one axis); rope and
+    pos None: nothing is rotated."""
+    (_native or lib()).kv_append_axes(cache, block_table, k, v, seq, slot, pos, rope, sections, interleaved, q, q_out,
+                                      status, stream)
+
+
+def dsim_prompt_attention_workspace(n_tokens, n_seq, n_q_heads, n_heads, head_dim):
+    return (_native or lib()).prompt_attention_workspace(n_tokens, n_seq, n_q_heads, n_heads, head_dim)
+
+
+def alloc_prompt_attention_workspace(n_tokens, n_seq, n_q_heads, n_heads, head_dim, device="cuda"):
+    """A caller-owned workspace for dsim_prompt_attention and
+    dsim_tree_attention calls of these sizes (torch uint8)."""
+    import torch
+    return torch.empty(max(dsim_prompt_attention_workspace(n_tokens, n_seq, n_q_heads, n_heads, head_dim), 16),
+                       dtype=torch.uint8, device=device)
+
+
+def _rows_workspace(q, cache, block_table, stream):
+    """A workspace for one call, as _workspace."""
+    import torch
+    if not torch.is_tensor(q) or not torch.is_tensor(block_table):
+        raise ValueError("q and block_table must be torch tensors")
+    if not isinstance(cache, dict) or not torch.is_tensor(cache.get("k")):
+        raise ValueError("cache must be a dict of torch tensors")
+    if q.dim() != 3 or cache["k"].dim() != 4 or block_table.dim() != 2:
+        raise ValueError("q must have shape (tokens, query heads, head_dim), not %s" % (tuple(q.shape),))
+    need = dsim_prompt_attention_workspace(q.shape[0], block_table.shape[0], q.shape[1], cache["k"].shape[2], q.shape[2])
+    if need == 0:
+        raise ValueError("q must have a multiple of the cache's heads, heads of a size that the operator takes, and "
+                         "fewer than 2^31 rows")
+    workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    if stream is not None and q.is_cuda:
+        workspace.record_stream(stream if hasattr(stream, "cuda_stream")
+                                else torch.cuda.ExternalStream(stream, device=q.device))
+    return workspace
+
+
+def dsim_prompt_attention(q, cache, block_table, start, seq_len, out, scale=None, window=0, cap=0.0, slopes=None,
+                          prefix_len=None, first_key=None, workspace=None, lse=None, status=None, stream=None):
+    """q, out: (tokens, query heads, head_dim), out may be q; start: int32
+    (sequences + 1,), tokens start[s] to start[s + 1] - 1 are the last ones of
+    sequence s; seq_len: int32 (sequences,), those included; scale: None for
+    head_dim^-0.5; cap: scores become cap * tanh(score / cap); slopes: fp32
+    (query heads,), of the bias by distance; prefix_len: int32 (sequences,),
+    keys that every token sees; first_key: int32 (tokens,), where the token's
+    document begins; lse: fp32 (tokens, query heads); status: int32
+    (sequences,); workspace: uint8 of at least
+    dsim_prompt_attention_workspace(...) bytes (None: one is allocated with
+    torch for this call)."""
+    if workspace is None:
+        workspace = _rows_workspace(q, cache, block_table, stream)
+    (_native or lib()).prompt_attention(q, cache, block_table, start, seq_len, out, scale, window, cap, slopes, prefix_len,
+                                        first_key, workspace, lse, status, stream)
+
+
+def dsim_tree_attention(q, cache, block_table, start, context_len, tree_mask, out, depth=None, scale=None, window=0,
+                        cap=0.0, slopes=None, workspace=None, lse=None, status=None, stream=None):
+    """As dsim_prompt_attention, for drafted tokens whose keys lie behind a
+    context of context_len: int32 (sequences,) keys.  tree_mask: int32 (tokens,
+    words), bit m % 32 of word m // 32 set where the token attends to node m of
+    its sequence; depth: int32 (tokens,), for windows and slopes."""
+    if workspace is None:
+        workspace = _rows_workspace(q, cache, block_table, stream)
+    (_native or lib()).tree_attention(q, cache, block_table, start, context_len, tree_mask, out, depth, scale, window, cap,
+                                      slopes, workspace, lse, status, stream)
+
+
+def alloc_page_pool(n_pages, n_seq, device="cuda"):
+    """A pool of n_pages pages that n_seq rows of a block table may hold, all
+    of them free: a dict of "refs" (pages,), "free" (bits of the pages that
+    nobody holds, in 32-bit words) and "held" (rows,), int32."""
+    import torch
+    free = torch.full(((n_pages + 31) // 32,), -1, dtype=torch.int32, device=device)
+    if n_pages % 32:
+        free[-1] = (1 << n_pages % 32) - 1
+    return {"refs": torch.zeros(n_pages, dtype=torch.int32, device=device), "free": free,
+            "held": torch.zeros(n_seq, dtype=torch.int32, device=device)}
+
+
+def dsim_kv_reserve(pool, block_table, page_size, seq_len, new_len, status, stream=None):
+    """Pages for new_len: int32 (rows,) places in every row (negative: left
+    alone), of which seq_len are in use; status: int32 (rows,)."""
+    (_native or lib()).kv_reserve(pool, block_table, page_size, seq_len, new_len, status, stream)
+
+
+def dsim_kv_release(pool, block_table, page_size, row, keep_len, status=None, stream=None):
+    """Rows row: int32 (n,) (negative: none) give back what lies behind their
+    first keep_len: int32 (n,) places; status: int32 (n,) or None."""
+    (_native or lib()).kv_release(pool, block_table, page_size, row, keep_len, status, stream)
+
+
+def dsim_kv_fork(layers, pool, block_table, seq_len, src, dst, status, stream=None):
+    """Rows dst: int32 (n,) become second holders of rows src's seq_len places,
+    with copies of pages that end in the middle; layers: a cache or a list of
+    them; seq_len: int32 (rows,), set for dst; status: int32 (n,)."""
+    (_native or lib()).kv_fork(layers, pool, block_table, seq_len, src, dst, status, stream)
+
+
+def dsim_kv_copy_pages(layers, src, dst, stream=None):
+    """Pages dst: int32 (n,) of every layer become what pages src are."""
+    (_native or lib()).kv_copy_pages(layers, src, dst, stream)
+
+
+def dsim_kv_compact(layers, block_table, start, keep, n_keep, status=None, stream=None):
+    """Places start + keep[:, j], j < n_keep, of every sequence move to start +
+    j; start, n_keep: int32 (sequences,); keep: int32 (sequences, width),
+    ascending; status: int32 (sequences,) or None."""
+    (_native or lib()).kv_compact(layers, block_table, start, keep, n_keep, status, stream)
