@@ -22,6 +22,7 @@ constexpr int kExtra = 4;
 constexpr int kMinTiles = 4;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 struct Params {
     const void *k, *v, *q;
@@ -273,8 +274,9 @@ template <bool EXACT> __device__ inline float tanh_of(float y)
         const float a = fabsf(y), z = y * y;
         const float big = 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(2.0f * kLog2e * a) + 1.0f);
         // y - y^3 / 3 + 2 y^5 / 15 - 17 y^7 / 315
-        const float small = a * (1.0f + z * (-0.33333333f + z * (0.13333333f + z * -0.05396825f)));
-        return copysignf(a < 0.2f ? small : big, y);
+        float small = a * (1.0f + z * (-0.33333333f + z * (0.13333333f + z * -0.05396825f)));
+        small = a < 0.2f ? small : big;
+        return copysignf(small, y);
     }
 }
 
@@ -287,7 +289,8 @@ __device__ inline float rescale(float from, float to, float scale)
 // T: type of the queries, CT: of the cache, DP: the head's size padded, WR:
 // blocks of 32 rows in a workgroup.  The four waves are WR x WK: those of a
 // block of rows share out the keys of a tile.
-template <class T, class CT, int DP_, int WR_> struct Shape {
+// WHOLE: pages of a multiple of 16 slots, so that 16 keys lie in one page.
+template <class T, class CT, int DP_, int WR_, bool WHOLE> struct Shape {
     static constexpr int DP = DP_, WR = WR_, WK = kWaves / WR;
     static constexpr bool F32 = sizeof(T) == 4;
     static constexpr int U = !F32 && WR == 4 ? 2 : 1;          // times 32 keys of a tile for each wave
@@ -296,9 +299,17 @@ template <class T, class CT, int DP_, int WR_> struct Shape {
     static constexpr int NC = PITCH / 16;                      // its pieces of 16 bytes
     static constexpr int IN = DP * sizeof(CT) / 16;            // those of a row of the cache
     static constexpr int NQ = KT * IN / kBlock;                // that a thread loads, of keys and of values
+    static constexpr int TILE = KT * PITCH;                    // bytes of a tile's keys or values
+    // Keys and values go to shared memory by themselves, a tile ahead, where
+    // they need no widening and two tiles fit.
+    static constexpr bool DMA = WHOLE && sizeof(CT) == sizeof(T) && 4 * TILE <= 144 * 1024;
     static constexpr int SUMS = 32 * DP * 4 * (WK - 1) * WR;   // outputs of waves that are joined
-    static constexpr int LDS = 2 * KT * PITCH > SUMS ? 2 * KT * PITCH : SUMS;
-    static constexpr int PER_CU = DP <= 128 && LDS <= 76 * 1024 ? 2 : 1;   // workgroups, all resident at once
+    static constexpr int TILES = (DMA ? 4 : 2) * TILE, LDS = TILES > SUMS ? TILES : SUMS;
+    static constexpr int PER_CU = DP <= 128 && LDS <= 78 * 1024 ? 2 : 1;   // workgroups, all resident at once
+    // Rows of a wave's share of a tile, in groups of one page.
+    static constexpr int SHARE = KT / kWaves, GROUP = SHARE < 16 ? SHARE : 16, GROUPS = SHARE / GROUP;
+    static constexpr int RI = 64 / IN > 0 ? 64 / IN : 1;       // rows of the cache that a wave loads at once
+    static constexpr int LOADS = GROUP / RI;                   // loads of a group's keys
     // Offset for the weights' exponents.  fp16 ends at 2^-24: weights up to
     // 2^14 instead of 1 keep all that are above 2^-38 of the largest.
     static constexpr float UP = __is_same(T, f16) ? 14.0f : 0.0f;
@@ -314,6 +325,45 @@ template <class T, class CT, int DP_, int WR_> struct Shape {
         return F32 ? c : c ^ (NC == 8 ? (row >> 1 & 1) << 2 : (row & 3) << 2);
     }
 };
+
+// Shared memory by its 32-bit address.
+using lds_char = __attribute__((address_space(3))) char;
+__device__ inline uint32_t address(const void *p) { return (uint32_t)(uintptr_t)(const lds_char *)p; }
+template <class V> __device__ inline V shared(uint32_t at)
+{
+    return *(const __attribute__((address_space(3))) V *)(uintptr_t)at;
+}
+
+// 16 bytes a lane from global memory to 1,024 bytes of shared memory, not
+// waited for.  (The builtin makes every later read of shared memory wait for
+// it: the compiler does not see that it is to another tile.  No register is
+// written; arrived() stands before the barrier that the readers pass.)
+__device__ inline void to_shared(const void *from, uint32_t off, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :
+                 : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(off), "s"(from)
+                 : "memory", "m0");
+}
+
+// a value that is the same for all lanes, in scalar registers
+__device__ inline int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+template <class P> __device__ inline const P *uniform(const P *p)
+{
+    const uint64_t x = (uint64_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+    return (const P *)((uint64_t)hi << 32 | lo);
+}
+
+// x, as if it might be another from here on: what follows from it is computed
+// again instead of kept in registers
+__device__ inline uint32_t again(uint32_t x)
+{
+    asm("" : "+v"(x));
+    return x;
+}
+
+__device__ inline void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 template <class T> struct Mfma;
 template <> struct Mfma<f16> {
@@ -366,21 +416,21 @@ struct Scores {
     }
 };
 
-template <class T, class CT, int DP, int WR>
-__global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR>::PER_CU)) void k_rows(Params p)
+template <class T, class CT, int DP, int WR, bool WHOLE>
+__global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR, WHOLE>::PER_CU)) void k_rows(Params p)
 {
-    using S = Shape<T, CT, DP, WR>;
+    using S = Shape<T, CT, DP, WR, WHOLE>;
     constexpr int WK = S::WK, U = S::U, KT = S::KT, M = S::M;
     constexpr int OB = DP / 32;   // blocks of 32 outputs
     constexpr int QV = S::F32 ? DP / 8 : DP / 16;
     using Q = typename std::conditional<S::F32, f32x4, vec<T, 8>>::type;
-    __shared__ __attribute__((aligned(16))) char s_buf[S::LDS];
+    __shared__ __attribute__((aligned(1024))) char s_buf[S::LDS];
     __shared__ float s_m[kWaves][32], s_l[kWaves][32];
     __shared__ int32_t s_lo, s_hi;
-    __shared__ uint32_t s_bad[2][KT / 32], s_note[2];
-    char *const s_k = s_buf, *const s_v = s_buf + KT * S::PITCH;
+    __shared__ uint32_t s_bad[2][KT / 32], s_note[2], s_waves[2][kWaves];
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave - wr * WK;
+    const uint32_t buf = address(s_buf);
 
     // this workgroup's run
     int s, kv, b;         // sequence, cache head, block of the sequence
@@ -459,6 +509,9 @@ __global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR>::PER_CU)) void k_rows
             n = max(c1 - kExtra, 0) - t0;
             if (n == 0) continue;   // the next run begins the block
         }
+        t0 = uniform(t0);
+        n = uniform(n);
+        span = make_int2(uniform(span.x), uniform(span.y));
         const int32_t first_tile = span.x / KT;
         if (span.y == 0) n = 0;   // (no keys: the rows are written all the same)
 
@@ -501,16 +554,27 @@ __global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR>::PER_CU)) void k_rows
             }
         }
         __syncthreads();
-        const int32_t all_lo = s_lo, all_hi = s_hi;
+        const int32_t all_lo = uniform(s_lo), all_hi = uniform(s_hi);
+        // Where the lane reads keys, row r of 32 and their piece g, and values,
+        // transposed: elements 4 (lane % 4) on of 16 of rows 4 g + lane / 4 % 4.
+        // (Pieces further on are reached by exclusive or: the tile begins at a
+        // multiple of a row.)
+        // Of the padded elements the last quarter is left out where it holds none.
+        const bool high = p.d > DP * 3 / 4;
+        const uint32_t k_at = buf + (wk * S::KW + r) * S::PITCH + S::key_piece(r, g) * 16;
+        const uint32_t v_row = 4 * g + (lane >> 2 & 3);
+        const uint32_t v_at = buf + S::TILE + (wk * S::KW + v_row) * S::PITCH +
+                              S::value_piece(v_row, 2 * (lane >> 4 & 1) + (lane & 3) / 2) * 16 + (lane & 1) * 8;
 
         const CT *kb = static_cast<const CT *>(p.k) + kv * p.head_stride;
         const CT *vb = static_cast<const CT *>(p.v) + kv * p.head_stride;
         const int32_t *table = p.table + s * p.table_stride;
-        u32x4 kx[S::NQ], vx[S::NQ];
+        const int32_t last = t0 + n;
+        u32x4 kx[S::DMA ? 1 : S::NQ], vx[S::DMA ? 1 : S::NQ];
         uint32_t bad_keys = 0;   // bit q: the page of piece q's key
         auto load = [&](int32_t k0) {
 #pragma unroll
-            for (int j = 0; j < S::NQ; ++j) {
+            for (int j = 0; j < (S::DMA ? 0 : S::NQ); ++j) {
                 const int piece = j * kBlock + tid, c = piece % S::IN;
                 const int32_t key = min(max(k0 + piece / S::IN, span.x), span.y - 1);
                 const int32_t of = divide(key, p.page_mul, p.page_shift), page = table[of];
@@ -527,9 +591,10 @@ __global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR>::PER_CU)) void k_rows
         // pieces of the tile to shared memory; partial: values that are not
         // finite are told of
         auto store = [&](int turn, bool partial) {
+            char *const s_k = s_buf, *const s_v = s_buf + S::TILE;
             bool odd = false;
 #pragma unroll
-            for (int j = 0; j < S::NQ; ++j) {
+            for (int j = 0; j < (S::DMA ? 0 : S::NQ); ++j) {
                 const int piece = j * kBlock + tid, key = piece / S::IN, c = piece % S::IN;
                 if (bad_keys >> j & 1) {
                     atomicOr(&s_bad[turn][key / 32], 1u << key % 32);
@@ -552,36 +617,129 @@ __global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR>::PER_CU)) void k_rows
             }
             if (odd) atomicOr(&s_note[turn], 2u);
         };
+        // The wave's share of a tile straight to shared memory.  The pages of
+        // the next one are asked for a tile ahead.
+        int32_t page[S::GROUPS], slot[S::GROUPS];
+        const uint32_t slot_bytes = (uint32_t)p.slot_stride * (uint32_t)sizeof(CT);
+        const auto group_key = [&](int32_t k0, int j) {   // the first key of a group, or of the nearest attended ones
+            constexpr int32_t whole = ~(S::GROUP - 1);
+            return min(max(k0 + wave * S::SHARE + j * S::GROUP, span.x & whole), (span.y - 1) & whole);
+        };
+        auto fetch = [&](int32_t tile) {
+#pragma unroll
+            for (int j = 0; j < S::GROUPS; ++j) {
+                const int32_t key = group_key((first_tile + min(tile, last - 1)) * KT, j);
+                const int32_t of = divide(key, p.page_mul, p.page_shift);
+                page[j] = table[of];
+                slot[j] = key - of * p.page_size;
+            }
+        };
+        auto send = [&](int32_t k0, int turn) {
+            uint32_t bad = 0;
+#pragma unroll
+            for (int j = 0; j < S::GROUPS; ++j) {
+                const int32_t key = group_key(k0, j), low = max(span.x - key, 0), high = min(span.y - 1 - key, S::GROUP - 1);
+                const int first_row = wave * S::SHARE + j * S::GROUP;
+                const uint32_t k_to = turn * 2 * S::TILE + first_row * S::PITCH, v_to = k_to + S::TILE;
+                const int32_t of = uniform(page[j]);
+                if (of < 0 || of >= p.n_pages) {
+                    bad |= 1u << j;   // (0: rows that do not attend to them must not see what lies there)
+                    for (int c = lane; c < S::GROUP * S::PITCH / 16; c += 64) {
+                        *reinterpret_cast<u32x4 *>(s_buf + k_to + c * 16) = u32x4{0, 0, 0, 0};
+                        *reinterpret_cast<u32x4 *>(s_buf + v_to + c * 16) = u32x4{0, 0, 0, 0};
+                    }
+                    continue;
+                }
+                const int64_t at = of * p.page_stride + slot[j] * p.slot_stride;
+                const CT *const k_from = uniform(kb + at), *const v_from = uniform(vb + at);
+                const uint32_t mine = again(lane), row0 = mine / S::IN, piece = mine % S::IN;
+#pragma unroll
+                for (int c = 0; c < S::LOADS; ++c) {
+                    const int row = c * S::RI + row0;
+                    const uint32_t off = __umul24(min(max(row, low), high), slot_bytes);
+                    const uint32_t kp = S::key_piece(first_row + row, piece), vp = S::value_piece(first_row + row, piece);
+                    if (p.d == DP || kp * (16 / (int)sizeof(CT)) < (uint32_t)p.d) to_shared(k_from, off + kp * 16, buf + k_to + c * 1024);
+                    if (p.d == DP || vp * (16 / (int)sizeof(CT)) < (uint32_t)p.d) to_shared(v_from, off + vp * 16, buf + v_to + c * 1024);
+                }
+            }
+            if (lane == 0) s_waves[turn][wave] = bad;
+        };
 
         float m = -HUGE_VALF, l = x.bad ? __builtin_nanf("") : 0.0f;
         f32x16 o[OB];
 #pragma unroll
         for (int e = 0; e < OB; ++e) o[e] = f32x16(0.0f);
 
-        if (n > 0) load((first_tile + t0) * KT);
-        for (int32_t tile = t0; tile < t0 + n; ++tile) {
+        if (S::DMA && p.d < DP) {   // what the padded rows' ends are multiplied as
+            for (int c = tid; c < S::TILES / 16; c += kBlock) reinterpret_cast<u32x4 *>(s_buf)[c] = u32x4{0, 0, 0, 0};
+            __syncthreads();
+        }
+        if (n > 0) {
+            if constexpr (S::DMA) {
+                fetch(t0);
+                send((first_tile + t0) * KT, t0 & 1);
+                fetch(t0 + 1);
+            } else {
+                load((first_tile + t0) * KT);
+            }
+        }
+#pragma unroll 1
+        for (int32_t tile = t0; tile < last; ++tile) {
             const int turn = tile & 1;
+            const uint32_t now = S::DMA ? turn * 2 * S::TILE : 0;   // the tile's place in s_buf
             const int32_t k0 = (first_tile + tile) * KT;
             const bool partial = !(k0 >= all_lo && k0 + KT <= all_hi);
-            __syncthreads();   // the tile before has been read
-            store(turn, partial);
-            if (tid == 0) s_note[turn ^ 1] = 0;
-            if (tid < KT / 32) s_bad[turn ^ 1][tid] = 0;
-            __syncthreads();
-            if (tile + 1 < t0 + n) load(k0 + KT);
-            const uint32_t note = s_note[turn];
+            uint32_t note;
+            uint32_t bad_of[U];   // bits of the keys without a page
+            if constexpr (S::DMA) {
+                arrived();
+                __syncthreads();   // the tile is there, the one before has been read
+                if (tile + 1 < last) {
+                    send(k0 + KT, turn ^ 1);
+                    fetch(tile + 2);
+                }
+                note = (s_waves[turn][0] | s_waves[turn][1] | s_waves[turn][2] | s_waves[turn][3]) != 0;
+                if (note) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        bad_of[u] = 0;
+                        for (int j = 0; j < 32 / S::GROUP; ++j) {
+                            const int at = (wk * S::KW + 32 * u) / S::GROUP + j;   // group of the tile
+                            if (s_waves[turn][at / S::GROUPS] >> at % S::GROUPS & 1)
+                                bad_of[u] |= (S::GROUP == 16 ? 0xffffu : 0xffu) << j * S::GROUP;
+                        }
+                    }
+                }
+                if (partial) {
+                    bool odd = false;
+                    for (int c = tid; c < S::TILE / 16; c += kBlock)
+                        if (S::value_piece(c / S::NC, c % S::NC) * (16 / (int)sizeof(T)) < p.d)
+                            odd |= !finite<T>(*reinterpret_cast<const u32x4 *>(s_buf + now + S::TILE + c * 16));
+                    if (__syncthreads_or(odd)) note |= 2;
+                }
+            } else {
+                __syncthreads();   // the tile before has been read
+                store(turn, partial);
+                if (tid == 0) s_note[turn ^ 1] = 0;
+                if (tid < KT / 32) s_bad[turn ^ 1][tid] = 0;
+                __syncthreads();
+                if (tile + 1 < last) load(k0 + KT);
+                note = s_note[turn];
+                if (note & 1)
+#pragma unroll
+                    for (int u = 0; u < U; ++u) bad_of[u] = s_bad[turn][(wk * S::KW + 32 * u) / 32];
+            }
 
             // scores of the wave's keys (rows) and rows (columns)
             f32x16 sx[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) sx[u] = f32x16(0.0f);
-#pragma unroll
-            for (int k = 0; k < QV; ++k) {
-                if (k * (S::F32 ? 8 : 16) >= p.d) break;
+            const uint32_t k_now = again(k_at + now);
+            const auto products = [&](int k) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const int key = wk * S::KW + 32 * u + r;
-                    const Q a = *reinterpret_cast<const Q *>(s_k + key * S::PITCH + S::key_piece(key, 2 * k + g) * 16);
+                    // (a block of 32 keys does not change a row's piece)
+                    const Q a = shared<Q>((k_now ^ 32 * k) + 32 * u * S::PITCH);
                     if constexpr (S::F32) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) sx[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], q[k][e], sx[u], 0, 0, 0);
@@ -589,6 +747,12 @@ __global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR>::PER_CU)) void k_rows
                         sx[u] = Mfma<T>::mul(a, q[k], sx[u]);
                     }
                 }
+            };
+#pragma unroll
+            for (int k = 0; k < QV * 3 / 4; ++k) products(k);
+            if (high) {
+#pragma unroll
+                for (int k = QV * 3 / 4; k < QV; ++k) products(k);
             }
             // element i of a lane's: key 8 (i / 4) + 4 g + i % 4 of 32
             uint32_t in32[U];
@@ -596,19 +760,26 @@ __global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR>::PER_CU)) void k_rows
             for (int u = 0; u < U; ++u) {
                 const int32_t kw = k0 + wk * S::KW + 32 * u;
                 if (!sc.raw) {
+                    sx[u] *= sc.in;
+                    if (p.cap > 0.0f) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float y = sx[u][e] * sc.in;
-                        if (p.cap > 0.0f) y = tanh_of<S::F32>(y) * sc.cap;
-                        sx[u][e] = y;
+                        for (int e = 0; e < 16; ++e) sx[u][e] = tanh_of<S::F32>(sx[u][e]) * sc.cap;
                     }
                     if (p.slopes) {
+                        if (p.tree && kw + 32 > x.len) {
+#pragma unroll 1
+                            for (int e = 0; e < 16; ++e) {   // (keys of nodes are where their nodes are)
+                                int32_t at = kw + 8 * (e / 4) + 4 * g + e % 4;
+                                if (at >= x.len)
+                                    at = (int32_t)min((int64_t)x.len + max(p.depth[x.start + min(at - x.len, x.n - 1)], 0), (int64_t)INT32_MAX);
+                                const float y = sc.slope * (float)abs(in.position - at);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            int32_t at = kw + 8 * (e / 4) + 4 * g + e % 4;
-                            if (p.tree && at >= x.len)
-                                at = (int32_t)min((int64_t)x.len + max(p.depth[x.start + min(at - x.len, x.n - 1)], 0), (int64_t)INT32_MAX);
-                            sx[u][e] -= sc.slope * (float)abs(in.position - at);
+                                for (int k = 0; k < 16; ++k) sx[u][k] -= k == e ? y : 0.0f;
+                            }
+                        } else {
+                            const int32_t at = in.position - kw - 4 * g;
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) sx[u][e] -= sc.slope * (float)abs(at - (8 * (e / 4) + e % 4));
                         }
                     }
                 }
@@ -632,7 +803,7 @@ __global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR>::PER_CU)) void k_rows
                         sx[u][e] = mine >> (8 * (e / 4) + e % 4) & 1 ? sx[u][e] : -HUGE_VALF;
                 }
                 if (note & 1) {
-                    if (in32[u] & s_bad[turn][(wk * S::KW + 32 * u) / 32]) {
+                    if (in32[u] & bad_of[u]) {
                         l = __builtin_nanf("");
                         if (valid && p.status) atomicOr(&p.status[s], DSIM_ST_BAD_PAGE);
                     }
@@ -655,11 +826,20 @@ __global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR>::PER_CU)) void k_rows
                 for (int e = 0; e < OB; ++e) o[e] *= f;
                 m = to;
             }
-            const float base = m == -HUGE_VALF ? 0.0f : m;
+            // exp2((x - m) unit + UP): with one instruction where the products
+            // with `unit` are far from where their rounding shows (that of m's
+            // is the same for all weights)
+            float base = m == -HUGE_VALF ? 0.0f : m;
+            if (__builtin_amdgcn_ballot_w64(fabsf(base * sc.unit) > 0x1p20f) != 0) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) sx[u] -= base;
+                base = 0.0f;
+            }
+            const float add = S::UP - base * sc.unit;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sx[u][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sx[u][e] - base, sc.unit, S::UP));
+                for (int e = 0; e < 16; ++e) sx[u][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sx[u][e], sc.unit, add));
                 if (partial) {   // (a scale of 0 times -inf is NaN)
                     const uint32_t mine = in32[u] >> 4 * g;
 #pragma unroll
@@ -693,54 +873,61 @@ __global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR>::PER_CU)) void k_rows
                         for (int e = 0; e < 4; ++e) {
                             const int at = (32 * d + 8 * e + 4 * g) * (int)sizeof(T);
                             const vec<float, 4> v = to_f32<T, 4>(*reinterpret_cast<const vec<T, 4> *>(
-                                s_v + key * S::PITCH + S::value_piece(key, at / 16) * 16 + at % 16));
+                                s_buf + now + S::TILE + key * S::PITCH + S::value_piece(key, at / 16) * 16 + at % 16));
                             if (attended)
 #pragma unroll
                                 for (int c = 0; c < 4; ++c) o[d][4 * e + c] = __builtin_fmaf(w, v[c], o[d][4 * e + c]);
                         }
                 }
             } else if constexpr (S::F32) {
+                const uint32_t v_now = again(buf + now + S::TILE + (wk * S::KW + 4 * g) * S::PITCH + 4 * r);
+                const auto products = [&](int d) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int key = wk * S::KW + 8 * (e / 4) + 4 * g + e % 4;
+                    for (int e = 0; e < 16; ++e)
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(
+                            shared<float>(v_now + (8 * (e / 4) + e % 4) * S::PITCH + 128 * d), sx[0][e], o[d], 0, 0, 0);
+                };
+                constexpr int kLow = (OB * 3 + 3) / 4;
 #pragma unroll
-                    for (int d = 0; d < OB; ++d) {
-                        if (32 * d >= p.d) break;
-                        const float a = *reinterpret_cast<const float *>(s_v + key * S::PITCH + (32 * d + r) * 4);
-                        o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, sx[0][e], o[d], 0, 0, 0);
-                    }
+                for (int d = 0; d < kLow; ++d) products(d);
+                if (high) {
+#pragma unroll
+                    for (int d = kLow; d < OB; ++d) products(d);
                 }
             } else {
-                typedef short s16x4 __attribute__((ext_vector_type(4)));
                 using lds4 = __attribute__((address_space(3))) s16x4;
-                const int sub = lane & 15;
+                vec<T, 8> w[2 * U], w2[2 * U];
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        vec<float, 8> w;
+                        vec<float, 8> y;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) w[e] = sx[u][8 * half + e];
-                        const vec<T, 8> hi = from_f32<T, 8>(w);
-                        vec<T, 8> lo;
-                        if constexpr (S::SPLIT) lo = from_f32<T, 8>(w - to_f32<T, 8>(hi));
-#pragma unroll
-                        for (int d = 0; d < OB; ++d) {
-                            if (32 * d >= p.d) break;
-                            s16x4 part[2];
-#pragma unroll
-                            for (int k = 0; k < 2; ++k) {
-                                const int key = wk * S::KW + 32 * u + 16 * half + 8 * k + 4 * g + sub / 4;
-                                const int at = 32 * d + 16 * (lane >> 4 & 1) + 4 * (sub & 3), c = at / 8;
-                                part[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                    (lds4 *)(s_v + key * S::PITCH + S::value_piece(key, c) * 16 + at % 8 * 2));
-                            }
-                            typedef short s16x8 __attribute__((ext_vector_type(8)));
-                            const vec<T, 8> a = __builtin_bit_cast(vec<T, 8>, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
-                            o[d] = Mfma<T>::mul(a, hi, o[d]);
-                            if constexpr (S::SPLIT) o[d] = Mfma<T>::mul(a, lo, o[d]);
-                        }
+                        for (int e = 0; e < 8; ++e) y[e] = sx[u][8 * half + e];
+                        w[2 * u + half] = from_f32<T, 8>(y);
+                        if constexpr (S::SPLIT) w2[2 * u + half] = from_f32<T, 8>(y - to_f32<T, 8>(w[2 * u + half]));
                     }
+                const uint32_t v_now = again(v_at + now);
+                const auto products = [&](int d) {
+#pragma unroll
+                    for (int k = 0; k < 2 * U; ++k) {
+                        s16x4 part[2];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                (lds4 *)(uintptr_t)((v_now ^ 64 * d) + (16 * k + 8 * j) * S::PITCH));
+                        const vec<T, 8> a = __builtin_bit_cast(vec<T, 8>, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+                        o[d] = Mfma<T>::mul(a, w[k], o[d]);
+                        if constexpr (S::SPLIT) o[d] = Mfma<T>::mul(a, w2[k], o[d]);
+                    }
+                };
+                constexpr int kLow = (OB * 3 + 3) / 4;
+#pragma unroll
+                for (int d = 0; d < kLow; ++d) products(d);
+                if (high) {
+#pragma unroll
+                    for (int d = kLow; d < OB; ++d) products(d);
+                }
             }
         }
 
@@ -842,9 +1029,9 @@ template <class T> __global__ __launch_bounds__(kBlock) void k_join(Params p, fl
     if (lane == 0) write_lse(p, t, head, m, sc.unit, l, up);
 }
 
-template <class T, class CT, int DP, int WR> dsim_status launch(Params &p, hipStream_t s)
+template <class T, class CT, int DP, int WR, bool WHOLE> dsim_status launch(Params &p, hipStream_t s)
 {
-    using S = Shape<T, CT, DP, WR>;
+    using S = Shape<T, CT, DP, WR, WHOLE>;
     const auto check = [](const char *what) {
         const hipError_t e = hipGetLastError();
         return e == hipSuccess ? DSIM_OK : hip_fail(e, what);
@@ -855,19 +1042,26 @@ template <class T, class CT, int DP, int WR> dsim_status launch(Params &p, hipSt
         if ((st = check("attention plan launch"))) return st;
     }
     if (p.direct) {
-        hipLaunchKernelGGL((k_rows<T, CT, DP, WR>), dim3((unsigned)(p.max_blocks * p.n_heads)), dim3(kBlock), 0, s, p);
+        hipLaunchKernelGGL((k_rows<T, CT, DP, WR, WHOLE>), dim3((unsigned)(p.max_blocks * p.n_heads)), dim3(kBlock), 0, s, p);
         return check("attention launch");
     }
     const int grid = kCus * S::PER_CU;
-    hipLaunchKernelGGL((k_rows<T, CT, DP, WR>), dim3(grid), dim3(kBlock), 0, s, p);
+    hipLaunchKernelGGL((k_rows<T, CT, DP, WR, WHOLE>), dim3(grid), dim3(kBlock), 0, s, p);
     if ((st = check("attention launch"))) return st;
     hipLaunchKernelGGL((k_join<T>), dim3(grid, S::M / kWaves), dim3(kBlock), 0, s, p, S::UP);
     return check("attention join launch");
 }
 
+template <class T, class CT, int DP, int WR> dsim_status launch(Params &p, hipStream_t s)
+{
+    // 16 slots of a page at offsets of 24-bit products
+    const bool whole = p.page_size % 16 == 0 && p.slot_stride * (int64_t)sizeof(CT) < 1 << 24;
+    return whole ? launch<T, CT, DP, WR, true>(p, s) : launch<T, CT, DP, WR, false>(p, s);
+}
+
 template <class T, class CT, int DP> dsim_status launch(Params &p, hipStream_t s)
 {
-    if constexpr (!(sizeof(T) == 4 && DP == 256))
+    if constexpr (DP <= 128)
         if (p.rows == 32) return launch<T, CT, DP, 1>(p, s);
     if (p.rows == 64) return launch<T, CT, DP, 2>(p, s);
     return launch<T, CT, DP, 4>(p, s);
