@@ -37,10 +37,10 @@ struct Place {
     int64_t at;
     int32_t status, pos;
     bool skip;
-    int32_t axis[DSIM_MAX_AXES];   // positions of the rotation, where it has its own
+    vec<int32_t, DSIM_MAX_AXES> axis;   // positions of the rotation, where it has its own
 };
 
-template <bool AXES> __device__ inline Place place_of(const AppendArgs &a, const AxesArgs &x, int64_t t)
+template <int AXES> __device__ inline Place place_of(const AppendArgs &a, const AxesArgs &x, int64_t t)
 {
     Place p{0, 0, 0, false, {}};
     const int32_t s = a.seq[t];
@@ -48,9 +48,9 @@ template <bool AXES> __device__ inline Place place_of(const AppendArgs &a, const
     p.skip = s < 0;
     if (p.skip) return p;
     if (s >= a.c.n_seq) p.status |= DSIM_ST_BAD_SEQUENCE;
-    if (p.pos < 0 || (int64_t)p.pos >= (int64_t)a.c.table_width * a.c.page_size || (!AXES && a.rope && p.pos >= a.n_rope))
+    if (p.pos < 0 || (int64_t)p.pos >= (int64_t)a.c.table_width * a.c.page_size || (AXES == 0 && a.rope && p.pos >= a.n_rope))
         p.status |= DSIM_ST_BAD_POSITION;
-    if constexpr (AXES) {
+    if constexpr (AXES > 0) {
 #pragma unroll
         for (int i = 0; i < DSIM_MAX_AXES; ++i) {
             const int32_t at = i < x.n_axes ? x.pos[t * x.n_axes + i] : 0;
@@ -71,52 +71,40 @@ template <bool AXES> __device__ inline Place place_of(const AppendArgs &a, const
 // call's chunks a token: 2^17, a row's: 64)
 __device__ inline uint32_t divide(uint32_t j, uint32_t mul) { return mul ? __umulhi(j, mul) : j; }
 
-// Cosines and sines of pairs e .. e + N - 1, which with positions on several
-// axes need not lie in one row of the table.
-template <bool AXES, int N>
+// Cosines and sines of pairs e .. e + N - 1.  AXES 0: of the token's one row;
+// 1: those of a chunk are of one axis; 2: of any.
+template <int AXES, int N>
 __device__ inline void angles(const AppendArgs &a, const AxesArgs &x, const Place &p, const float *cs, int e,
                               vec<float, N> &c, vec<float, N> &s)
 {
     using V = vec<float, N>;
     const int half = a.rot_dim / 2;
-    if constexpr (AXES) {
-        const auto row = [&](int pair) {
-            int at = p.axis[0];
+    const vec<int32_t, DSIM_MAX_AXES> axis = p.axis;
+    const int end0 = x.end[0], end1 = x.end[1], end2 = x.end[2];
+    const auto row = [=](int pair) {
+        int at = pair >= end0 ? axis[1] : axis[0];
+        at = pair >= end1 ? axis[2] : at;
+        at = pair >= end2 ? axis[3] : at;
+        return a.rope + (int64_t)at * a.rot_dim;
+    };
+    if constexpr (AXES == 2) {
 #pragma unroll
-            for (int i = 1; i < DSIM_MAX_AXES; ++i) at = pair >= x.end[i - 1] ? p.axis[i] : at;
-            return a.rope + (int64_t)at * a.rot_dim;
-        };
-        const float *r = row(e), *last = row(e + N - 1);
-        c = *reinterpret_cast<const V *>(r + e);
-        s = *reinterpret_cast<const V *>(r + half + e);
-        if (r != last) {   // (a section ends inside, or both ends happen to be of different rows)
-#pragma unroll
-            for (int k = 1; k < N; ++k) {
-                const float *at = row(e + k);
-                c[k] = at[e + k];
-                s[k] = at[half + e + k];
-            }
-        } else {
-            // sections between that begin and end inside
-#pragma unroll
-            for (int k = 1; k < N - 1; ++k) {
-                const float *at = row(e + k);
-                if (at != r) {
-                    c[k] = at[e + k];
-                    s[k] = at[half + e + k];
-                }
-            }
+        for (int k = 0; k < N; ++k) {
+            const float *r = row(e + k);
+            c[k] = r[e + k];
+            s[k] = r[half + e + k];
         }
     } else {
-        c = *reinterpret_cast<const V *>(cs + e);
-        s = *reinterpret_cast<const V *>(cs + half + e);
+        const float *r = AXES == 1 ? row(e) : cs;
+        c = *reinterpret_cast<const V *>(r + e);
+        s = *reinterpret_cast<const V *>(r + half + e);
     }
 }
 
 // T: type of the new rows; CT: of the cache; VEC: elements per load.  A
 // thread takes one chunk of VEC elements, or, where pairs (i, i + R/2) are
 // rotated, one chunk of each half.
-template <class T, class CT, int VEC, bool AXES>
+template <class T, class CT, int VEC, int AXES>
 __global__ __launch_bounds__(kMaxBlock) void k_append(AppendArgs a, AxesArgs axes, uint32_t mul_head, uint32_t mul_value)
 {
     using V = vec<float, VEC>;
@@ -188,7 +176,7 @@ __global__ __launch_bounds__(kMaxBlock) void k_append(AppendArgs a, AxesArgs axe
     }
 }
 
-template <class T, class CT, int VEC, bool AXES> void launch(const AppendArgs &a, const AxesArgs &x, hipStream_t s)
+template <class T, class CT, int VEC, int AXES> void launch(const AppendArgs &a, const AxesArgs &x, hipStream_t s)
 {
     // A workgroup takes a token.  Few tokens: a thread for every chunk, up to
     // 512 (bf16, 32 query and 8 cache heads of 128: 256 tokens 4.1 us, with
@@ -211,7 +199,7 @@ template <class T, class CT, int VEC, bool AXES> void launch(const AppendArgs &a
     hipLaunchKernelGGL((k_append<T, CT, VEC, AXES>), grid, dim3(block), 0, s, a, x, mul(n_rot + rest), mul(a.c.head_dim / VEC));
 }
 
-template <class T, class CT, bool AXES> void launch(const AppendArgs &a, const AxesArgs &x, hipStream_t s)
+template <class T, class CT, int AXES> void launch(const AppendArgs &a, const AxesArgs &x, hipStream_t s)
 {
     // chunks of 16 bytes of T; 4 elements where a half of the rotated part
     // is no whole number of 8
@@ -225,7 +213,7 @@ template <class T, class CT, bool AXES> void launch(const AppendArgs &a, const A
     }
 }
 
-template <bool AXES> dsim_status launch_any(const AppendArgs &a, const AxesArgs &x, hipStream_t s)
+template <int AXES> dsim_status launch_any(const AppendArgs &a, const AxesArgs &x, hipStream_t s)
 {
     if (a.dtype == DSIM_F32)
         launch<float, float, AXES>(a, x, s);
@@ -243,8 +231,15 @@ template <bool AXES> dsim_status launch_any(const AppendArgs &a, const AxesArgs 
 
 }  // namespace
 
-dsim_status launch_append(const AppendArgs &a, hipStream_t s) { return launch_any<false>(a, AxesArgs{}, s); }
+dsim_status launch_append(const AppendArgs &a, hipStream_t s) { return launch_any<0>(a, AxesArgs{}, s); }
 
-dsim_status launch_append_axes(const AppendArgs &a, const AxesArgs &x, hipStream_t s) { return launch_any<true>(a, x, s); }
+dsim_status launch_append_axes(const AppendArgs &a, const AxesArgs &x, hipStream_t s)
+{
+    // the pairs of a thread's chunk
+    const int pairs = (a.dtype == DSIM_F32 || a.rot_dim % 16 ? 4 : 8) / (a.interleaved ? 2 : 1);
+    bool whole = true;
+    for (int i = 0; i < x.n_axes; ++i) whole &= x.end[i] % pairs == 0;
+    return whole ? launch_any<1>(a, x, s) : launch_any<2>(a, x, s);
+}
 
 }  // namespace dsim

@@ -13,22 +13,16 @@
 namespace dsim {
 namespace {
 
-constexpr int kBlock = 256;
-constexpr int kRows = 8;   // pieces of 16 bytes that a thread has in flight
+// Pieces of 16 bytes that a thread has in flight.
+constexpr int rows_at_once(int block) { return block > 256 ? 4 : 8; }
 
-__device__ inline int64_t place(const Layers &l, const CompactArgs &a, int32_t s, int64_t at, bool &ok)
-{
-    const int64_t page = a.table[s * a.table_stride + at / l.page_size];
-    ok &= page >= 0 && page < l.n_pages;
-    return page * l.page_stride + at % l.page_size * l.slot_stride;
-}
-
-// blockIdx.x: sequence; y: layer's keys or values; z: head and piece of its rows
-__global__ __launch_bounds__(kBlock) void k_compact(Layers l, CompactArgs a, int pieces, int per_row, bool tells)
+// blockIdx.x: sequence; y: layer's keys or values; z: columns, pieces of 16
+// bytes of a token's rows, `per` of them.  A thread takes one of them of
+// every `ways`-th token.
+template <int BLOCK> __global__ __launch_bounds__(BLOCK) void k_compact(Layers l, CompactArgs a, int per)
 {
     __shared__ int32_t s_n, s_bad;
     const int32_t s = blockIdx.x;
-    const int head = blockIdx.z / pieces, piece = blockIdx.z - head * pieces;
     const int64_t start = a.start[s], room = (int64_t)a.table_width * l.page_size;
     const int32_t *keep = a.keep + s * a.keep_stride;
     const int32_t want = min(max(a.n_keep[s], 0), a.keep_width);
@@ -38,7 +32,7 @@ __global__ __launch_bounds__(kBlock) void k_compact(Layers l, CompactArgs a, int
     }
     __syncthreads();
     // the list ends before the first entry that does not ascend or has no place
-    for (int32_t j = threadIdx.x; j < want; j += kBlock) {
+    for (int32_t j = threadIdx.x; j < want; j += BLOCK) {
         const int32_t k = keep[j];
         if (k < 0 || (j > 0 && k <= keep[j - 1]) || start + k >= room) {
             atomicMin(&s_n, j);
@@ -47,32 +41,64 @@ __global__ __launch_bounds__(kBlock) void k_compact(Layers l, CompactArgs a, int
     }
     __syncthreads();
     const int32_t n = s_n;
-    const int chunk = threadIdx.x % per_row + piece * per_row, way = threadIdx.x / per_row, ways = kBlock / per_row;
-    const bool used = way < ways && chunk < l.chunks;
-    u32x4 *base = static_cast<u32x4 *>(l.p[blockIdx.y]) + head * l.head_stride + chunk;
+    const int ways = BLOCK / per, way = threadIdx.x / per, column = blockIdx.z * per + threadIdx.x - way * per;
+    const int head = column / l.chunks;
+    const bool used = way < ways && head < l.n_heads;
+    u32x4 *base = static_cast<u32x4 *>(l.p[blockIdx.y]) + head * l.head_stride + (column - head * l.chunks);
+    constexpr int kRows = rows_at_once(BLOCK);
     bool ok = true;
-    for (int32_t j0 = 0; j0 < n; j0 += kRows * ways) {
-        u32x4 x[kRows];
-        int64_t to[kRows];
+    int64_t from[kRows], to[kRows];   // of the batch that begins at j0; to < 0: nothing moves
+    const int32_t *table = a.table + s * a.table_stride;
+    auto find = [&](int32_t j0) {
+        // (every load stands without a condition, so that none waits for another)
+        int32_t of[kRows], src[kRows], dst[kRows], src_page[kRows], dst_page[kRows];
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
             const int32_t j = j0 + i * ways + way;
-            to[i] = -1;
-            if (!used || j >= n || keep[j] == j) continue;
-            bool there = true;
-            const int64_t from = place(l, a, s, start + keep[j], there);
-            const int64_t dst = place(l, a, s, start + j, there);
-            ok &= there;
-            if (!there) continue;
-            to[i] = dst;
-            x[i] = base[from];
+            of[i] = keep[j < n ? j : 0];
         }
-        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const int32_t j = j0 + i * ways + way;
+            const bool moves = used && j < n && of[i] != j;
+            to[i] = moves ? 0 : -1;
+            src[i] = (int32_t)start + (moves ? of[i] : 0);
+            dst[i] = (int32_t)start + (moves ? j : 0);
+            src_page[i] = (int32_t)((uint64_t)(uint32_t)src[i] * a.div_mul >> a.div_shift);
+            dst_page[i] = (int32_t)((uint64_t)(uint32_t)dst[i] * a.div_mul >> a.div_shift);
+            src[i] -= src_page[i] * l.page_size;
+            dst[i] -= dst_page[i] * l.page_size;
+            src_page[i] = table[src_page[i]];
+            dst_page[i] = table[dst_page[i]];
+        }
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const bool there = src_page[i] >= 0 && src_page[i] < l.n_pages && dst_page[i] >= 0 && dst_page[i] < l.n_pages;
+            ok &= there || to[i] < 0;
+            from[i] = src_page[i] * l.page_stride + src[i] * l.slot_stride;
+            to[i] = there && to[i] == 0 ? dst_page[i] * l.page_stride + dst[i] * l.slot_stride : -1;
+        }
+    };
+    if (n > 0) find(0);
+    for (int32_t j0 = 0; j0 < n; j0 += kRows * ways) {
+        u32x4 x[kRows];
+        int64_t now[kRows];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            now[i] = to[i];
+            if (now[i] >= 0) x[i] = base[from[i]];
+        }
+        if (j0 + kRows * ways < n) find(j0 + kRows * ways);   // (places of the next, while these are on their way)
+        // All of the batch is read when the first of it is written; what
+        // the next one reads is not written here, so nobody waits for stores.
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) asm volatile("" : "+v"(x[i]));
+        __builtin_amdgcn_s_barrier();
 #pragma unroll
         for (int i = 0; i < kRows; ++i)
-            if (to[i] >= 0) base[to[i]] = x[i];
+            if (now[i] >= 0) base[now[i]] = x[i];
     }
-    if (tells && a.status && blockIdx.y == 0 && blockIdx.z == 0) {
+    if (a.status && blockIdx.y == 0 && blockIdx.z == 0) {
         if (!ok) atomicOr(&s_bad, DSIM_ST_BAD_PAGE);
         __syncthreads();
         if (threadIdx.x == 0) a.status[s] = s_bad | (n < want || start < 0 ? DSIM_ST_BAD_POSITION : 0);
@@ -81,11 +107,27 @@ __global__ __launch_bounds__(kBlock) void k_compact(Layers l, CompactArgs a, int
 
 }  // namespace
 
-dsim_status launch_compact(const Layers &l, const CompactArgs &a, hipStream_t s)
+dsim_status launch_compact(const Layers &l, const CompactArgs &args, hipStream_t s)
 {
-    const int pieces = (l.chunks + 7) / 8, per_row = (l.chunks + pieces - 1) / pieces;
-    hipLaunchKernelGGL(k_compact, dim3(a.n_seq, 2 * l.n, l.n_heads * pieces), dim3(kBlock), 0, s, l, a, pieces, per_row,
-                       a.status != nullptr);
+    CompactArgs a = args;
+    // ceil(2^(31 + k) / n), k = ceil(log2 n): t / n = t * mul >> shift for t < 2^31
+    int k = 0;
+    while ((1 << k) < l.page_size) ++k;
+    a.div_shift = 31 + k;
+    a.div_mul = (uint32_t)((((uint64_t)1 << a.div_shift) + l.page_size - 1) / l.page_size);
+    const int64_t columns = (int64_t)l.n_heads * l.chunks;
+    const int block = a.keep_width > 64 ? 1024 : 256;
+    // as many columns as leave enough ways for the list at once, 128 bytes at least
+    int64_t per = (int64_t)block * rows_at_once(block) / (a.keep_width > 0 ? a.keep_width : 1);
+    per = per < 8 ? 8 : per > block ? block : per;
+    if (per > columns) per = columns;
+    const int64_t parts = (columns + per - 1) / per;
+    per = (columns + parts - 1) / parts;
+    const dim3 grid(a.n_seq, 2 * l.n, (unsigned)parts);
+    if (block == 1024)
+        hipLaunchKernelGGL((k_compact<1024>), grid, dim3(1024), 0, s, l, a, (int)per);
+    else
+        hipLaunchKernelGGL((k_compact<256>), grid, dim3(256), 0, s, l, a, (int)per);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? DSIM_OK : hip_fail(e, "compact launch");
 }

@@ -40,6 +40,7 @@ struct CompactArgs {
     int32_t *status;
     int64_t table_stride, keep_stride;
     int32_t n_seq, table_width, keep_width;
+    uint32_t div_mul, div_shift;   // t / page_size = t * div_mul >> div_shift
 };
 
 // Kernel launchers (each returns DSIM_OK or DSIM_EHIP).

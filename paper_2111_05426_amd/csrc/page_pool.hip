@@ -73,17 +73,23 @@ __device__ inline void deal(const dsim_page_pool &p, int64_t n, Take take, Got g
     scan(mine, s_sum, total);
     const int64_t avail = total;
 
-    int64_t before = 0, dealt = 0;
+    // (what the first kDeal need is kept: it takes three loads in a row)
+    const Need mine_ = tid < n ? take(tid) : Need{0, 0, true};
+    int64_t before = 0, dealt = 0, at_ = 0;
     for (int64_t i0 = 0; i0 < n; i0 += kDeal) {
         const int64_t i = i0 + tid;
-        const Need x = i < n ? take(i) : Need{0, 0, true};
+        const Need x = i0 == 0 ? mine_ : i < n ? take(i) : Need{0, 0, true};
         const int64_t at = before + scan(x.pages, s_sum, total);
+        if (i0 == 0) at_ = at;
         const bool enough = x.pages == 0 || at + x.pages <= avail;
         if (i < n && !x.skip) got(i, x.status | (enough ? 0 : DSIM_ST_NO_PAGE));
-        // (who gets theirs come first: the sum to the last of them is what is dealt)
-        int64_t sum;
-        scan(x.pages > 0 && enough ? x.pages : 0, s_sum, sum);
-        dealt += sum;
+        if (before + total <= avail) {
+            dealt += total;
+        } else {   // who gets theirs come first: the sum to the last of them is what is dealt
+            int64_t sum;
+            scan(x.pages > 0 && enough ? x.pages : 0, s_sum, sum);
+            dealt += sum;
+        }
         before += total;
     }
     for (int64_t r0 = 0; r0 < dealt; r0 += kWindow) {
@@ -107,8 +113,9 @@ __device__ inline void deal(const dsim_page_pool &p, int64_t n, Take take, Got g
         before = 0;
         for (int64_t i0 = 0; i0 < n && before < r1; i0 += kDeal) {
             const int64_t i = i0 + tid;
-            const Need x = i < n ? take(i) : Need{0, 0, true};
-            const int64_t at = before + scan(x.pages, s_sum, total);
+            const Need x = i0 == 0 ? mine_ : i < n ? take(i) : Need{0, 0, true};
+            int64_t at = at_;
+            if (n > kDeal) at = before + scan(x.pages, s_sum, total);
             if (at + x.pages <= avail)
                 for (int64_t r = max(at, r0); r < min(at + x.pages, r1); ++r) put(i, r - at, s_page[r - r0]);
             before += total;
@@ -141,8 +148,8 @@ __global__ __launch_bounds__(kDeal) void k_reserve(dsim_page_pool p, const int32
     deal(p, p.n_seq, take, [&](int64_t s, int32_t st) { status[s] = st; },
          [&](int64_t s, int64_t j, int32_t page) { p.block_table[s * p.table_stride + p.held[s] + j] = page; });
     for (int64_t s = threadIdx.x; s < p.n_seq; s += kDeal) {
-        const Need x = take(s);
-        if (!x.skip && x.pages > 0 && status[s] == 0) p.held[s] += (int32_t)x.pages;
+        const int64_t want = new_len[s], more = pages_of(want, p.page_size) - p.held[s];
+        if (want >= 0 && status[s] == 0 && more > 0) p.held[s] += (int32_t)more;
     }
 }
 
