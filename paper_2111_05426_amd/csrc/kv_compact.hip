@@ -116,7 +116,7 @@ dsim_status launch_compact(const Layers &l, const CompactArgs &args, hipStream_t
     a.div_shift = 31 + k;
     a.div_mul = (uint32_t)((((uint64_t)1 << a.div_shift) + l.page_size - 1) / l.page_size);
     const int64_t columns = (int64_t)l.n_heads * l.chunks;
-    const int block = a.keep_width > 64 ? 1024 : 256;
+    const int block = a.keep_width > 64 ? 512 : 256;
     // as many columns as leave enough ways for the list at once, 128 bytes at least
     int64_t per = (int64_t)block * rows_at_once(block) / (a.keep_width > 0 ? a.keep_width : 1);
     per = per < 8 ? 8 : per > block ? block : per;
@@ -124,8 +124,8 @@ dsim_status launch_compact(const Layers &l, const CompactArgs &args, hipStream_t
     const int64_t parts = (columns + per - 1) / per;
     per = (columns + parts - 1) / parts;
     const dim3 grid(a.n_seq, 2 * l.n, (unsigned)parts);
-    if (block == 1024)
-        hipLaunchKernelGGL((k_compact<1024>), grid, dim3(1024), 0, s, l, a, (int)per);
+    if (block == 512)
+        hipLaunchKernelGGL((k_compact<512>), grid, dim3(512), 0, s, l, a, (int)per);
     else
         hipLaunchKernelGGL((k_compact<256>), grid, dim3(256), 0, s, l, a, (int)per);
     const hipError_t e = hipGetLastError();

@@ -266,9 +266,9 @@ __device__ inline vec<float, 2> halves(float x)   // those of lanes r and 32 + r
 }
 
 // tanh, off by less than 2^-20 of itself (fp32: the library's)
-template <bool EXACT> __device__ inline float tanh_of(float y)
+template <bool F32> __device__ inline float tanh_of(float y)
 {
-    if constexpr (EXACT) {
+    if constexpr (F32) {
         return tanhf(y);
     } else {
         const float a = fabsf(y), z = y * y;
@@ -277,6 +277,24 @@ template <bool EXACT> __device__ inline float tanh_of(float y)
         float small = a * (1.0f + z * (-0.33333333f + z * (0.13333333f + z * -0.05396825f)));
         small = a < 0.2f ? small : big;
         return copysignf(small, y);
+    }
+}
+
+// Scores over the cap become capped ones in base-2 units (cap2).  Where weights
+// are rounded to T's bits before the second product, a cap of at most 128
+// takes tanh as 1 - 2 / (exp(2 y) + 1), off by at most 2^-21 of 1: 2^-14 of a
+// weight.
+template <bool F32, bool EXACT> __device__ inline void cap_of(f32x16 &x, float cap, float cap2)
+{
+    if (!EXACT && cap <= 128.0f) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float y = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[e] * (2.0f * kLog2e)) + 1.0f);
+            x[e] = __builtin_fmaf(y, -2.0f * cap2, cap2);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = tanh_of<F32>(x[e]) * cap2;
     }
 }
 
@@ -311,8 +329,9 @@ template <class T, class CT, int DP_, int WR_, bool WHOLE> struct Shape {
     static constexpr int RI = 64 / IN > 0 ? 64 / IN : 1;       // rows of the cache that a wave loads at once
     static constexpr int LOADS = GROUP / RI;                   // loads of a group's keys
     // Offset for the weights' exponents.  fp16 ends at 2^-24: weights up to
-    // 2^14 instead of 1 keep all that are above 2^-38 of the largest.
-    static constexpr float UP = __is_same(T, f16) ? 14.0f : 0.0f;
+    // 2^15 (2^11 where they are held against the largest) keep all that are
+    // above 2^-35 of the largest.
+    static constexpr float SLACK = __is_same(T, f16) ? 4.0f : 8.0f, UP = __is_same(T, f16) ? 11.0f : 0.0f;
     // Whether weights enter the second product as two numbers of T.
     static constexpr bool SPLIT = !F32 && WR < 4;
 
@@ -361,6 +380,30 @@ __device__ inline uint32_t again(uint32_t x)
 {
     asm("" : "+v"(x));
     return x;
+}
+
+// N operands from shared memory and the products of each, four operands ahead
+// of their products: the compiler on its own reads each right before its
+// product and waits.  `first` has the first four.
+template <int N, class A, class Read, class Mul>
+__device__ inline void in_order(A (&first)[4], Read read, Mul mul)
+{
+    constexpr int kOnly = 0x2 | 0x4;   // vector and scalar arithmetic may move across
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        A next[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i + 4 + k < N) next[k] = read(i + 4 + k);
+        __builtin_amdgcn_sched_barrier(kOnly);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i + k < N) mul(i + k, first[k]);
+        __builtin_amdgcn_sched_barrier(kOnly);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i + 4 + k < N) first[k] = next[k];
+    }
 }
 
 __device__ inline void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
@@ -416,13 +459,14 @@ struct Scores {
     }
 };
 
-template <class T, class CT, int DP, int WR, bool WHOLE>
-__global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR, WHOLE>::PER_CU)) void k_rows(Params p)
+// OB: blocks of 32 elements of a head that are multiplied.
+template <class T, class CT, int DP, int WR, bool WHOLE, int OB>
+__global__ __launch_bounds__(kBlock)
+__attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape<T, CT, DP, WR, WHOLE>::PER_CU)))) void k_rows(Params p)
 {
     using S = Shape<T, CT, DP, WR, WHOLE>;
     constexpr int WK = S::WK, U = S::U, KT = S::KT, M = S::M;
-    constexpr int OB = DP / 32;   // blocks of 32 outputs
-    constexpr int QV = S::F32 ? DP / 8 : DP / 16;
+    constexpr int QV = S::F32 ? OB * 4 : OB * 2;
     using Q = typename std::conditional<S::F32, f32x4, vec<T, 8>>::type;
     __shared__ __attribute__((aligned(1024))) char s_buf[S::LDS];
     __shared__ float s_m[kWaves][32], s_l[kWaves][32];
@@ -559,8 +603,6 @@ __global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR, WHOLE>::PER_CU)) void
         // transposed: elements 4 (lane % 4) on of 16 of rows 4 g + lane / 4 % 4.
         // (Pieces further on are reached by exclusive or: the tile begins at a
         // multiple of a row.)
-        // Of the padded elements the last quarter is left out where it holds none.
-        const bool high = p.d > DP * 3 / 4;
         const uint32_t k_at = buf + (wk * S::KW + r) * S::PITCH + S::key_piece(r, g) * 16;
         const uint32_t v_row = 4 * g + (lane >> 2 & 3);
         const uint32_t v_at = buf + S::TILE + (wk * S::KW + v_row) * S::PITCH +
@@ -665,7 +707,10 @@ __global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR, WHOLE>::PER_CU)) void
             if (lane == 0) s_waves[turn][wave] = bad;
         };
 
-        float m = -HUGE_VALF, l = x.bad ? __builtin_nanf("") : 0.0f;
+        // Weights are held against m, a score that is at most kSlack base-2
+        // units below the row's largest: what is summed is scaled only where
+        // one above `limit` comes.
+        float m = -HUGE_VALF, limit = -HUGE_VALF, l = x.bad ? __builtin_nanf("") : 0.0f;
         f32x16 o[OB];
 #pragma unroll
         for (int e = 0; e < OB; ++e) o[e] = f32x16(0.0f);
@@ -683,176 +728,243 @@ __global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR, WHOLE>::PER_CU)) void
                 load((first_tile + t0) * KT);
             }
         }
-#pragma unroll 1
-        for (int32_t tile = t0; tile < last; ++tile) {
-            const int turn = tile & 1;
-            const uint32_t now = S::DMA ? turn * 2 * S::TILE : 0;   // the tile's place in s_buf
-            const int32_t k0 = (first_tile + tile) * KT;
-            const bool partial = !(k0 >= all_lo && k0 + KT <= all_hi);
-            uint32_t note;
-            uint32_t bad_of[U];   // bits of the keys without a page
-            if constexpr (S::DMA) {
-                arrived();
-                __syncthreads();   // the tile is there, the one before has been read
-                if (tile + 1 < last) {
-                    send(k0 + KT, turn ^ 1);
-                    fetch(tile + 2);
-                }
-                note = (s_waves[turn][0] | s_waves[turn][1] | s_waves[turn][2] | s_waves[turn][3]) != 0;
-                if (note) {
+        // (here, so that no tile waits for them: the wait would be for the next
+        // tile's keys too)
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        bad_of[u] = 0;
-                        for (int j = 0; j < 32 / S::GROUP; ++j) {
-                            const int at = (wk * S::KW + 32 * u) / S::GROUP + j;   // group of the tile
-                            if (s_waves[turn][at / S::GROUPS] >> at % S::GROUPS & 1)
-                                bad_of[u] |= (S::GROUP == 16 ? 0xffffu : 0xffu) << j * S::GROUP;
-                        }
-                    }
-                }
-                if (partial) {
-                    bool odd = false;
-                    for (int c = tid; c < S::TILE / 16; c += kBlock)
-                        if (S::value_piece(c / S::NC, c % S::NC) * (16 / (int)sizeof(T)) < p.d)
-                            odd |= !finite<T>(*reinterpret_cast<const u32x4 *>(s_buf + now + S::TILE + c * 16));
-                    if (__syncthreads_or(odd)) note |= 2;
-                }
-            } else {
-                __syncthreads();   // the tile before has been read
-                store(turn, partial);
-                if (tid == 0) s_note[turn ^ 1] = 0;
-                if (tid < KT / 32) s_bad[turn ^ 1][tid] = 0;
-                __syncthreads();
-                if (tile + 1 < last) load(k0 + KT);
-                note = s_note[turn];
-                if (note & 1)
-#pragma unroll
-                    for (int u = 0; u < U; ++u) bad_of[u] = s_bad[turn][(wk * S::KW + 32 * u) / 32];
-            }
-
-            // scores of the wave's keys (rows) and rows (columns)
-            f32x16 sx[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) sx[u] = f32x16(0.0f);
-            const uint32_t k_now = again(k_at + now);
-            const auto products = [&](int k) {
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    // (a block of 32 keys does not change a row's piece)
-                    const Q a = shared<Q>((k_now ^ 32 * k) + 32 * u * S::PITCH);
-                    if constexpr (S::F32) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) sx[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], q[k][e], sx[u], 0, 0, 0);
-                    } else {
-                        sx[u] = Mfma<T>::mul(a, q[k], sx[u]);
-                    }
-                }
-            };
-#pragma unroll
-            for (int k = 0; k < QV * 3 / 4; ++k) products(k);
-            if (high) {
-#pragma unroll
-                for (int k = QV * 3 / 4; k < QV; ++k) products(k);
-            }
-            // element i of a lane's: key 8 (i / 4) + 4 g + i % 4 of 32
-            uint32_t in32[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int32_t kw = k0 + wk * S::KW + 32 * u;
-                if (!sc.raw) {
-                    sx[u] *= sc.in;
-                    if (p.cap > 0.0f) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) sx[u][e] = tanh_of<S::F32>(sx[u][e]) * sc.cap;
-                    }
-                    if (p.slopes) {
-                        if (p.tree && kw + 32 > x.len) {
-#pragma unroll 1
-                            for (int e = 0; e < 16; ++e) {   // (keys of nodes are where their nodes are)
-                                int32_t at = kw + 8 * (e / 4) + 4 * g + e % 4;
-                                if (at >= x.len)
-                                    at = (int32_t)min((int64_t)x.len + max(p.depth[x.start + min(at - x.len, x.n - 1)], 0), (int64_t)INT32_MAX);
-                                const float y = sc.slope * (float)abs(in.position - at);
-#pragma unroll
-                                for (int k = 0; k < 16; ++k) sx[u][k] -= k == e ? y : 0.0f;
-                            }
-                        } else {
-                            const int32_t at = in.position - kw - 4 * g;
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) sx[u][e] -= sc.slope * (float)abs(at - (8 * (e / 4) + e % 4));
-                        }
-                    }
-                }
-                in32[u] = ~0u;
-                if (partial) {
-                    const int32_t lo = min(max(in.lo - kw, 0), 32), hi = min(max(in.hi - kw, 0), 32);
-                    in32[u] = (uint32_t)((1ull << hi) - 1) & ~(uint32_t)((1ull << lo) - 1);
-                    if (p.tree && kw + 32 > x.len && kw < x.keys) {
-                        // bits of the nodes from the first of these keys on
-                        const int32_t node = kw - x.len, w = max(node, 0) >> 5;
-                        uint64_t bits = mask[w];
-                        if (w + 1 < p.mask_words) bits |= (uint64_t)mask[w + 1] << 32;
-                        uint32_t word = node < 0 ? (uint32_t)(bits << -node) : (uint32_t)(bits >> (node & 31));
-                        const int32_t end = x.keys - kw;   // > 0
-                        if (end < 32) word &= (1u << end) - 1;
-                        in32[u] |= word;
-                    }
-                    const uint32_t mine = in32[u] >> 4 * g;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        sx[u][e] = mine >> (8 * (e / 4) + e % 4) & 1 ? sx[u][e] : -HUGE_VALF;
-                }
-                if (note & 1) {
-                    if (in32[u] & bad_of[u]) {
-                        l = __builtin_nanf("");
-                        if (valid && p.status) atomicOr(&p.status[s], DSIM_ST_BAD_PAGE);
-                    }
-                }
-            }
-            // weights against the running maximum
-            float top = sx[0][0];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) top = fmaxf(top, sx[u][e]);
-            {
-                const auto y = halves(top);
-                top = fmaxf(y[0], y[1]);
-            }
-            if (__builtin_amdgcn_ballot_w64(top > m) != 0) {
-                const float to = fmaxf(m, top), f = rescale(m, to, sc.unit);
-                l *= f;
-#pragma unroll
-                for (int e = 0; e < OB; ++e) o[e] *= f;
-                m = to;
-            }
-            // exp2((x - m) unit + UP): with one instruction where the products
-            // with `unit` are far from where their rounding shows (that of m's
-            // is the same for all weights)
+        for (int k = 0; k < QV; ++k) asm volatile("" : "+v"(q[k]));
+        f32x16 sx[U];
+        uint32_t in32[U], note = 0;
+        float top = -HUGE_VALF;
+        bool fresh = true, partial = false;
+        // Weights of the scores: exp2((x - m) unit + UP), with one instruction
+        // where the products with `unit` are far from where their rounding
+        // shows.
+        const auto weigh = [&]() {
             float base = m == -HUGE_VALF ? 0.0f : m;
-            if (__builtin_amdgcn_ballot_w64(fabsf(base * sc.unit) > 0x1p20f) != 0) {
+            if (__builtin_amdgcn_ballot_w64(fabsf(base * sc.unit) > 0x1p10f) != 0) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) sx[u] -= base;
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sx[u][e] -= base;
                 base = 0.0f;
             }
             const float add = S::UP - base * sc.unit;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
+            for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) sx[u][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sx[u][e], sc.unit, add));
-                if (partial) {   // (a scale of 0 times -inf is NaN)
-                    const uint32_t mine = in32[u] >> 4 * g;
+            if (partial && sc.unit == 0.0f) {   // (0 times -inf is NaN)
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const uint32_t mine = again(in32[u] >> 4 * g);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) sx[u][e] = mine >> (8 * (e / 4) + e % 4) & 1 ? sx[u][e] : 0.0f;
                 }
-#pragma unroll
-                for (int e = 0; e < 16; ++e) l += sx[u][e];
             }
-            // outputs (rows) of the rows (columns)
-            if (partial && (note & 2)) {
+            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum[e % 4] += sx[u][e];
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        };
+
+        // What scales the outputs or adds to them one by one stands outside the
+        // inner loop, which leaves it to them: a tile is begun again behind it.
+        for (int32_t tile = t0;;) {
+#pragma unroll 1
+            for (; tile < last; ++tile, fresh = true) {
+                const int turn = tile & 1;
+                const uint32_t now = S::DMA ? turn * 2 * S::TILE : 0;   // the tile's place in s_buf
+                const int32_t k0 = (first_tile + tile) * KT;
+                partial = !(k0 >= all_lo && k0 + KT <= all_hi);
+                if (fresh) {
+                    if constexpr (S::DMA) {
+                        arrived();
+                        __syncthreads();   // the tile is there, the one before has been read
+                        if (tile + 1 < last) {
+                            send(k0 + KT, turn ^ 1);
+                            fetch(tile + 2);
+                        }
+                        note = (s_waves[turn][0] | s_waves[turn][1] | s_waves[turn][2] | s_waves[turn][3]) != 0;
+                        if (partial) {
+                            bool odd = false;
+                            for (int c = tid; c < S::TILE / 16; c += kBlock)
+                                if (S::value_piece(c / S::NC, c % S::NC) * (16 / (int)sizeof(T)) < p.d)
+                                    odd |= !finite<T>(*reinterpret_cast<const u32x4 *>(s_buf + now + S::TILE + c * 16));
+                            if (__syncthreads_or(odd)) note |= 2;
+                        }
+                    } else {
+                        __syncthreads();   // the tile before has been read
+                        store(turn, partial);
+                        if (tid == 0) s_note[turn ^ 1] = 0;
+                        if (tid < KT / 32) s_bad[turn ^ 1][tid] = 0;
+                        __syncthreads();
+                        if (tile + 1 < last) load(k0 + KT);
+                        note = s_note[turn];
+                    }
+                    note = uniform((int32_t)note);
+                }
+
+                // scores of the wave's keys (rows) and rows (columns)
+#pragma unroll
+                for (int u = 0; u < U; ++u) sx[u] = f32x16(0.0f);
+                const uint32_t k_now = again(k_at + now);
+                {
+                    // (a block of 32 keys does not change a row's piece)
+                    const auto read = [&](int i) { return shared<Q>((k_now ^ 32 * (i / U)) + 32 * (i % U) * S::PITCH); };
+                    Q a[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) a[i] = read(i);
+                    in_order<QV * U>(a, read, [&](int i, const Q &x) {
+                        if constexpr (S::F32) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) sx[i % U] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], q[i / U][e], sx[i % U], 0, 0, 0);
+                        } else {
+                            sx[i % U] = Mfma<T>::mul(x, q[i / U], sx[i % U]);
+                        }
+                    });
+                }
+                // element i of a lane's: key 8 (i / 4) + 4 g + i % 4 of 32
+                if (!sc.raw) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const int32_t kw = k0 + wk * S::KW + 32 * u;
+                        sx[u] *= sc.in;
+                        if (p.cap > 0.0f) cap_of<S::F32, S::F32 || S::SPLIT>(sx[u], p.cap, sc.cap);
+                        if (p.slopes) {
+                            if (p.tree && kw + 32 > x.len) {
+#pragma unroll 1
+                                for (int e = 0; e < 16; ++e) {   // (keys of nodes are where their nodes are)
+                                    int32_t at = kw + 8 * (e / 4) + 4 * g + e % 4;
+                                    if (at >= x.len)
+                                        at = (int32_t)min((int64_t)x.len + max(p.depth[x.start + min(at - x.len, x.n - 1)], 0), (int64_t)INT32_MAX);
+                                    const float y = sc.slope * (float)abs(in.position - at);
+#pragma unroll
+                                    for (int k = 0; k < 16; ++k) sx[u][k] -= k == e ? y : 0.0f;
+                                }
+                            } else {
+                                const int32_t at = (int32_t)again(in.position - kw - 4 * g);
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) sx[u][e] -= sc.slope * (float)abs(at - (8 * (e / 4) + e % 4));
+                            }
+                        }
+                    }
+                }
+                if (partial) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const int32_t kw = k0 + wk * S::KW + 32 * u;
+                        const int32_t lo = min(max(in.lo - kw, 0), 32), hi = min(max(in.hi - kw, 0), 32);
+                        in32[u] = (uint32_t)((1ull << hi) - 1) & ~(uint32_t)((1ull << lo) - 1);
+                        if (p.tree && kw + 32 > x.len && kw < x.keys) {
+                            // bits of the nodes from the first of these keys on
+                            const int32_t node = kw - x.len, w = max(node, 0) >> 5;
+                            uint64_t bits = mask[w];
+                            if (w + 1 < p.mask_words) bits |= (uint64_t)mask[w + 1] << 32;
+                            uint32_t word = node < 0 ? (uint32_t)(bits << -node) : (uint32_t)(bits >> (node & 31));
+                            const int32_t end = x.keys - kw;   // > 0
+                            if (end < 32) word &= (1u << end) - 1;
+                            in32[u] |= word;
+                        }
+                        const uint32_t mine = again(in32[u] >> 4 * g);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            sx[u][e] = mine >> (8 * (e / 4) + e % 4) & 1 ? sx[u][e] : -HUGE_VALF;
+                    }
+                }
+                if (note & 1) {
+#pragma unroll 1
+                    for (int u = 0; u < U; ++u) {
+                        uint32_t bad = 0;   // bits of the keys without a page
+                        if constexpr (S::DMA) {
+                            for (int j = 0; j < 32 / S::GROUP; ++j) {
+                                const int at = (wk * S::KW + 32 * u) / S::GROUP + j;   // group of the tile
+                                if (s_waves[turn][at / S::GROUPS] >> at % S::GROUPS & 1)
+                                    bad |= (S::GROUP == 16 ? 0xffffu : 0xffu) << j * S::GROUP;
+                            }
+                        } else {
+                            bad = s_bad[turn][(wk * S::KW + 32 * u) / 32];
+                        }
+                        if ((partial ? u ? in32[U - 1] : in32[0] : ~0u) & bad) {
+                            l = __builtin_nanf("");
+                            if (valid && p.status) atomicOr(&p.status[s], DSIM_ST_BAD_PAGE);
+                        }
+                    }
+                }
+                top = sx[0][0];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) top = fmaxf(top, sx[u][e]);
+                {
+                    const auto y = halves(top);
+                    top = fmaxf(y[0], y[1]);
+                }
+                // (once a tile: whatever the scores, every loop ends)
+                if ((fresh && __builtin_amdgcn_ballot_w64(top > limit) != 0) || (note & 2)) break;
+                // outputs (rows) of the rows (columns); the first values come
+                // while the weights are computed
+                if constexpr (S::F32) {
+                    const uint32_t v_now = again(buf + now + S::TILE + (wk * S::KW + 4 * g) * S::PITCH + 4 * r);
+                    const auto read = [&](int i) {
+                        const int e = i / OB, d = i % OB;
+                        return shared<float>(v_now + (8 * (e / 4) + e % 4) * S::PITCH + 128 * d);
+                    };
+                    float a[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) a[i] = read(i);
+                    weigh();
+                    in_order<16 * OB>(a, read, [&](int i, float x) {
+                        o[i % OB] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, sx[0][i / OB], o[i % OB], 0, 0, 0);
+                    });
+                } else {
+                    using lds4 = __attribute__((address_space(3))) s16x4;
+                    const uint32_t v_now = again(v_at + now);
+                    const auto read = [&](int i) {
+                        const int k = i / OB, d = i % OB;
+                        s16x4 part[2];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                (lds4 *)(uintptr_t)((v_now ^ 64 * d) + (16 * k + 8 * j) * S::PITCH));
+                        return __builtin_bit_cast(vec<T, 8>, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+                    };
+                    vec<T, 8> a[4], w[2 * U], w2[2 * U];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) a[i] = read(i);
+                    weigh();
+#pragma unroll
+                    for (int k = 0; k < 2 * U; ++k) {
+                        vec<float, 8> y;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) y[e] = sx[k / 2][8 * (k % 2) + e];
+                        w[k] = from_f32<T, 8>(y);
+                        if constexpr (S::SPLIT) w2[k] = from_f32<T, 8>(y - to_f32<T, 8>(w[k]));
+                    }
+                    in_order<2 * U * OB>(a, read, [&](int i, const vec<T, 8> &x) {
+                        o[i % OB] = Mfma<T>::mul(x, w[i / OB], o[i % OB]);
+                        if constexpr (S::SPLIT) o[i % OB] = Mfma<T>::mul(x, w2[i / OB], o[i % OB]);
+                    });
+                }
+            }
+            if (tile >= last) break;
+
+            {
+                const float to = top > limit ? top : m, f = rescale(m, to, sc.unit);
+                l *= f;
+#pragma unroll
+                for (int e = 0; e < OB; ++e) o[e] *= f;
+                m = to;
+                limit = m == -HUGE_VALF ? m : m + S::SLACK / sc.unit;
+            }
+            fresh = false;
+            if (note & 2) {
                 // Values that are not finite, and rows that do not attend to
                 // them: a weight of 0 would make them NaN, so each product
                 // stands alone.
+                const char *const from = s_buf + (S::DMA ? (tile & 1) * 2 * S::TILE : 0) + S::TILE;
+                weigh();
 #pragma unroll 1
                 for (int k = 0; k < 32 * U; ++k) {
                     float mine = 0.0f;   // the weight, in a lane of the key's half
@@ -873,61 +985,16 @@ __global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR, WHOLE>::PER_CU)) void
                         for (int e = 0; e < 4; ++e) {
                             const int at = (32 * d + 8 * e + 4 * g) * (int)sizeof(T);
                             const vec<float, 4> v = to_f32<T, 4>(*reinterpret_cast<const vec<T, 4> *>(
-                                s_buf + now + S::TILE + key * S::PITCH + S::value_piece(key, at / 16) * 16 + at % 16));
-                            if (attended)
+                                from + key * S::PITCH + S::value_piece(key, at / 16) * 16 + at % 16));
 #pragma unroll
-                                for (int c = 0; c < 4; ++c) o[d][4 * e + c] = __builtin_fmaf(w, v[c], o[d][4 * e + c]);
+                            for (int c = 0; c < 4; ++c) {
+                                const float y = __builtin_fmaf(w, v[c], o[d][4 * e + c]);
+                                o[d][4 * e + c] = attended ? y : o[d][4 * e + c];
+                            }
                         }
                 }
-            } else if constexpr (S::F32) {
-                const uint32_t v_now = again(buf + now + S::TILE + (wk * S::KW + 4 * g) * S::PITCH + 4 * r);
-                const auto products = [&](int d) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(
-                            shared<float>(v_now + (8 * (e / 4) + e % 4) * S::PITCH + 128 * d), sx[0][e], o[d], 0, 0, 0);
-                };
-                constexpr int kLow = (OB * 3 + 3) / 4;
-#pragma unroll
-                for (int d = 0; d < kLow; ++d) products(d);
-                if (high) {
-#pragma unroll
-                    for (int d = kLow; d < OB; ++d) products(d);
-                }
-            } else {
-                using lds4 = __attribute__((address_space(3))) s16x4;
-                vec<T, 8> w[2 * U], w2[2 * U];
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        vec<float, 8> y;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) y[e] = sx[u][8 * half + e];
-                        w[2 * u + half] = from_f32<T, 8>(y);
-                        if constexpr (S::SPLIT) w2[2 * u + half] = from_f32<T, 8>(y - to_f32<T, 8>(w[2 * u + half]));
-                    }
-                const uint32_t v_now = again(v_at + now);
-                const auto products = [&](int d) {
-#pragma unroll
-                    for (int k = 0; k < 2 * U; ++k) {
-                        s16x4 part[2];
-#pragma unroll
-                        for (int j = 0; j < 2; ++j)
-                            part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                (lds4 *)(uintptr_t)((v_now ^ 64 * d) + (16 * k + 8 * j) * S::PITCH));
-                        const vec<T, 8> a = __builtin_bit_cast(vec<T, 8>, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
-                        o[d] = Mfma<T>::mul(a, w[k], o[d]);
-                        if constexpr (S::SPLIT) o[d] = Mfma<T>::mul(a, w2[k], o[d]);
-                    }
-                };
-                constexpr int kLow = (OB * 3 + 3) / 4;
-#pragma unroll
-                for (int d = 0; d < kLow; ++d) products(d);
-                if (high) {
-#pragma unroll
-                    for (int d = kLow; d < OB; ++d) products(d);
-                }
+                ++tile;
+                fresh = true;
             }
         }
 
@@ -946,7 +1013,7 @@ __global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR, WHOLE>::PER_CU)) void
             l *= f;
             m = top;
             if (g == 0) s_l[wave][r] = l;
-            float *sums = reinterpret_cast<float *>(s_buf) + (wr * (WK - 1) + wk - 1) * (32 * DP) + lane;
+            float *sums = reinterpret_cast<float *>(s_buf) + (wr * (WK - 1) + wk - 1) * (1024 * OB) + lane;
 #pragma unroll
             for (int e = 0; e < OB; ++e) {
                 o[e] *= f;
@@ -959,7 +1026,7 @@ __global__ __launch_bounds__(kBlock, (Shape<T, CT, DP, WR, WHOLE>::PER_CU)) void
 #pragma unroll
                 for (int w = 1; w < WK; ++w) {
                     l += s_l[wr * WK + w][r];
-                    const float *from = reinterpret_cast<const float *>(s_buf) + (wr * (WK - 1) + w - 1) * (32 * DP) + lane;
+                    const float *from = reinterpret_cast<const float *>(s_buf) + (wr * (WK - 1) + w - 1) * (1024 * OB) + lane;
 #pragma unroll
                     for (int e = 0; e < OB; ++e)
 #pragma unroll
@@ -1029,7 +1096,7 @@ template <class T> __global__ __launch_bounds__(kBlock) void k_join(Params p, fl
     if (lane == 0) write_lse(p, t, head, m, sc.unit, l, up);
 }
 
-template <class T, class CT, int DP, int WR, bool WHOLE> dsim_status launch(Params &p, hipStream_t s)
+template <class T, class CT, int DP, int WR, bool WHOLE, int OB> dsim_status launch(Params &p, hipStream_t s)
 {
     using S = Shape<T, CT, DP, WR, WHOLE>;
     const auto check = [](const char *what) {
@@ -1041,13 +1108,9 @@ template <class T, class CT, int DP, int WR, bool WHOLE> dsim_status launch(Para
         hipLaunchKernelGGL((k_plan<S::KT>), dim3(1), dim3(kPlan), 0, s, p);
         if ((st = check("attention plan launch"))) return st;
     }
-    if (p.direct) {
-        hipLaunchKernelGGL((k_rows<T, CT, DP, WR, WHOLE>), dim3((unsigned)(p.max_blocks * p.n_heads)), dim3(kBlock), 0, s, p);
-        return check("attention launch");
-    }
-    const int grid = kCus * S::PER_CU;
-    hipLaunchKernelGGL((k_rows<T, CT, DP, WR, WHOLE>), dim3(grid), dim3(kBlock), 0, s, p);
-    if ((st = check("attention launch"))) return st;
+    const int grid = p.direct ? (int)(p.max_blocks * p.n_heads) : kCus * S::PER_CU;
+    hipLaunchKernelGGL((k_rows<T, CT, DP, WR, WHOLE, OB>), dim3(grid), dim3(kBlock), 0, s, p);
+    if ((st = check("attention launch")) || p.direct) return st;
     hipLaunchKernelGGL((k_join<T>), dim3(grid, S::M / kWaves), dim3(kBlock), 0, s, p, S::UP);
     return check("attention join launch");
 }
@@ -1056,7 +1119,10 @@ template <class T, class CT, int DP, int WR> dsim_status launch(Params &p, hipSt
 {
     // 16 slots of a page at offsets of 24-bit products
     const bool whole = p.page_size % 16 == 0 && p.slot_stride * (int64_t)sizeof(CT) < 1 << 24;
-    return whole ? launch<T, CT, DP, WR, true>(p, s) : launch<T, CT, DP, WR, false>(p, s);
+    if (!whole) return launch<T, CT, DP, WR, false, DP / 32>(p, s);
+    if constexpr (DP > 64)
+        if (p.d <= DP * 3 / 4) return launch<T, CT, DP, WR, true, DP / 32 * 3 / 4>(p, s);
+    return launch<T, CT, DP, WR, true, DP / 32>(p, s);
 }
 
 template <class T, class CT, int DP> dsim_status launch(Params &p, hipStream_t s)
