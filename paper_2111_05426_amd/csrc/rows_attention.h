@@ -117,14 +117,15 @@ __device__ inline Range range_of(const Params &p, const Seq &x, int s, int32_t i
                     p.depth ? p.depth[t] : 0);
 }
 
-// The keys that some token of tokens i0 to i1 attends to lie in [x, y).
-__device__ inline int2 span_of(const Params &p, const Seq &x, int s, int32_t i0, int32_t i1)
+// The keys that some token of tokens i0 to i1 attends to lie in [x, y); with
+// first keys, of every `lanes`-th of them.
+__device__ inline int2 span_of(const Params &p, const Seq &x, int s, int32_t i0, int32_t i1, int lane, int lanes)
 {
     if (x.bad) return make_int2(0, 0);
     if (p.tree) return make_int2(p.window > 0 ? min(max(x.len - p.window + 1, 0), x.len) : 0, x.keys);
     int lo = INT32_MAX, hi = 0;
     if (p.first_key) {
-        for (int32_t i = i0; i <= i1; ++i) {
+        for (int32_t i = i0 + lane; i <= i1; i += lanes) {
             const Range r = range_of(p, x, s, i);
             if (r.lo >= r.hi) continue;
             lo = min(lo, r.lo);
@@ -181,7 +182,19 @@ template <class A> __device__ inline int32_t find(A a, int32_t n, int64_t x)
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
+// The sequence of a block: the last that begins at it or before.
+__device__ inline int sequence_of(const Params &p, int32_t b)
+{
+    int lo = 0, hi = p.n_seq;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        (p.first[mid] <= b ? lo : hi) = mid;
+    }
+    return lo;
+}
+
 // Blocks of rows, their keys and what they cost, and the sequences' status.
+constexpr int kLanes = 16;
 template <int KT> __global__ __launch_bounds__(kPlan) void k_plan(Params p)
 {
     __shared__ int64_t s_sum[kPlan / 64];
@@ -206,22 +219,30 @@ template <int KT> __global__ __launch_bounds__(kPlan) void k_plan(Params p)
     const int32_t n = (int32_t)min(before, p.max_blocks);
     if (threadIdx.x == 0) p.first[p.n_seq] = n;
     __syncthreads();
+    // The blocks' keys, by several lanes where each token has its own.
+    const int lanes = p.first_key ? kLanes : 1;
+    for (int32_t at = threadIdx.x; at < n * lanes; at += kPlan) {
+        const int32_t b = at / lanes;
+        const int s = sequence_of(p, b);
+        const Seq x = seq_of(p, s);
+        const int32_t r0 = (b - p.first[s]) * p.rows, r1 = min(r0 + p.rows, x.n * p.group);
+        int2 span = span_of(p, x, s, r0 / p.group, (r1 - 1) / p.group, at % lanes, lanes);
+        if (lanes > 1) {
+            if (span.y == 0) span.x = INT32_MAX;
+#pragma unroll
+            for (int o = 1; o < kLanes; o <<= 1) {
+                span.x = min(span.x, __shfl_xor(span.x, o));
+                span.y = max(span.y, __shfl_xor(span.y, o));
+            }
+            if (span.y == 0) span.x = 0;
+        }
+        if (at % lanes == 0) p.span[b] = span;
+    }
+    __syncthreads();
     before = 0;
     for (int32_t b0 = 0; b0 < n; b0 += kPlan) {
         const int32_t b = b0 + threadIdx.x;
-        int64_t cost = 0;
-        if (b < n) {
-            int lo = 0, hi = p.n_seq;   // the last sequence that begins at b or before
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) / 2;
-                (p.first[mid] <= b ? lo : hi) = mid;
-            }
-            const Seq x = seq_of(p, lo);
-            const int32_t r0 = (b - p.first[lo]) * p.rows, r1 = min(r0 + p.rows, x.n * p.group);
-            const int2 span = span_of(p, x, lo, r0 / p.group, (r1 - 1) / p.group);
-            p.span[b] = span;
-            cost = tiles_of<KT>(span) + kExtra;
-        }
+        const int64_t cost = b < n ? tiles_of<KT>(p.span[b]) + kExtra : 0;
         const int64_t at = before + scan<kPlan>(cost, s_sum, total);
         if (b < n) p.cost[b] = at;
         before += total;
@@ -534,7 +555,16 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
             left = 0;
             x = seq_of(p, s);
             const int32_t r0 = b * M, r1 = min(r0 + M, x.n * p.group);
-            span = span_of(p, x, s, r0 / p.group, (r1 - 1) / p.group);
+            span = span_of(p, x, s, r0 / p.group, (r1 - 1) / p.group, lane, 64);
+            if (p.first_key) {
+                if (span.y == 0) span.x = INT32_MAX;
+#pragma unroll
+                for (int o = 1; o < 64; o <<= 1) {
+                    span.x = min(span.x, __shfl_xor(span.x, o));
+                    span.y = max(span.y, __shfl_xor(span.y, o));
+                }
+                if (span.y == 0) span.x = 0;
+            }
             n = tiles = tiles_of<KT>(span);
         } else {
             while (b >= p.first[s + 1] - p.first[s]) {   // the next head, or sequence
@@ -1066,34 +1096,55 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
     if (tid == 0 && !p.direct) p.cut[index] = cut;
 }
 
-// Joins the parts of a block that a run's end cut: a wave a row, its lanes
-// four outputs each.
+// Joins the parts of a block that a run's end cut, kJoinRows rows a
+// workgroup: the rows' maxima and sums first, then four outputs a thread.
+constexpr int kJoinRows = 32;
 template <class T> __global__ __launch_bounds__(kBlock) void k_join(Params p, float up)
 {
-    const int index = blockIdx.x;
+    constexpr int kWays = kBlock / kJoinRows;
+    __shared__ float s_m[kWays][kJoinRows], s_l[kWays][kJoinRows];
+    const int index = blockIdx.x, tid = threadIdx.x;
     const int4 cut = p.cut[index];
-    if (cut.x == 0) return;
-    const int n = cut.x, s = cut.y, kv = cut.z, lane = threadIdx.x & 63;
-    const int at = blockIdx.y * kWaves + (threadIdx.x >> 6);   // row of the block
-    const Seq x = seq_of(p, s);
-    const int32_t row = cut.w * p.rows + at;
-    if (row >= x.n * p.group) return;
-    const int32_t i = divide(row, p.group_mul, p.group_shift), t = x.start + i, head = kv * p.group + row - i * p.group;
+    const int n = cut.x, s = cut.y, kv = cut.z, first = blockIdx.y * kJoinRows;
+    if (n == 0) return;
+    const int32_t start = p.start[s], total_rows = (p.start[s + 1] - start) * p.group;
     const Scores sc = Scores::of(p, kv, 0.0f);
     auto part = [&](int j) { return Part::of(p, j == 0 ? 2 * index + 1 : 2 * (index + j)); };
-    float m = -HUGE_VALF;
-    for (int j = 0; j < n; ++j) m = fmaxf(m, part(j).m[at]);
-    float l = 0.0f;
-    f32x4 o = {0, 0, 0, 0};
-    const int d = 4 * lane;
-    for (int j = 0; j < n; ++j) {
-        const Part y = part(j);
-        const float f = rescale(y.m[at], m, sc.unit);
-        l += y.l[at] * f;
-        if (d < p.d) o += *reinterpret_cast<const f32x4 *>(y.o + (int64_t)at * p.d + d) * f;
+    {
+        const int at = tid % kJoinRows, way = tid / kJoinRows;
+        float m = -HUGE_VALF, l = 0.0f;
+        for (int j = way; j < n; j += kWays) m = fmaxf(m, part(j).m[first + at]);
+        s_m[way][at] = m;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWays; ++w) m = fmaxf(m, s_m[w][at]);
+        for (int j = way; j < n; j += kWays) l += part(j).l[first + at] * rescale(part(j).m[first + at], m, sc.unit);
+        s_l[way][at] = l;
+        __syncthreads();
+        if (way == 0) {
+            s_m[0][at] = m;
+#pragma unroll
+            for (int w = 1; w < kWays; ++w) l += s_l[w][at];
+            s_l[0][at] = l;
+            const int32_t row = cut.w * p.rows + first + at, i = divide(row, p.group_mul, p.group_shift);
+            if (row < total_rows) write_lse(p, start + i, kv * p.group + row - i * p.group, m, sc.unit, l, up);
+        }
+        __syncthreads();
     }
-    if (d < p.d) write_row<T>(p, t, head, d, o, l);
-    if (lane == 0) write_lse(p, t, head, m, sc.unit, l, up);
+    const int quads = p.d / 4;
+    for (int e = tid; e < kJoinRows * quads; e += kBlock) {
+        const int at = e / quads, d = 4 * (e - at * quads);
+        const int32_t row = cut.w * p.rows + first + at, i = divide(row, p.group_mul, p.group_shift);
+        if (row >= total_rows) break;
+        const float m = s_m[0][at];
+        f32x4 o = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) {
+            const Part y = part(j);
+            o += *reinterpret_cast<const f32x4 *>(y.o + (int64_t)(first + at) * p.d + d) * rescale(y.m[first + at], m, sc.unit);
+        }
+        write_row<T>(p, start + i, kv * p.group + row - i * p.group, d, o, s_l[0][at]);
+    }
 }
 
 template <class T, class CT, int DP, int WR, bool WHOLE, int OB> dsim_status launch(Params &p, hipStream_t s)
@@ -1111,7 +1162,7 @@ template <class T, class CT, int DP, int WR, bool WHOLE, int OB> dsim_status lau
     const int grid = p.direct ? (int)(p.max_blocks * p.n_heads) : kCus * S::PER_CU;
     hipLaunchKernelGGL((k_rows<T, CT, DP, WR, WHOLE, OB>), dim3(grid), dim3(kBlock), 0, s, p);
     if ((st = check("attention launch")) || p.direct) return st;
-    hipLaunchKernelGGL((k_join<T>), dim3(grid, S::M / kWaves), dim3(kBlock), 0, s, p, S::UP);
+    hipLaunchKernelGGL((k_join<T>), dim3(grid, S::M / kJoinRows), dim3(kBlock), 0, s, p, S::UP);
     return check("attention join launch");
 }
 
