@@ -386,6 +386,23 @@ __device__ inline void to_shared(const void *from, uint32_t off, uint32_t to)
                  : "memory", "m0");
 }
 
+// The kernel's argument, read where it is needed: what few tiles need does not
+// take scalar registers from the others.
+template <class P> __device__ inline const P &argument()
+{
+    auto at = __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    return *(const P *)at;
+}
+
+// x, which is the same for all lanes, kept in scalar registers from here on (not
+// read again from the kernel's argument)
+template <class V> __device__ inline V kept(V x)
+{
+    asm volatile("" : "+s"(x));
+    return x;
+}
+
 // a value that is the same for all lanes, in scalar registers
 __device__ inline int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 template <class P> __device__ inline const P *uniform(const P *p)
@@ -405,9 +422,10 @@ __device__ inline uint32_t again(uint32_t x)
 
 // N operands from shared memory and the products of each, four operands ahead
 // of their products: the compiler on its own reads each right before its
-// product and waits.  `first` has the first four.
-template <int N, class A, class Read, class Mul>
-__device__ inline void in_order(A (&first)[4], Read read, Mul mul)
+// product and waits.  `first` has the first four; other(i) comes before the
+// products of i to i + 3.
+template <int N, class A, class Read, class Mul, class Other>
+__device__ inline void in_order(A (&first)[4], Read read, Mul mul, Other other)
 {
     constexpr int kOnly = 0x2 | 0x4;   // vector and scalar arithmetic may move across
 #pragma unroll
@@ -416,6 +434,7 @@ __device__ inline void in_order(A (&first)[4], Read read, Mul mul)
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             if (i + 4 + k < N) next[k] = read(i + 4 + k);
+        other(i);
         __builtin_amdgcn_sched_barrier(kOnly);
 #pragma unroll
         for (int k = 0; k < 4; ++k)
@@ -615,16 +634,26 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
         }
         if (tid < KT / 32) s_bad[0][tid] = s_bad[1][tid] = 0;
         __syncthreads();
+        int32_t wave_lo, wave_hi;   // none of the wave's rows attends to keys outside
         {
             int32_t lo = in.lo, hi = in.hi;   // all rows attend to the keys of [largest lo, least hi)
+            int32_t any_lo = in.lo < in.hi ? in.lo : INT32_MAX, any_hi = in.hi;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 lo = max(lo, __shfl_xor(lo, o));
                 hi = min(hi, __shfl_xor(hi, o));
+                any_lo = min(any_lo, __shfl_xor(any_lo, o));
+                any_hi = max(any_hi, __shfl_xor(any_hi, o));
             }
             if (lane == 0) {
                 atomicMax(&s_lo, lo);
                 atomicMin(&s_hi, hi);
+            }
+            wave_lo = uniform(any_lo);
+            wave_hi = uniform(any_hi);
+            if (p.tree) {
+                wave_lo = min(wave_lo, x.len);
+                wave_hi = x.keys;
             }
         }
         __syncthreads();
@@ -692,29 +721,55 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
         // The wave's share of a tile straight to shared memory.  The pages of
         // the next one are asked for a tile ahead.
         int32_t page[S::GROUPS], slot[S::GROUPS];
-        const uint32_t slot_bytes = (uint32_t)p.slot_stride * (uint32_t)sizeof(CT);
+        constexpr int32_t kWhole = ~(S::GROUP - 1);
+        const char *k_base = nullptr, *v_base = nullptr;
+        const int32_t *entries = nullptr;
+        uint32_t slot_bytes = 0, n_pages = 0, page_mul = 0, page_shift = 0;
+        int64_t page_bytes = 0;
+        int32_t page_size = 0, least_key = 0, most_key = 0, last_key = 0;
+        if constexpr (S::DMA) {
+            k_base = kept(reinterpret_cast<const char *>(uniform(kb)));
+            v_base = kept(reinterpret_cast<const char *>(uniform(vb)));
+            entries = kept(uniform(table));
+            slot_bytes = kept((uint32_t)p.slot_stride * (uint32_t)sizeof(CT));
+            page_bytes = kept(p.page_stride * (int64_t)sizeof(CT));
+            n_pages = kept((uint32_t)p.n_pages);
+            page_mul = kept(p.page_mul);
+            page_shift = kept(p.page_shift);
+            page_size = kept(p.page_size);
+            least_key = kept(span.x);
+            last_key = kept(span.y - 1);
+            most_key = last_key & kWhole;
+        }
         const auto group_key = [&](int32_t k0, int j) {   // the first key of a group, or of the nearest attended ones
-            constexpr int32_t whole = ~(S::GROUP - 1);
-            return min(max(k0 + wave * S::SHARE + j * S::GROUP, span.x & whole), (span.y - 1) & whole);
+            return min(max(k0 + wave * S::SHARE + j * S::GROUP, least_key & kWhole), most_key);
         };
         auto fetch = [&](int32_t tile) {
 #pragma unroll
             for (int j = 0; j < S::GROUPS; ++j) {
                 const int32_t key = group_key((first_tile + min(tile, last - 1)) * KT, j);
-                const int32_t of = divide(key, p.page_mul, p.page_shift);
-                page[j] = table[of];
-                slot[j] = key - of * p.page_size;
+                const int32_t of = divide(key, page_mul, page_shift);
+                page[j] = entries[of];
+                slot[j] = key - of * page_size;
             }
         };
+        // a lane's row of a load and its piece of it, from the first row's keys
+        const int row0 = lane / S::IN, piece = lane % S::IN, first_row = wave * S::SHARE;
+        uint32_t k_off[S::LOADS], v_off[S::LOADS];
+#pragma unroll
+        for (int c = 0; c < S::LOADS; ++c) {
+            k_off[c] = row0 * slot_bytes + S::key_piece(first_row + c * S::RI + row0, piece) * 16;
+            v_off[c] = row0 * slot_bytes + S::value_piece(c * S::RI + row0, piece) * 16;
+        }
+        const int exact = p.d == DP;
         auto send = [&](int32_t k0, int turn) {
             uint32_t bad = 0;
 #pragma unroll
             for (int j = 0; j < S::GROUPS; ++j) {
-                const int32_t key = group_key(k0, j), low = max(span.x - key, 0), high = min(span.y - 1 - key, S::GROUP - 1);
-                const int first_row = wave * S::SHARE + j * S::GROUP;
-                const uint32_t k_to = turn * 2 * S::TILE + first_row * S::PITCH, v_to = k_to + S::TILE;
-                const int32_t of = uniform(page[j]);
-                if (of < 0 || of >= p.n_pages) {
+                const int32_t key = group_key(k0, j), low = max(least_key - key, 0), high = min(last_key - key, S::GROUP - 1);
+                const uint32_t k_to = turn * 2 * S::TILE + (first_row + j * S::GROUP) * S::PITCH, v_to = k_to + S::TILE;
+                const uint32_t of = (uint32_t)uniform(page[j]);
+                if (of >= n_pages) {   // (below 0 too)
                     bad |= 1u << j;   // (0: rows that do not attend to them must not see what lies there)
                     for (int c = lane; c < S::GROUP * S::PITCH / 16; c += 64) {
                         *reinterpret_cast<u32x4 *>(s_buf + k_to + c * 16) = u32x4{0, 0, 0, 0};
@@ -722,16 +777,24 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                     }
                     continue;
                 }
-                const int64_t at = of * p.page_stride + slot[j] * p.slot_stride;
-                const CT *const k_from = uniform(kb + at), *const v_from = uniform(vb + at);
-                const uint32_t mine = again(lane), row0 = mine / S::IN, piece = mine % S::IN;
+                const int64_t at = of * page_bytes + (int64_t)((uint64_t)(uint32_t)uniform(slot[j]) * slot_bytes);
+                const char *const k_from = k_base + at, *const v_from = v_base + at;
+                if (exact && low == 0 && high == S::GROUP - 1) {
 #pragma unroll
-                for (int c = 0; c < S::LOADS; ++c) {
-                    const int row = c * S::RI + row0;
-                    const uint32_t off = __umul24(min(max(row, low), high), slot_bytes);
-                    const uint32_t kp = S::key_piece(first_row + row, piece), vp = S::value_piece(first_row + row, piece);
-                    if (p.d == DP || kp * (16 / (int)sizeof(CT)) < (uint32_t)p.d) to_shared(k_from, off + kp * 16, buf + k_to + c * 1024);
-                    if (p.d == DP || vp * (16 / (int)sizeof(CT)) < (uint32_t)p.d) to_shared(v_from, off + vp * 16, buf + v_to + c * 1024);
+                    for (int c = 0; c < S::LOADS; ++c) {
+                        to_shared(k_from + (uint64_t)(c * S::RI * slot_bytes), k_off[c], buf + k_to + c * 1024);
+                        to_shared(v_from + (uint64_t)(c * S::RI * slot_bytes), v_off[c], buf + v_to + c * 1024);
+                    }
+                } else {   // (a key outside the attended ones stands for the nearest of them)
+                    const uint32_t mine = again(lane), d = argument<Params>().d;
+#pragma unroll 1
+                    for (int c = 0; c < S::LOADS; ++c) {
+                        const int row = c * S::RI + mine / S::IN;
+                        const uint32_t off = __umul24(min(max(row, low), high), slot_bytes);
+                        const uint32_t kp = S::key_piece(first_row + row, mine % S::IN), vp = S::value_piece(row, mine % S::IN);
+                        if (kp * (16 / (int)sizeof(CT)) < d) to_shared(k_from, off + kp * 16, buf + k_to + c * 1024);
+                        if (vp * (16 / (int)sizeof(CT)) < d) to_shared(v_from, off + vp * 16, buf + v_to + c * 1024);
+                    }
                 }
             }
             if (lane == 0) s_waves[turn][wave] = bad;
@@ -808,13 +871,29 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                 const uint32_t now = S::DMA ? turn * 2 * S::TILE : 0;   // the tile's place in s_buf
                 const int32_t k0 = (first_tile + tile) * KT;
                 partial = !(k0 >= all_lo && k0 + KT <= all_hi);
+                bool spread = false, skip = false;
+                int64_t from[S::GROUPS];
                 if (fresh) {
                     if constexpr (S::DMA) {
                         arrived();
                         __syncthreads();   // the tile is there, the one before has been read
+                        // The next tile's loads one by one between the products,
+                        // which would wait for their way out otherwise; those of
+                        // a tile at an end of the keys, or without a page, at once.
+                        skip = k0 + wk * S::KW >= wave_hi || k0 + (wk + 1) * S::KW <= wave_lo;
                         if (tile + 1 < last) {
-                            send(k0 + KT, turn ^ 1);
-                            fetch(tile + 2);
+                            spread = exact && !skip;
+#pragma unroll
+                            for (int j = 0; j < S::GROUPS; ++j) {
+                                const int32_t key = k0 + KT + wave * S::SHARE + j * S::GROUP;
+                                const uint32_t of = (uint32_t)uniform(page[j]);
+                                spread &= key >= least_key && key + S::GROUP - 1 <= last_key && of < n_pages;
+                                from[j] = of * page_bytes + (int64_t)((uint64_t)(uint32_t)uniform(slot[j]) * slot_bytes);
+                            }
+                            if (!spread) {
+                                send(k0 + KT, turn ^ 1);
+                                fetch(tile + 2);
+                            }
                         }
                         note = (s_waves[turn][0] | s_waves[turn][1] | s_waves[turn][2] | s_waves[turn][3]) != 0;
                         if (partial) {
@@ -835,6 +914,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                     }
                     note = uniform((int32_t)note);
                 }
+                if (S::DMA ? skip : k0 + wk * S::KW >= wave_hi || k0 + (wk + 1) * S::KW <= wave_lo) continue;
 
                 // scores of the wave's keys (rows) and rows (columns)
 #pragma unroll
@@ -843,32 +923,51 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                 {
                     // (a block of 32 keys does not change a row's piece)
                     const auto read = [&](int i) { return shared<Q>((k_now ^ 32 * (i / U)) + 32 * (i % U) * S::PITCH); };
-                    Q a[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) a[i] = read(i);
-                    in_order<QV * U>(a, read, [&](int i, const Q &x) {
+                    const auto mul = [&](int i, const Q &x) {
                         if constexpr (S::F32) {
 #pragma unroll
                             for (int e = 0; e < 4; ++e) sx[i % U] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], q[i / U][e], sx[i % U], 0, 0, 0);
                         } else {
                             sx[i % U] = Mfma<T>::mul(x, q[i / U], sx[i % U]);
                         }
-                    });
+                    };
+                    Q a[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) a[i] = read(i);
+                    if (spread) {
+                        constexpr int kAll = 2 * S::GROUPS * S::LOADS, kEach = (kAll * 4 + QV * U - 1) / (QV * U);
+                        in_order<QV * U>(a, read, mul, [&](int i) {
+#pragma unroll
+                            for (int k = i / 4 * kEach; k < (i / 4 + 1) * kEach && k < kAll; ++k) {
+                                const int c = k / 2 % S::LOADS, j = k / 2 / S::LOADS;
+                                const uint32_t to = buf + (turn ^ 1) * 2 * S::TILE + (first_row + j * S::GROUP) * S::PITCH + c * 1024;
+                                if (k % 2 == 0)
+                                    to_shared(k_base + from[j] + (uint64_t)(c * S::RI * slot_bytes), k_off[c], to);
+                                else
+                                    to_shared(v_base + from[j] + (uint64_t)(c * S::RI * slot_bytes), v_off[c], to + S::TILE);
+                            }
+                        });
+                        if (lane == 0) s_waves[turn ^ 1][wave] = 0;
+                        fetch(tile + 2);
+                    } else {
+                        in_order<QV * U>(a, read, mul, [](int) {});
+                    }
                 }
                 // element i of a lane's: key 8 (i / 4) + 4 g + i % 4 of 32
                 if (!sc.raw) {
+                    const auto &a = argument<Params>();
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
                         const int32_t kw = k0 + wk * S::KW + 32 * u;
                         sx[u] *= sc.in;
-                        if (p.cap > 0.0f) cap_of<S::F32, S::F32 || S::SPLIT>(sx[u], p.cap, sc.cap);
-                        if (p.slopes) {
-                            if (p.tree && kw + 32 > x.len) {
+                        if (a.cap > 0.0f) cap_of<S::F32, S::F32 || S::SPLIT>(sx[u], a.cap, sc.cap);
+                        if (a.slopes) {
+                            if (a.tree && kw + 32 > x.len) {
 #pragma unroll 1
                                 for (int e = 0; e < 16; ++e) {   // (keys of nodes are where their nodes are)
                                     int32_t at = kw + 8 * (e / 4) + 4 * g + e % 4;
                                     if (at >= x.len)
-                                        at = (int32_t)min((int64_t)x.len + max(p.depth[x.start + min(at - x.len, x.n - 1)], 0), (int64_t)INT32_MAX);
+                                        at = (int32_t)min((int64_t)x.len + max(a.depth[x.start + min(at - x.len, x.n - 1)], 0), (int64_t)INT32_MAX);
                                     const float y = sc.slope * (float)abs(in.position - at);
 #pragma unroll
                                     for (int k = 0; k < 16; ++k) sx[u][k] -= k == e ? y : 0.0f;
@@ -882,16 +981,17 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                     }
                 }
                 if (partial) {
+                    const auto &a = argument<Params>();
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
                         const int32_t kw = k0 + wk * S::KW + 32 * u;
                         const int32_t lo = min(max(in.lo - kw, 0), 32), hi = min(max(in.hi - kw, 0), 32);
                         in32[u] = (uint32_t)((1ull << hi) - 1) & ~(uint32_t)((1ull << lo) - 1);
-                        if (p.tree && kw + 32 > x.len && kw < x.keys) {
+                        if (a.tree && kw + 32 > x.len && kw < x.keys) {
                             // bits of the nodes from the first of these keys on
                             const int32_t node = kw - x.len, w = max(node, 0) >> 5;
                             uint64_t bits = mask[w];
-                            if (w + 1 < p.mask_words) bits |= (uint64_t)mask[w + 1] << 32;
+                            if (w + 1 < a.mask_words) bits |= (uint64_t)mask[w + 1] << 32;
                             uint32_t word = node < 0 ? (uint32_t)(bits << -node) : (uint32_t)(bits >> (node & 31));
                             const int32_t end = x.keys - kw;   // > 0
                             if (end < 32) word &= (1u << end) - 1;
@@ -918,7 +1018,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                         }
                         if ((partial ? u ? in32[U - 1] : in32[0] : ~0u) & bad) {
                             l = __builtin_nanf("");
-                            if (valid && p.status) atomicOr(&p.status[s], DSIM_ST_BAD_PAGE);
+                            if (int32_t *status = argument<Params>().status; status && valid) atomicOr(&status[s], DSIM_ST_BAD_PAGE);
                         }
                     }
                 }
@@ -947,7 +1047,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                     weigh();
                     in_order<16 * OB>(a, read, [&](int i, float x) {
                         o[i % OB] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, sx[0][i / OB], o[i % OB], 0, 0, 0);
-                    });
+                    }, [](int) {});
                 } else {
                     using lds4 = __attribute__((address_space(3))) s16x4;
                     const uint32_t v_now = again(v_at + now);
@@ -975,7 +1075,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                     in_order<2 * U * OB>(a, read, [&](int i, const vec<T, 8> &x) {
                         o[i % OB] = Mfma<T>::mul(x, w[i / OB], o[i % OB]);
                         if constexpr (S::SPLIT) o[i % OB] = Mfma<T>::mul(x, w2[i / OB], o[i % OB]);
-                    });
+                    }, [](int) {});
                 }
             }
             if (tile >= last) break;
