@@ -11,10 +11,9 @@
 namespace dsim {
 namespace rows {
 
-constexpr int kWaves = 4;
-constexpr int kBlock = 64 * kWaves;
 constexpr int kCus = 256;
 constexpr int kMaxGrid = 2 * kCus;
+constexpr int kJoin = 256;           // threads of the join
 constexpr int kPlan = 1024;          // threads of the plan
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // What a block of rows costs beside its tiles, in tiles.
@@ -330,23 +329,27 @@ __device__ inline float rescale(float from, float to, float scale)
 // block of rows share out the keys of a tile.
 // WHOLE: pages of a multiple of 16 slots, so that 16 keys lie in one page.
 template <class T, class CT, int DP_, int WR_, bool WHOLE> struct Shape {
-    static constexpr int DP = DP_, WR = WR_, WK = kWaves / WR;
+    static constexpr int DP = DP_, WR = WR_, WAVES = WR == 8 ? 8 : 4, BLOCK = 64 * WAVES, WK = WAVES / WR;
     static constexpr bool F32 = sizeof(T) == 4;
-    static constexpr int U = !F32 && WR == 4 ? 2 : 1;          // times 32 keys of a tile for each wave
-    static constexpr int KW = 32 * U, KT = WK * KW, M = 32 * WR;
+    static constexpr int U = !F32 && WR >= 4 ? 2 : 1;          // times 32 keys of a tile for each wave
+    // A tile is H steps of KS keys, KW of them a wave's: what has to be done
+    // once a tile is done less often.
+    static constexpr int H = (WR == 8 || (WR == 4 && DP == 64)) && sizeof(T) == 2 ? 2 : 1;
+    static constexpr int KW = 32 * U, KS = WK * KW, KT = KS * H, M = 32 * WR;
     static constexpr int PITCH = DP * sizeof(T);               // of a row in shared memory
     static constexpr int NC = PITCH / 16;                      // its pieces of 16 bytes
     static constexpr int IN = DP * sizeof(CT) / 16;            // those of a row of the cache
-    static constexpr int NQ = KT * IN / kBlock;                // that a thread loads, of keys and of values
+    static constexpr int NQ = KT * IN / BLOCK;                // that a thread loads, of keys and of values
     static constexpr int TILE = KT * PITCH;                    // bytes of a tile's keys or values
     // Keys and values go to shared memory by themselves, a tile ahead, where
     // they need no widening and two tiles fit.
     static constexpr bool DMA = WHOLE && sizeof(CT) == sizeof(T) && 4 * TILE <= 144 * 1024;
     static constexpr int SUMS = 32 * DP * 4 * (WK - 1) * WR;   // outputs of waves that are joined
     static constexpr int TILES = (DMA ? 4 : 2) * TILE, LDS = TILES > SUMS ? TILES : SUMS;
-    static constexpr int PER_CU = DP <= 128 && LDS <= 78 * 1024 ? 2 : 1;   // workgroups, all resident at once
+    static constexpr int PER_CU = DP <= 128 && WR < 8 && LDS <= 78 * 1024 ? 2 : 1;   // workgroups, all resident at once
+    static constexpr int PER_SIMD = PER_CU * WAVES / 4;
     // Rows of a wave's share of a tile, in groups of one page.
-    static constexpr int SHARE = KT / kWaves, GROUP = SHARE < 16 ? SHARE : 16, GROUPS = SHARE / GROUP;
+    static constexpr int SHARE = KT / WAVES, GROUP = SHARE < 16 ? SHARE : 16, GROUPS = SHARE / GROUP;
     static constexpr int RI = 64 / IN > 0 ? 64 / IN : 1;       // rows of the cache that a wave loads at once
     static constexpr int LOADS = GROUP / RI;                   // loads of a group's keys
     // Offset for the weights' exponents.  fp16 ends at 2^-24: weights up to
@@ -501,17 +504,17 @@ struct Scores {
 
 // OB: blocks of 32 elements of a head that are multiplied.
 template <class T, class CT, int DP, int WR, bool WHOLE, int OB>
-__global__ __launch_bounds__(kBlock)
-__attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape<T, CT, DP, WR, WHOLE>::PER_CU)))) void k_rows(Params p)
+__global__ __launch_bounds__((Shape<T, CT, DP, WR, WHOLE>::BLOCK))
+__attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Shape<T, CT, DP, WR, WHOLE>::PER_SIMD)))) void k_rows(Params p)
 {
     using S = Shape<T, CT, DP, WR, WHOLE>;
     constexpr int WK = S::WK, U = S::U, KT = S::KT, M = S::M;
     constexpr int QV = S::F32 ? OB * 4 : OB * 2;
     using Q = typename std::conditional<S::F32, f32x4, vec<T, 8>>::type;
     __shared__ __attribute__((aligned(1024))) char s_buf[S::LDS];
-    __shared__ float s_m[kWaves][32], s_l[kWaves][32];
+    __shared__ float s_m[S::WAVES][32], s_l[S::WAVES][32];
     __shared__ int32_t s_lo, s_hi;
-    __shared__ uint32_t s_bad[2][KT / 32], s_note[2], s_waves[2][kWaves];
+    __shared__ uint32_t s_bad[2][KT / 32], s_note[2], s_waves[2][S::WAVES];
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave - wr * WK;
     const uint32_t buf = address(s_buf);
@@ -676,7 +679,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
         auto load = [&](int32_t k0) {
 #pragma unroll
             for (int j = 0; j < (S::DMA ? 0 : S::NQ); ++j) {
-                const int piece = j * kBlock + tid, c = piece % S::IN;
+                const int piece = j * S::BLOCK + tid, c = piece % S::IN;
                 const int32_t key = min(max(k0 + piece / S::IN, span.x), span.y - 1);
                 const int32_t of = divide(key, p.page_mul, p.page_shift), page = table[of];
                 const bool ok = page >= 0 && page < p.n_pages, used = c * (16 / (int)sizeof(CT)) < p.d;
@@ -696,7 +699,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
             bool odd = false;
 #pragma unroll
             for (int j = 0; j < (S::DMA ? 0 : S::NQ); ++j) {
-                const int piece = j * kBlock + tid, key = piece / S::IN, c = piece % S::IN;
+                const int piece = j * S::BLOCK + tid, key = piece / S::IN, c = piece % S::IN;
                 if (bad_keys >> j & 1) {
                     atomicOr(&s_bad[turn][key / 32], 1u << key % 32);
                     atomicOr(&s_note[turn], 1u);
@@ -758,8 +761,8 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
         uint32_t k_off[S::LOADS], v_off[S::LOADS];
 #pragma unroll
         for (int c = 0; c < S::LOADS; ++c) {
-            k_off[c] = row0 * slot_bytes + S::key_piece(first_row + c * S::RI + row0, piece) * 16;
-            v_off[c] = row0 * slot_bytes + S::value_piece(c * S::RI + row0, piece) * 16;
+            k_off[c] = (c * S::RI + row0) * slot_bytes + S::key_piece(first_row + c * S::RI + row0, piece) * 16;
+            v_off[c] = (c * S::RI + row0) * slot_bytes + S::value_piece(c * S::RI + row0, piece) * 16;
         }
         const int exact = p.d == DP;
         auto send = [&](int32_t k0, int turn) {
@@ -782,8 +785,8 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                 if (exact && low == 0 && high == S::GROUP - 1) {
 #pragma unroll
                     for (int c = 0; c < S::LOADS; ++c) {
-                        to_shared(k_from + (uint64_t)(c * S::RI * slot_bytes), k_off[c], buf + k_to + c * 1024);
-                        to_shared(v_from + (uint64_t)(c * S::RI * slot_bytes), v_off[c], buf + v_to + c * 1024);
+                        to_shared(k_from, k_off[c], buf + k_to + c * 1024);
+                        to_shared(v_from, v_off[c], buf + v_to + c * 1024);
                     }
                 } else {   // (a key outside the attended ones stands for the nearest of them)
                     const uint32_t mine = again(lane), d = argument<Params>().d;
@@ -809,7 +812,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
         for (int e = 0; e < OB; ++e) o[e] = f32x16(0.0f);
 
         if (S::DMA && p.d < DP) {   // what the padded rows' ends are multiplied as
-            for (int c = tid; c < S::TILES / 16; c += kBlock) reinterpret_cast<u32x4 *>(s_buf)[c] = u32x4{0, 0, 0, 0};
+            for (int c = tid; c < S::TILES / 16; c += S::BLOCK) reinterpret_cast<u32x4 *>(s_buf)[c] = u32x4{0, 0, 0, 0};
             __syncthreads();
         }
         if (n > 0) {
@@ -864,23 +867,26 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
 
         // What scales the outputs or adds to them one by one stands outside the
         // inner loop, which leaves it to them: a tile is begun again behind it.
-        for (int32_t tile = t0;;) {
+        for (int32_t step = t0 * S::H;;) {
 #pragma unroll 1
-            for (; tile < last; ++tile, fresh = true) {
+            for (; step < last * S::H; ++step, fresh = true) {
+                const int32_t tile = step / S::H, half = step - tile * S::H;
                 const int turn = tile & 1;
-                const uint32_t now = S::DMA ? turn * 2 * S::TILE : 0;   // the tile's place in s_buf
-                const int32_t k0 = (first_tile + tile) * KT;
-                partial = !(k0 >= all_lo && k0 + KT <= all_hi);
-                bool spread = false, skip = false;
+                const uint32_t now = (S::DMA ? turn * 2 * S::TILE : 0) + half * (S::KS * S::PITCH);   // the step's place in s_buf
+                const int32_t k0 = first_tile * KT + step * S::KS;
+                partial = !(k0 >= all_lo && k0 + S::KS <= all_hi);
+                const bool skip = k0 + wk * S::KW >= wave_hi || k0 + (wk + 1) * S::KW <= wave_lo;
+                bool spread = false;
                 int64_t from[S::GROUPS];
-                if (fresh) {
+                uint32_t without = 0;   // groups of the tile without a page
+                if (fresh && half == 0) {
+                    const bool any = !(k0 >= all_lo && k0 + KT <= all_hi);
                     if constexpr (S::DMA) {
                         arrived();
                         __syncthreads();   // the tile is there, the one before has been read
                         // The next tile's loads one by one between the products,
                         // which would wait for their way out otherwise; those of
                         // a tile at an end of the keys, or without a page, at once.
-                        skip = k0 + wk * S::KW >= wave_hi || k0 + (wk + 1) * S::KW <= wave_lo;
                         if (tile + 1 < last) {
                             spread = exact && !skip;
 #pragma unroll
@@ -895,26 +901,30 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                                 fetch(tile + 2);
                             }
                         }
-                        note = (s_waves[turn][0] | s_waves[turn][1] | s_waves[turn][2] | s_waves[turn][3]) != 0;
-                        if (partial) {
+#pragma unroll
+                        for (int w = 0; w < S::WAVES; ++w) without |= s_waves[turn][w];
+                        note = 0;
+                        if (any) {
                             bool odd = false;
-                            for (int c = tid; c < S::TILE / 16; c += kBlock)
+                            for (int c = tid; c < S::TILE / 16; c += S::BLOCK)
                                 if (S::value_piece(c / S::NC, c % S::NC) * (16 / (int)sizeof(T)) < p.d)
                                     odd |= !finite<T>(*reinterpret_cast<const u32x4 *>(s_buf + now + S::TILE + c * 16));
-                            if (__syncthreads_or(odd)) note |= 2;
+                            if (__syncthreads_or(odd)) note = 2;
                         }
                     } else {
                         __syncthreads();   // the tile before has been read
-                        store(turn, partial);
+                        store(turn, any);
                         if (tid == 0) s_note[turn ^ 1] = 0;
                         if (tid < KT / 32) s_bad[turn ^ 1][tid] = 0;
                         __syncthreads();
                         if (tile + 1 < last) load(k0 + KT);
-                        note = s_note[turn];
+                        note = uniform((int32_t)s_note[turn]);
                     }
-                    note = uniform((int32_t)note);
                 }
-                if (S::DMA ? skip : k0 + wk * S::KW >= wave_hi || k0 + (wk + 1) * S::KW <= wave_lo) continue;
+                if (skip) {
+                    if (S::DMA && fresh && half == 0) note |= uniform((int32_t)without) != 0;
+                    continue;
+                }
 
                 // scores of the wave's keys (rows) and rows (columns)
 #pragma unroll
@@ -942,9 +952,9 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                                 const int c = k / 2 % S::LOADS, j = k / 2 / S::LOADS;
                                 const uint32_t to = buf + (turn ^ 1) * 2 * S::TILE + (first_row + j * S::GROUP) * S::PITCH + c * 1024;
                                 if (k % 2 == 0)
-                                    to_shared(k_base + from[j] + (uint64_t)(c * S::RI * slot_bytes), k_off[c], to);
+                                    to_shared(k_base + from[j], k_off[c], to);
                                 else
-                                    to_shared(v_base + from[j] + (uint64_t)(c * S::RI * slot_bytes), v_off[c], to + S::TILE);
+                                    to_shared(v_base + from[j], v_off[c], to + S::TILE);
                             }
                         });
                         if (lane == 0) s_waves[turn ^ 1][wave] = 0;
@@ -953,6 +963,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                         in_order<QV * U>(a, read, mul, [](int) {});
                     }
                 }
+                if (S::DMA && fresh && half == 0) note |= uniform((int32_t)without) != 0;
                 // element i of a lane's: key 8 (i / 4) + 4 g + i % 4 of 32
                 if (!sc.raw) {
                     const auto &a = argument<Params>();
@@ -1009,12 +1020,12 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                         uint32_t bad = 0;   // bits of the keys without a page
                         if constexpr (S::DMA) {
                             for (int j = 0; j < 32 / S::GROUP; ++j) {
-                                const int at = (wk * S::KW + 32 * u) / S::GROUP + j;   // group of the tile
+                                const int at = (half * S::KS + wk * S::KW + 32 * u) / S::GROUP + j;   // group of the tile
                                 if (s_waves[turn][at / S::GROUPS] >> at % S::GROUPS & 1)
-                                    bad |= (S::GROUP == 16 ? 0xffffu : 0xffu) << j * S::GROUP;
+                                    bad |= ((1u << S::GROUP) - 1) << j * S::GROUP;
                             }
                         } else {
-                            bad = s_bad[turn][(wk * S::KW + 32 * u) / 32];
+                            bad = s_bad[turn][(half * S::KS + wk * S::KW + 32 * u) / 32];
                         }
                         if ((partial ? u ? in32[U - 1] : in32[0] : ~0u) & bad) {
                             l = __builtin_nanf("");
@@ -1032,7 +1043,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                     top = fmaxf(y[0], y[1]);
                 }
                 // (once a tile: whatever the scores, every loop ends)
-                if ((fresh && __builtin_amdgcn_ballot_w64(top > limit) != 0) || (note & 2)) break;
+                if ((fresh && __builtin_amdgcn_ballot_w64(top > limit) != 0) || (partial && (note & 2))) break;
                 // outputs (rows) of the rows (columns); the first values come
                 // while the weights are computed
                 if constexpr (S::F32) {
@@ -1078,7 +1089,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                     }, [](int) {});
                 }
             }
-            if (tile >= last) break;
+            if (step >= last * S::H) break;
 
             {
                 const float to = top > limit ? top : m, f = rescale(m, to, sc.unit);
@@ -1089,10 +1100,11 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                 limit = m == -HUGE_VALF ? m : m + S::SLACK / sc.unit;
             }
             fresh = false;
-            if (note & 2) {
+            if (partial && (note & 2)) {
                 // Values that are not finite, and rows that do not attend to
                 // them: a weight of 0 would make them NaN, so each product
                 // stands alone.
+                const int32_t tile = step / S::H, half = step - tile * S::H;
                 const char *const from = s_buf + (S::DMA ? (tile & 1) * 2 * S::TILE : 0) + S::TILE;
                 weigh();
 #pragma unroll 1
@@ -1108,7 +1120,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                     }
                     const auto both = halves(mine);
                     const float w = k >> 2 & 1 ? both[1] : both[0];
-                    const int key = wk * S::KW + k;
+                    const int key = half * S::KS + wk * S::KW + k;
 #pragma unroll
                     for (int d = 0; d < OB; ++d)
 #pragma unroll
@@ -1123,7 +1135,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
                             }
                         }
                 }
-                ++tile;
+                ++step;
                 fresh = true;
             }
         }
@@ -1199,9 +1211,9 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_CU), (Shape
 // Joins the parts of a block that a run's end cut, kJoinRows rows a
 // workgroup: the rows' maxima and sums first, then four outputs a thread.
 constexpr int kJoinRows = 32;
-template <class T> __global__ __launch_bounds__(kBlock) void k_join(Params p, float up)
+template <class T> __global__ __launch_bounds__(kJoin) void k_join(Params p, float up)
 {
-    constexpr int kWays = kBlock / kJoinRows;
+    constexpr int kWays = kJoin / kJoinRows;
     __shared__ float s_m[kWays][kJoinRows], s_l[kWays][kJoinRows];
     const int index = blockIdx.x, tid = threadIdx.x;
     const int4 cut = p.cut[index];
@@ -1232,7 +1244,7 @@ template <class T> __global__ __launch_bounds__(kBlock) void k_join(Params p, fl
         __syncthreads();
     }
     const int quads = p.d / 4;
-    for (int e = tid; e < kJoinRows * quads; e += kBlock) {
+    for (int e = tid; e < kJoinRows * quads; e += kJoin) {
         const int at = e / quads, d = 4 * (e - at * quads);
         const int32_t row = cut.w * p.rows + first + at, i = divide(row, p.group_mul, p.group_shift);
         if (row >= total_rows) break;
@@ -1260,9 +1272,9 @@ template <class T, class CT, int DP, int WR, bool WHOLE, int OB> dsim_status lau
         if ((st = check("attention plan launch"))) return st;
     }
     const int grid = p.direct ? (int)(p.max_blocks * p.n_heads) : kCus * S::PER_CU;
-    hipLaunchKernelGGL((k_rows<T, CT, DP, WR, WHOLE, OB>), dim3(grid), dim3(kBlock), 0, s, p);
+    hipLaunchKernelGGL((k_rows<T, CT, DP, WR, WHOLE, OB>), dim3(grid), dim3(S::BLOCK), 0, s, p);
     if ((st = check("attention launch")) || p.direct) return st;
-    hipLaunchKernelGGL((k_join<T>), dim3(grid, S::M / kJoinRows), dim3(kBlock), 0, s, p, S::UP);
+    hipLaunchKernelGGL((k_join<T>), dim3(grid, S::M / kJoinRows), dim3(kJoin), 0, s, p, S::UP);
     return check("attention join launch");
 }
 
@@ -1281,6 +1293,8 @@ template <class T, class CT, int DP> dsim_status launch(Params &p, hipStream_t s
     if constexpr (DP <= 128)
         if (p.rows == 32) return launch<T, CT, DP, 1>(p, s);
     if (p.rows == 64) return launch<T, CT, DP, 2>(p, s);
+    if constexpr (DP <= 128)
+        if (p.rows == 256) return launch<T, CT, DP, 8>(p, s);
     return launch<T, CT, DP, 4>(p, s);
 }
 

@@ -10,7 +10,7 @@ namespace rows {
 static int rows_of(int64_t n_tok, int32_t n_seq, int32_t group, int32_t head_dim)
 {
     const int64_t average = n_seq > 0 ? (n_tok * group + n_seq - 1) / n_seq : 0;
-    return average <= 32 && head_dim <= 128 ? 32 : average <= 64 ? 64 : 128;
+    return average <= 32 && head_dim <= 128 ? 32 : average <= 64 ? 64 : average <= 512 || head_dim > 128 ? 128 : 256;
 }
 
 static int64_t blocks(int64_t n_tok, int32_t n_seq, int32_t group, int rows)
@@ -28,7 +28,7 @@ struct Layout {
         first = up(span + 8 * (size_t)n_blocks);
         cut = up(first + 4 * ((size_t)n_seq + 1));
         part = cut + sizeof(int4) * kMaxGrid;
-        end = part + (size_t)kMaxGrid * 2 * rows * (d + 2) * sizeof(float);
+        end = part + (size_t)(rows == 256 ? kCus : kMaxGrid) * 2 * rows * (d + 2) * sizeof(float);
     }
 };
 

@@ -217,6 +217,16 @@ def test_in_place(dtype, cache, width):
     check(dtype, cache, 4, 2, 128, 16, new, lens, width=width, in_place=True, tree=True)
 
 
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("heads,kv,d,slots", [(4, 1, 128, 16), (4, 1, 64, 48), (4, 1, 80, 7), (5, 5, 256, 16), (3, 1, 112, 32)])
+def test_many_rows(dtype, cache, heads, kv, d, slots):
+    """Prompts of the largest blocks of rows."""
+    new, lens = [700, 3, 560, 1], [700, 900, 561, 1]
+    check(dtype, cache, heads, kv, d, slots, new, lens, seed=2)
+    check(dtype, cache, heads, kv, d, slots, new, lens, seed=3, window=333, cap=30.0, prefix=[40, 0, 500, 0])
+    check(dtype, cache, heads, kv, d, slots, [300, 1, 800], [40, 900, 0], seed=4, tree=True, width=2000 // slots)
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.3, 1e-30, 5.0])
 def test_scales(scale):
     check(BF16, BF16, 4, 2, 64, 16, [20, 60], [50, 60], scale=scale)
