@@ -116,6 +116,16 @@ __device__ inline Range range_of(const Params &p, const Seq &x, int s, int32_t i
                     p.depth ? p.depth[t] : 0);
 }
 
+// Whether token i attends to a key.
+__device__ inline bool attends(const Params &p, const Seq &x, int s, int32_t i, int32_t key)
+{
+    const Range r = range_of(p, x, s, i);
+    if (key >= r.lo && key < r.hi) return true;
+    if (!p.tree || key < x.len || key >= x.keys) return false;
+    const int32_t node = key - x.len;
+    return p.mask[(x.start + i) * p.mask_stride + node / 32] >> node % 32 & 1;
+}
+
 // The keys that some token of tokens i0 to i1 attends to lie in [x, y); with
 // first keys, of every `lanes`-th of them.
 __device__ inline int2 span_of(const Params &p, const Seq &x, int s, int32_t i0, int32_t i1, int lane, int lanes)
@@ -249,19 +259,24 @@ template <int KT> __global__ __launch_bounds__(kPlan) void k_plan(Params p)
     if (threadIdx.x == 0) p.cost[n] = before;
 }
 
-// 16 bytes of T hold nothing but numbers
-template <class T> __device__ inline bool finite(u32x4 x)
+// What is not finite of 16 bytes of T becomes 0; whether there was any.
+template <class T> __device__ inline bool clean(u32x4 &x)
 {
     constexpr uint32_t top = __is_same(T, f16) ? 0x7c00u : 0x7f80u;
-    bool ok = true;
+    bool odd = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (sizeof(T) == 4)
-            ok &= (x[i] & 0x7f800000u) != 0x7f800000u;
-        else
-            ok &= (x[i] & top) != top && (x[i] & top << 16) != top << 16;
+        uint32_t keep = ~0u;
+        if (sizeof(T) == 4) {
+            if ((x[i] & 0x7f800000u) == 0x7f800000u) keep = 0;
+        } else {
+            if ((x[i] & top) == top) keep &= 0xffff0000u;
+            if ((x[i] & top << 16) == top << 16) keep &= 0xffffu;
+        }
+        odd |= keep != ~0u;
+        x[i] &= keep;
     }
-    return ok;
+    return odd;
 }
 
 // eight e4m3 in fp16 or bf16, exactly
@@ -459,6 +474,23 @@ template <> struct Mfma<bf16> {
     __device__ static f32x16 mul(vec<bf16, 8> a, vec<bf16, 8> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 
+// The left operand of keys 16 k to 16 k + 15 of a tile's values: the lane's
+// place of the first is `at`.
+template <class T, int PITCH> __device__ inline vec<T, 8> values(uint32_t at, int k)
+{
+    using lds4 = __attribute__((address_space(3))) s16x4;
+    s16x4 part[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+        part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(uintptr_t)(at + (16 * k + 8 * j) * PITCH));
+    return __builtin_bit_cast(vec<T, 8>, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+__device__ inline float value_of(float x) { return x; }
+__device__ inline float value_of(f16 x) { return (float)x; }
+__device__ inline float value_of(bf16 x) { return (float)x; }
+__device__ inline float value_of(e4m3 x) { return (x.bits & 0x7f) == 0x7f ? __builtin_nanf("") : 0.0f; }   // (or a finite one)
+
 // A part of a block: the outputs of its rows, their maxima and sums.
 struct Part {
     float *o, *m, *l;
@@ -470,13 +502,14 @@ struct Part {
 };
 
 template <class T>
-__device__ inline void write_row(const Params &p, int64_t t, int head, int d, f32x4 x, float l)
+__device__ inline void write_row(const Params &p, int64_t t, int head, int d, f32x4 x)
 {
-    // (a row that attends to a bad page has the sum NaN)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = l == 0.0f ? 0.0f : x[k] / l;
     *reinterpret_cast<vec<T, 4> *>(static_cast<T *>(p.out) + t * p.out_row + head * p.out_head + d) = from_f32<T, 4>(x);
 }
+
+// What a row's outputs are multiplied by.  (One that attends to nothing has
+// the sum 0, one that attends to a bad page NaN.)
+__device__ inline float share_of(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 
 __device__ inline void write_lse(const Params &p, int64_t t, int head, float m, float scale, float l, float up)
 {
@@ -513,7 +546,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
     using Q = typename std::conditional<S::F32, f32x4, vec<T, 8>>::type;
     __shared__ __attribute__((aligned(1024))) char s_buf[S::LDS];
     __shared__ float s_m[S::WAVES][32], s_l[S::WAVES][32];
-    __shared__ int32_t s_lo, s_hi;
+    __shared__ int32_t s_lo, s_hi, s_odd;
     __shared__ uint32_t s_bad[2][KT / 32], s_note[2], s_waves[2][S::WAVES];
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave - wr * WK;
@@ -634,6 +667,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
             s_lo = 0;
             s_hi = INT32_MAX;
             s_note[0] = s_note[1] = 0;
+            s_odd = 0;
         }
         if (tid < KT / 32) s_bad[0][tid] = s_bad[1][tid] = 0;
         __syncthreads();
@@ -692,8 +726,10 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                 }
             }
         };
-        // pieces of the tile to shared memory; partial: values that are not
-        // finite are told of
+        // Pieces of the tile to shared memory.  Of tiles that not all rows
+        // attend to all of, values that are not finite become 0, for a weight
+        // of 0 would make them NaN: what they make of the rows that do attend
+        // to them is put right behind the block.
         auto store = [&](int turn, bool partial) {
             char *const s_k = s_buf, *const s_v = s_buf + S::TILE;
             bool odd = false;
@@ -708,18 +744,19 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                     const auto kk = __builtin_bit_cast(vec<uint32_t, 4>, kx[j]), vv = __builtin_bit_cast(vec<uint32_t, 4>, vx[j]);
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        const vec<T, 8> a = widen8<T>(kk[2 * half], kk[2 * half + 1]), v = widen8<T>(vv[2 * half], vv[2 * half + 1]);
+                        const vec<T, 8> a = widen8<T>(kk[2 * half], kk[2 * half + 1]);
+                        u32x4 v = __builtin_bit_cast(u32x4, widen8<T>(vv[2 * half], vv[2 * half + 1]));
+                        if (partial) odd |= clean<T>(v);
                         *reinterpret_cast<vec<T, 8> *>(s_k + key * S::PITCH + S::key_piece(key, 2 * c + half) * 16) = a;
-                        *reinterpret_cast<vec<T, 8> *>(s_v + key * S::PITCH + S::value_piece(key, 2 * c + half) * 16) = v;
-                        if (partial) odd |= !finite<T>(__builtin_bit_cast(u32x4, v));
+                        *reinterpret_cast<u32x4 *>(s_v + key * S::PITCH + S::value_piece(key, 2 * c + half) * 16) = v;
                     }
                 } else {
                     *reinterpret_cast<u32x4 *>(s_k + key * S::PITCH + S::key_piece(key, c) * 16) = kx[j];
+                    if (partial) odd |= clean<T>(vx[j]);
                     *reinterpret_cast<u32x4 *>(s_v + key * S::PITCH + S::value_piece(key, c) * 16) = vx[j];
-                    if (partial) odd |= !finite<T>(vx[j]);
                 }
             }
-            if (odd) atomicOr(&s_note[turn], 2u);
+            if (odd) s_odd = 1;
         };
         // The wave's share of a tile straight to shared memory.  The pages of
         // the next one are asked for a tile ahead.
@@ -904,12 +941,16 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
 #pragma unroll
                         for (int w = 0; w < S::WAVES; ++w) without |= s_waves[turn][w];
                         note = 0;
-                        if (any) {
-                            bool odd = false;
-                            for (int c = tid; c < S::TILE / 16; c += S::BLOCK)
-                                if (S::value_piece(c / S::NC, c % S::NC) * (16 / (int)sizeof(T)) < p.d)
-                                    odd |= !finite<T>(*reinterpret_cast<const u32x4 *>(s_buf + now + S::TILE + c * 16));
-                            if (__syncthreads_or(odd)) note = 2;
+                        if (any) {   // (see store)
+                            for (int c = tid; c < S::TILE / 16; c += S::BLOCK) {
+                                u32x4 *const at = reinterpret_cast<u32x4 *>(s_buf + now + S::TILE + c * 16);
+                                u32x4 v = *at;
+                                if (S::value_piece(c / S::NC, c % S::NC) * (16 / (int)sizeof(T)) < p.d && clean<T>(v)) {
+                                    *at = v;
+                                    s_odd = 1;
+                                }
+                            }
+                            __syncthreads();
                         }
                     } else {
                         __syncthreads();   // the tile before has been read
@@ -1043,7 +1084,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                     top = fmaxf(y[0], y[1]);
                 }
                 // (once a tile: whatever the scores, every loop ends)
-                if ((fresh && __builtin_amdgcn_ballot_w64(top > limit) != 0) || (partial && (note & 2))) break;
+                if ((fresh && __builtin_amdgcn_ballot_w64(top > limit) != 0)) break;
                 // outputs (rows) of the rows (columns); the first values come
                 // while the weights are computed
                 if constexpr (S::F32) {
@@ -1060,17 +1101,8 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                         o[i % OB] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, sx[0][i / OB], o[i % OB], 0, 0, 0);
                     }, [](int) {});
                 } else {
-                    using lds4 = __attribute__((address_space(3))) s16x4;
                     const uint32_t v_now = again(v_at + now);
-                    const auto read = [&](int i) {
-                        const int k = i / OB, d = i % OB;
-                        s16x4 part[2];
-#pragma unroll
-                        for (int j = 0; j < 2; ++j)
-                            part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                (lds4 *)(uintptr_t)((v_now ^ 64 * d) + (16 * k + 8 * j) * S::PITCH));
-                        return __builtin_bit_cast(vec<T, 8>, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
-                    };
+                    const auto read = [&](int i) { return values<T, S::PITCH>(v_now ^ 64 * (i % OB), i / OB); };
                     vec<T, 8> a[4], w[2 * U], w2[2 * U];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) a[i] = read(i);
@@ -1100,44 +1132,6 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                 limit = m == -HUGE_VALF ? m : m + S::SLACK / sc.unit;
             }
             fresh = false;
-            if (partial && (note & 2)) {
-                // Values that are not finite, and rows that do not attend to
-                // them: a weight of 0 would make them NaN, so each product
-                // stands alone.
-                const int32_t tile = step / S::H, half = step - tile * S::H;
-                const char *const from = s_buf + (S::DMA ? (tile & 1) * 2 * S::TILE : 0) + S::TILE;
-                weigh();
-#pragma unroll 1
-                for (int k = 0; k < 32 * U; ++k) {
-                    float mine = 0.0f;   // the weight, in a lane of the key's half
-                    bool attended = false;
-#pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        if (u == k >> 5) attended = in32[u] >> (k & 31) & 1;
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            if (u == k >> 5 && e == (k >> 3 & 3) * 4 + (k & 3)) mine = sx[u][e];
-                    }
-                    const auto both = halves(mine);
-                    const float w = k >> 2 & 1 ? both[1] : both[0];
-                    const int key = half * S::KS + wk * S::KW + k;
-#pragma unroll
-                    for (int d = 0; d < OB; ++d)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int at = (32 * d + 8 * e + 4 * g) * (int)sizeof(T);
-                            const vec<float, 4> v = to_f32<T, 4>(*reinterpret_cast<const vec<T, 4> *>(
-                                from + key * S::PITCH + S::value_piece(key, at / 16) * 16 + at % 16));
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) {
-                                const float y = __builtin_fmaf(w, v[c], o[d][4 * e + c]);
-                                o[d][4 * e + c] = attended ? y : o[d][4 * e + c];
-                            }
-                        }
-                }
-                ++step;
-                fresh = true;
-            }
         }
 
         // the halves' sums, and the waves that share the rows
@@ -1178,7 +1172,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
         }
         const bool whole = p.direct || tiles == n || span.y == 0;
         if (wk == 0 && valid) {
-            const float vs = p.v_scale ? p.v_scale[kv] : 1.0f;
+            const float vs = (p.v_scale ? p.v_scale[kv] : 1.0f) * (whole ? share_of(l) : 1.0f);
             const Part part = Part::of(p, 2 * index + (t0 == 0 ? 1 : 0));
             const int at = wr * 32 + r;
 #pragma unroll
@@ -1189,7 +1183,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                     if (d >= p.d) continue;
                     const f32x4 y = f32x4{o[e][4 * k], o[e][4 * k + 1], o[e][4 * k + 2], o[e][4 * k + 3]} * vs;
                     if (whole)
-                        write_row<T>(p, t, head, d, y, l);
+                        write_row<T>(p, t, head, d, y);
                     else
                         *reinterpret_cast<f32x4 *>(part.o + at * p.d + d) = y;
                 }
@@ -1199,6 +1193,33 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                 } else {
                     part.m[at] = m;
                     part.l[at] = l;
+                }
+            }
+        }
+        if (n > 0) {
+            __syncthreads();   // (and every tile has been looked at)
+            if (s_odd) {
+                // The values that were taken as 0, added to the rows that attend
+                // to them: infinities and NaN, a thread a column.
+                __threadfence();
+                const Part part = Part::of(p, 2 * index + (t0 == 0 ? 1 : 0));
+                for (int32_t key = max((first_tile + t0) * KT, span.x); key < min((first_tile + last) * KT, span.y); ++key) {
+                    const int32_t k0 = key / KT * KT;
+                    if (k0 >= all_lo && k0 + KT <= all_hi) continue;   // (was not cleaned)
+                    const int32_t of = divide(key, p.page_mul, p.page_shift), page = table[of];
+                    if (page < 0 || page >= p.n_pages || tid >= p.d) continue;
+                    const float v = value_of(vb[page * p.page_stride + (key - of * p.page_size) * p.slot_stride + tid]);
+                    if (fabsf(v) < HUGE_VALF) continue;
+                    for (int at = 0; at < M && b * M + at < total_rows; ++at) {
+                        const int32_t i = (b * M + at) / p.group, h = b * M + at - i * p.group;
+                        if (!attends(p, x, s, i, key)) continue;
+                        if (whole) {
+                            T *const to = static_cast<T *>(p.out) + (x.start + i) * p.out_row + (kv * p.group + h) * p.out_head + tid;
+                            *to = (T)((float)*to + v);
+                        } else {
+                            part.o[at * p.d + tid] += v;
+                        }
+                    }
                 }
             }
         }
@@ -1255,7 +1276,7 @@ template <class T> __global__ __launch_bounds__(kJoin) void k_join(Params p, flo
             const Part y = part(j);
             o += *reinterpret_cast<const f32x4 *>(y.o + (int64_t)(first + at) * p.d + d) * rescale(y.m[first + at], m, sc.unit);
         }
-        write_row<T>(p, start + i, kv * p.group + row - i * p.group, d, o, s_l[0][at]);
+        write_row<T>(p, start + i, kv * p.group + row - i * p.group, d, o * share_of(s_l[0][at]));
     }
 }
 
