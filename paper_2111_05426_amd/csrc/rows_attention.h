@@ -37,6 +37,7 @@ struct Params {
     int64_t *cost;        // [max_blocks + 1] sums of the blocks' costs, one head's
     int2 *span;           // [max_blocks] keys of a block
     int32_t *first;       // [n_seq + 1] sequences' first blocks
+    int64_t *base;        // [n_seq + 1] the costs before them
     int4 *cut;            // [kMaxGrid]
     float *part;
     float scale, cap;     // scale: natural units
@@ -191,22 +192,12 @@ template <class A> __device__ inline int32_t find(A a, int32_t n, int64_t x)
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// The sequence of a block: the last that begins at it or before.
-__device__ inline int sequence_of(const Params &p, int32_t b)
-{
-    int lo = 0, hi = p.n_seq;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        (p.first[mid] <= b ? lo : hi) = mid;
-    }
-    return lo;
-}
-
 // Blocks of rows, their keys and what they cost, and the sequences' status.
 constexpr int kLanes = 16;
 template <int KT> __global__ __launch_bounds__(kPlan) void k_plan(Params p)
 {
     __shared__ int64_t s_sum[kPlan / 64];
+    __shared__ int32_t s_first[kPlan + 1];   // what fits of first
     int64_t before = 0, total;
     for (int s0 = 0; s0 < p.n_seq; s0 += kPlan) {
         const int s = s0 + threadIdx.x;
@@ -220,6 +211,7 @@ template <int KT> __global__ __launch_bounds__(kPlan) void k_plan(Params p)
         // (more rows than tokens: starts that descend; what does not fit is refused)
         if (s < p.n_seq) {
             p.first[s] = (int32_t)min(at, p.max_blocks);
+            if (s < kPlan) s_first[s] = (int32_t)min(at, p.max_blocks);
             if (at + n > p.max_blocks) x.status = DSIM_ST_BAD_POSITION;
             if (p.status && x.len >= 0) p.status[s] = x.status;
         }
@@ -232,9 +224,14 @@ template <int KT> __global__ __launch_bounds__(kPlan) void k_plan(Params p)
     const int lanes = p.first_key ? kLanes : 1;
     for (int32_t at = threadIdx.x; at < n * lanes; at += kPlan) {
         const int32_t b = at / lanes;
-        const int s = sequence_of(p, b);
+        int s = 0, end = p.n_seq;   // the last sequence that begins at the block or before
+        const int32_t *const first = p.n_seq <= kPlan ? s_first : p.first;
+        while (end - s > 1) {
+            const int mid = (s + end) / 2;
+            (first[mid] <= b ? s : end) = mid;
+        }
         const Seq x = seq_of(p, s);
-        const int32_t r0 = (b - p.first[s]) * p.rows, r1 = min(r0 + p.rows, x.n * p.group);
+        const int32_t r0 = (b - first[s]) * p.rows, r1 = min(r0 + p.rows, x.n * p.group);
         int2 span = span_of(p, x, s, r0 / p.group, (r1 - 1) / p.group, at % lanes, lanes);
         if (lanes > 1) {
             if (span.y == 0) span.x = INT32_MAX;
@@ -257,6 +254,11 @@ template <int KT> __global__ __launch_bounds__(kPlan) void k_plan(Params p)
         before += total;
     }
     if (threadIdx.x == 0) p.cost[n] = before;
+    __syncthreads();
+    for (int s = threadIdx.x; s <= p.n_seq; s += kPlan) {
+        const int32_t first = s == p.n_seq ? n : p.first[s];
+        p.base[s] = first == n ? before : p.cost[first];
+    }
 }
 
 // What is not finite of 16 bytes of T becomes 0; whether there was any.
@@ -292,6 +294,18 @@ template <class T> __device__ inline vec<T, 8> widen8(uint32_t lo, uint32_t hi)
 {
     const vec<T, 2> a = widen2<T, false>(lo), b = widen2<T, true>(lo), c = widen2<T, false>(hi), d = widen2<T, true>(hi);
     return {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// The largest, or least, of the 32 lanes of each half.
+template <bool LARGEST> __device__ inline int32_t across(int32_t x)
+{
+    const auto of = [](int32_t a, int32_t b) { return LARGEST ? max(a, b) : min(a, b); };
+    x = of(x, __builtin_amdgcn_mov_dpp(x, 0x128, 0xf, 0xf, true));   // rows of 16, turned by 8, 4, 2, 1
+    x = of(x, __builtin_amdgcn_mov_dpp(x, 0x124, 0xf, 0xf, true));
+    x = of(x, __builtin_amdgcn_mov_dpp(x, 0x122, 0xf, 0xf, true));
+    x = of(x, __builtin_amdgcn_mov_dpp(x, 0x121, 0xf, 0xf, true));
+    const auto y = __builtin_amdgcn_permlane16_swap((uint32_t)x, (uint32_t)x, false, false);
+    return of((int32_t)y[0], (int32_t)y[1]);
 }
 
 __device__ inline vec<float, 2> halves(float x)   // those of lanes r and 32 + r
@@ -546,7 +560,8 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
     using Q = typename std::conditional<S::F32, f32x4, vec<T, 8>>::type;
     __shared__ __attribute__((aligned(1024))) char s_buf[S::LDS];
     __shared__ float s_m[S::WAVES][32], s_l[S::WAVES][32];
-    __shared__ int32_t s_lo, s_hi, s_odd;
+    __shared__ int2 s_range[S::WAVES];
+    __shared__ uint32_t s_odd;
     __shared__ uint32_t s_bad[2][KT / 32], s_note[2], s_waves[2][S::WAVES];
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave - wr * WK;
@@ -583,8 +598,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
     } else {
         // neighbouring runs on one XCD
         index = (index & 7) * (gridDim.x / 8) + (index >> 3);
-        const int32_t blocks = p.first[p.n_seq];
-        const int64_t total = p.cost[blocks] * p.n_heads, even = (total + gridDim.x - 1) / gridDim.x;
+        const int64_t total = p.base[p.n_seq] * p.n_heads, even = (total + gridDim.x - 1) / gridDim.x;
         run = even > kMinTiles ? even : kMinTiles;
         const int64_t begin = index * run, end = min(begin + run, total);
         if (begin >= total) {
@@ -592,15 +606,16 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
             return;
         }
         left = end - begin;
-        s = find([&](int32_t i) { return p.cost[p.first[i]] * p.n_heads; }, p.n_seq, begin);
+        s = find([&](int32_t i) { return p.base[i] * p.n_heads; }, p.n_seq, begin);
         const int32_t first = p.first[s], n = p.first[s + 1] - first;
-        const int64_t base = p.cost[first], each = p.cost[first + n] - base, at = begin - base * p.n_heads;
-        kv = (int)(at / each);
+        const int64_t base = p.base[s], each = p.base[s + 1] - base, at = begin - base * p.n_heads;
+        kv = (int)((at | each) >> 31 ? at / each : (uint32_t)at / (uint32_t)each);
         const int64_t z = at - kv * each;
         b = find([&](int32_t i) { return p.cost[first + i] - base; }, n, z);
         c0 = (int32_t)(z - (p.cost[first + b] - base));
     }
     int4 cut = make_int4(0, 0, 0, 0);
+    bool padded = false;
 
     for (; left > 0; ++b, c0 = 0) {
         int2 span;
@@ -644,57 +659,9 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
         const int32_t first_tile = span.x / KT;
         if (span.y == 0) n = 0;   // (no keys: the rows are written all the same)
 
-        // the lane's row
-        const int32_t total_rows = x.n * p.group, row = b * M + wr * 32 + r;
-        const bool valid = row < total_rows;
-        const int32_t my = min(row, total_rows - 1), i = divide(my, p.group_mul, p.group_shift), h = my - i * p.group;
-        const int32_t t = x.start + i, head = kv * p.group + h;
-        const Range in = range_of(p, x, s, i);
-        const Scores sc = Scores::of(p, kv, p.slopes ? p.slopes[head] : 0.0f);
-        const uint32_t *mask = p.tree ? p.mask + t * p.mask_stride : nullptr;
-        Q q[QV];
-        {
-            const T *from = static_cast<const T *>(p.q) + t * p.q_row + head * p.q_head;
-#pragma unroll
-            for (int k = 0; k < QV; ++k) {
-                const int at = (2 * k + g) * (S::F32 ? 4 : 8);
-                const Q y = at < p.d ? *reinterpret_cast<const Q *>(from + at) : Q(0);
-                q[k] = p.scale < 0.0f ? -y : y;
-            }
-        }
-        __syncthreads();   // (the block before has been written, s_lo and s_hi read)
-        if (tid == 0) {
-            s_lo = 0;
-            s_hi = INT32_MAX;
-            s_note[0] = s_note[1] = 0;
-            s_odd = 0;
-        }
+        __syncthreads();   // (the block before has been written)
+        if (tid == 0) s_note[0] = s_note[1] = s_odd = 0;
         if (tid < KT / 32) s_bad[0][tid] = s_bad[1][tid] = 0;
-        __syncthreads();
-        int32_t wave_lo, wave_hi;   // none of the wave's rows attends to keys outside
-        {
-            int32_t lo = in.lo, hi = in.hi;   // all rows attend to the keys of [largest lo, least hi)
-            int32_t any_lo = in.lo < in.hi ? in.lo : INT32_MAX, any_hi = in.hi;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                lo = max(lo, __shfl_xor(lo, o));
-                hi = min(hi, __shfl_xor(hi, o));
-                any_lo = min(any_lo, __shfl_xor(any_lo, o));
-                any_hi = max(any_hi, __shfl_xor(any_hi, o));
-            }
-            if (lane == 0) {
-                atomicMax(&s_lo, lo);
-                atomicMin(&s_hi, hi);
-            }
-            wave_lo = uniform(any_lo);
-            wave_hi = uniform(any_hi);
-            if (p.tree) {
-                wave_lo = min(wave_lo, x.len);
-                wave_hi = x.keys;
-            }
-        }
-        __syncthreads();
-        const int32_t all_lo = uniform(s_lo), all_hi = uniform(s_hi);
         // Where the lane reads keys, row r of 32 and their piece g, and values,
         // transposed: elements 4 (lane % 4) on of 16 of rows 4 g + lane / 4 % 4.
         // (Pieces further on are reached by exclusive or: the tile begins at a
@@ -710,12 +677,20 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
         const int32_t last = t0 + n;
         u32x4 kx[S::DMA ? 1 : S::NQ], vx[S::DMA ? 1 : S::NQ];
         uint32_t bad_keys = 0;   // bit q: the page of piece q's key
+        int32_t pages[S::DMA ? 1 : S::NQ];
+        auto look = [&](int32_t k0) {   // (a tile ahead of the loads)
+#pragma unroll
+            for (int j = 0; j < (S::DMA ? 0 : S::NQ); ++j) {
+                const int32_t key = min(max(k0 + (j * S::BLOCK + tid) / S::IN, span.x), span.y - 1);
+                pages[j] = table[divide(key, p.page_mul, p.page_shift)];
+            }
+        };
         auto load = [&](int32_t k0) {
 #pragma unroll
             for (int j = 0; j < (S::DMA ? 0 : S::NQ); ++j) {
                 const int piece = j * S::BLOCK + tid, c = piece % S::IN;
                 const int32_t key = min(max(k0 + piece / S::IN, span.x), span.y - 1);
-                const int32_t of = divide(key, p.page_mul, p.page_shift), page = table[of];
+                const int32_t of = divide(key, p.page_mul, p.page_shift), page = pages[j];
                 const bool ok = page >= 0 && page < p.n_pages, used = c * (16 / (int)sizeof(CT)) < p.d;
                 bad_keys = (bad_keys & ~(1u << j)) | (uint32_t)!ok << j;
                 kx[j] = vx[j] = u32x4{0, 0, 0, 0};
@@ -840,15 +815,8 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
             if (lane == 0) s_waves[turn][wave] = bad;
         };
 
-        // Weights are held against m, a score that is at most kSlack base-2
-        // units below the row's largest: what is summed is scaled only where
-        // one above `limit` comes.
-        float m = -HUGE_VALF, limit = -HUGE_VALF, l = x.bad ? __builtin_nanf("") : 0.0f;
-        f32x16 o[OB];
-#pragma unroll
-        for (int e = 0; e < OB; ++e) o[e] = f32x16(0.0f);
-
-        if (S::DMA && p.d < DP) {   // what the padded rows' ends are multiplied as
+        if (S::DMA && p.d < DP && (WK > 1 || !padded)) {   // what the padded rows' ends are multiplied as
+            padded = true;
             for (int c = tid; c < S::TILES / 16; c += S::BLOCK) reinterpret_cast<u32x4 *>(s_buf)[c] = u32x4{0, 0, 0, 0};
             __syncthreads();
         }
@@ -858,9 +826,56 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                 send((first_tile + t0) * KT, t0 & 1);
                 fetch(t0 + 1);
             } else {
+                look((first_tile + t0) * KT);
                 load((first_tile + t0) * KT);
+                look((first_tile + t0 + 1) * KT);
             }
         }
+        // the lane's row
+        const int32_t total_rows = x.n * p.group, row = b * M + wr * 32 + r;
+        const bool valid = row < total_rows;
+        const int32_t my = min(row, total_rows - 1), i = divide(my, p.group_mul, p.group_shift), h = my - i * p.group;
+        const int32_t t = x.start + i, head = kv * p.group + h;
+        Q q[QV];
+        {
+            const T *from = static_cast<const T *>(p.q) + t * p.q_row + head * p.q_head;
+#pragma unroll
+            for (int k = 0; k < QV; ++k) {
+                const int at = (2 * k + g) * (S::F32 ? 4 : 8);
+                q[k] = at < p.d ? *reinterpret_cast<const Q *>(from + at) : Q(0);
+            }
+        }
+        const Range in = range_of(p, x, s, i);
+        const Scores sc = Scores::of(p, kv, p.slopes ? p.slopes[head] : 0.0f);
+        const uint32_t *mask = p.tree ? p.mask + t * p.mask_stride : nullptr;
+        // All rows attend to the keys of [largest lo, least hi), and none of the
+        // wave's to keys outside [wave_lo, wave_hi).
+        int32_t all_lo = across<true>(in.lo), all_hi = across<false>(in.hi);
+        int32_t wave_lo = across<false>(in.lo < in.hi ? in.lo : INT32_MAX), wave_hi = across<true>(in.hi);
+        if (lane == 0) s_range[wave] = make_int2(all_lo, all_hi);
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < S::WAVES; ++w) {
+            all_lo = max(all_lo, s_range[w].x);
+            all_hi = min(all_hi, s_range[w].y);
+        }
+        all_lo = uniform(all_lo);
+        all_hi = uniform(all_hi);
+        wave_lo = uniform(p.tree ? min(wave_lo, x.len) : wave_lo);
+        wave_hi = uniform(p.tree ? x.keys : wave_hi);
+        if (p.scale < 0.0f) {
+#pragma unroll
+            for (int k = 0; k < QV; ++k) q[k] = -q[k];
+        }
+
+        // Weights are held against m, a score that is at most kSlack base-2
+        // units below the row's largest: what is summed is scaled only where
+        // one above `limit` comes.
+        float m = -HUGE_VALF, limit = -HUGE_VALF, l = x.bad ? __builtin_nanf("") : 0.0f;
+        f32x16 o[OB];
+#pragma unroll
+        for (int e = 0; e < OB; ++e) o[e] = f32x16(0.0f);
+
         // (here, so that no tile waits for them: the wait would be for the next
         // tile's keys too)
 #pragma unroll
@@ -958,7 +973,10 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                         if (tid == 0) s_note[turn ^ 1] = 0;
                         if (tid < KT / 32) s_bad[turn ^ 1][tid] = 0;
                         __syncthreads();
-                        if (tile + 1 < last) load(k0 + KT);
+                        if (tile + 1 < last) {
+                            load(k0 + KT);
+                            look(k0 + 2 * KT);
+                        }
                         note = uniform((int32_t)s_note[turn]);
                     }
                 }

@@ -19,14 +19,15 @@ static int64_t blocks(int64_t n_tok, int32_t n_seq, int32_t group, int rows)
 }
 
 struct Layout {
-    size_t cost, span, first, cut, part, end;
+    size_t cost, span, first, base, cut, part, end;
     Layout(int64_t n_blocks, int32_t n_seq, int rows, int32_t d)
     {
         const auto up = [](size_t x) { return (x + 15) / 16 * 16; };
         cost = 0;
         span = up(cost + 8 * ((size_t)n_blocks + 1));
         first = up(span + 8 * (size_t)n_blocks);
-        cut = up(first + 4 * ((size_t)n_seq + 1));
+        base = up(first + 4 * ((size_t)n_seq + 1));
+        cut = up(base + 8 * ((size_t)n_seq + 1));
         part = cut + sizeof(int4) * kMaxGrid;
         end = part + (size_t)(rows == 256 ? kCus : kMaxGrid) * 2 * rows * (d + 2) * sizeof(float);
     }
@@ -91,6 +92,7 @@ dsim_status launch_rows(const RowsArgs &a, hipStream_t s)
     p.cost = reinterpret_cast<int64_t *>(ws + at.cost);
     p.span = reinterpret_cast<int2 *>(ws + at.span);
     p.first = reinterpret_cast<int32_t *>(ws + at.first);
+    p.base = reinterpret_cast<int64_t *>(ws + at.base);
     p.cut = reinterpret_cast<int4 *>(ws + at.cut);
     p.part = reinterpret_cast<float *>(ws + at.part);
     // ceil(2^(31 + l) / n), l = ceil(log2 n): exact for t < 2^31
@@ -103,7 +105,7 @@ dsim_status launch_rows(const RowsArgs &a, hipStream_t s)
     divisor(p.page_size, p.page_mul, p.page_shift);
     divisor(p.group, p.group_mul, p.group_shift);
     const int64_t most = (int64_t)p.table_width * p.page_size;
-    p.direct = most <= 1024;
+    p.direct = most <= 1024 && p.max_blocks * p.n_heads <= 2 * kMaxGrid;
     if (a.q.dtype == DSIM_F32) return rows::launch_f32(p, s);
     return (a.q.dtype == DSIM_F16 ? rows::launch_f16 : rows::launch_bf16)(p, a.c.dtype == DSIM_E4M3, s);
 }
