@@ -176,6 +176,20 @@ template <int THREADS> __device__ inline int64_t scan(int64_t x, int64_t *s, int
     return before + incl - x;
 }
 
+// Sum of x over the lanes up to this one.
+__device__ inline int32_t prefix(int32_t x)
+{
+#define DSIM_STEP(control, rows) x += __builtin_amdgcn_update_dpp(0, x, control, rows, 0xf, true)
+    DSIM_STEP(0x111, 0xf);   // within rows of 16, from 1, 2, 4 and 8 lanes before
+    DSIM_STEP(0x112, 0xf);
+    DSIM_STEP(0x114, 0xf);
+    DSIM_STEP(0x118, 0xf);
+    DSIM_STEP(0x142, 0xa);   // the last of a row to the next one
+    DSIM_STEP(0x143, 0xc);   // the last of the first half to the second
+#undef DSIM_STEP
+    return x;
+}
+
 // The largest i < n with a(i) <= x, where a does not descend and a(0) <= x:
 // 64 probes at a time, the same for all lanes.
 template <class A> __device__ inline int32_t find(A a, int32_t n, int64_t x)
@@ -572,29 +586,32 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
     int32_t c0 = 0;
     int64_t left = 1, run = 0;
     int32_t index = blockIdx.x;
+    Seq found{};
     if (p.direct) {
         // one block of one head: found among the sequences
         int32_t block = index / p.n_heads;
         kv = index - block * p.n_heads;
         for (s = 0; s < p.n_seq; s += 64) {
-            int32_t n = s + lane < p.n_seq ? blocks_of(p, seq_of(p, s + lane)) : 0, incl = n;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int32_t y = __shfl_up(incl, o);
-                if (lane >= o) incl += y;
-            }
+            Seq mine{};
+            if (s + lane < p.n_seq) mine = seq_of(p, s + lane);
+            const int32_t n = blocks_of(p, mine), incl = prefix(n);
             const uint64_t behind = __builtin_amdgcn_ballot_w64(block < incl);
             if (behind) {
                 const int at = __builtin_ctzll(behind);
-                block -= __shfl(incl - n, at);
+                block -= __builtin_amdgcn_readlane(incl - n, at);
+                found.start = __builtin_amdgcn_readlane(mine.start, at);
+                found.n = __builtin_amdgcn_readlane(mine.n, at);
+                found.len = __builtin_amdgcn_readlane(mine.len, at);
+                found.keys = __builtin_amdgcn_readlane(mine.keys, at);
+                found.bad = __builtin_amdgcn_readlane(mine.bad, at);
                 s += at;
                 break;
             }
-            block -= __shfl(incl, 63);
+            block -= __builtin_amdgcn_readlane(incl, 63);
         }
         if (s >= p.n_seq) return;
-        s = __builtin_amdgcn_readfirstlane(s);
-        b = __builtin_amdgcn_readfirstlane(block);
+        s = uniform(s);
+        b = uniform(block);
     } else {
         // neighbouring runs on one XCD
         index = (index & 7) * (gridDim.x / 8) + (index >> 3);
@@ -623,7 +640,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
         int32_t t0 = 0, n = 0, tiles = 0;
         if (p.direct) {
             left = 0;
-            x = seq_of(p, s);
+            x = found;
             const int32_t r0 = b * M, r1 = min(r0 + M, x.n * p.group);
             span = span_of(p, x, s, r0 / p.group, (r1 - 1) / p.group, lane, 64);
             if (p.first_key) {
@@ -957,13 +974,19 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                         for (int w = 0; w < S::WAVES; ++w) without |= s_waves[turn][w];
                         note = 0;
                         if (any) {   // (see store)
-                            for (int c = tid; c < S::TILE / 16; c += S::BLOCK) {
-                                u32x4 *const at = reinterpret_cast<u32x4 *>(s_buf + now + S::TILE + c * 16);
-                                u32x4 v = *at;
-                                if (S::value_piece(c / S::NC, c % S::NC) * (16 / (int)sizeof(T)) < p.d && clean<T>(v)) {
-                                    *at = v;
-                                    s_odd = 1;
-                                }
+                            u32x4 *const v = reinterpret_cast<u32x4 *>(s_buf + now + S::TILE) + tid;
+                            constexpr int kPieces = S::TILE / 16 / S::BLOCK;
+#pragma unroll
+                            for (int c0 = 0; c0 < kPieces; c0 += 4) {
+                                u32x4 y[4];
+#pragma unroll
+                                for (int c = 0; c < 4 && c0 + c < kPieces; ++c) y[c] = v[(c0 + c) * S::BLOCK];
+#pragma unroll
+                                for (int c = 0; c < 4 && c0 + c < kPieces; ++c)   // (padding is 0)
+                                    if (clean<T>(y[c])) {
+                                        v[(c0 + c) * S::BLOCK] = y[c];
+                                        s_odd = 1;
+                                    }
                             }
                             __syncthreads();
                         }
@@ -1101,8 +1124,13 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                     const auto y = halves(top);
                     top = fmaxf(y[0], y[1]);
                 }
-                // (once a tile: whatever the scores, every loop ends)
-                if ((fresh && __builtin_amdgcn_ballot_w64(top > limit) != 0)) break;
+                if (__builtin_amdgcn_ballot_w64(top > limit) != 0) {
+                    // (once a tile: whatever the scores, every loop ends)
+                    if (fresh && __builtin_amdgcn_ballot_w64(top > limit && m != -HUGE_VALF) != 0) break;
+                    // rows that had none: nothing to scale
+                    m = m == -HUGE_VALF ? top : m;
+                    limit = m == -HUGE_VALF ? m : m + S::SLACK / sc.unit;
+                }
                 // outputs (rows) of the rows (columns); the first values come
                 // while the weights are computed
                 if constexpr (S::F32) {
@@ -1167,24 +1195,28 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
             l *= f;
             m = top;
             if (g == 0) s_l[wave][r] = l;
-            float *sums = reinterpret_cast<float *>(s_buf) + (wr * (WK - 1) + wk - 1) * (1024 * OB) + lane;
+            f32x4 *const sums = reinterpret_cast<f32x4 *>(s_buf) + wr * (WK - 1) * (256 * OB) + lane;
 #pragma unroll
             for (int e = 0; e < OB; ++e) {
                 o[e] *= f;
                 if (wk > 0)
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) sums[(16 * e + k) * 64] = o[e][k];
+                    for (int k = 0; k < 4; ++k)
+                        sums[(wk - 1) * (256 * OB) + (4 * e + k) * 64] = f32x4{o[e][4 * k], o[e][4 * k + 1], o[e][4 * k + 2], o[e][4 * k + 3]};
             }
             __syncthreads();
             if (wk == 0) {
 #pragma unroll
                 for (int w = 1; w < WK; ++w) {
                     l += s_l[wr * WK + w][r];
-                    const float *from = reinterpret_cast<const float *>(s_buf) + (wr * (WK - 1) + w - 1) * (1024 * OB) + lane;
 #pragma unroll
                     for (int e = 0; e < OB; ++e)
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) o[e][k] += from[(16 * e + k) * 64];
+                        for (int k = 0; k < 4; ++k) {
+                            const f32x4 y = sums[(w - 1) * (256 * OB) + (4 * e + k) * 64];
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) o[e][4 * k + c] += y[c];
+                        }
                 }
             }
         }
@@ -1332,7 +1364,7 @@ template <class T, class CT, int DP> dsim_status launch(Params &p, hipStream_t s
     if constexpr (DP <= 128)
         if (p.rows == 32) return launch<T, CT, DP, 1>(p, s);
     if (p.rows == 64) return launch<T, CT, DP, 2>(p, s);
-    if constexpr (DP <= 128)
+    if constexpr (DP <= 128 && sizeof(T) == 2)
         if (p.rows == 256) return launch<T, CT, DP, 8>(p, s);
     return launch<T, CT, DP, 4>(p, s);
 }

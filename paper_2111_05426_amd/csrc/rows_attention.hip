@@ -7,10 +7,12 @@ namespace dsim {
 namespace rows {
 
 // Rows of a block: no more than the average sequence has.
-static int rows_of(int64_t n_tok, int32_t n_seq, int32_t group, int32_t head_dim)
+static int rows_of(int64_t n_tok, int32_t n_seq, int32_t group, int32_t head_dim, bool f32)
 {
     const int64_t average = n_seq > 0 ? (n_tok * group + n_seq - 1) / n_seq : 0;
-    return average <= 32 && head_dim <= 128 ? 32 : average <= 64 ? 64 : average <= 512 || head_dim > 128 ? 128 : 256;
+    if (average <= 32 && head_dim <= 128) return 32;
+    if (average <= 64) return 64;
+    return average <= 512 || head_dim > 128 || f32 ? 128 : 256;
 }
 
 static int64_t blocks(int64_t n_tok, int32_t n_seq, int32_t group, int rows)
@@ -38,8 +40,13 @@ struct Layout {
 size_t rows_workspace(int64_t n_tok, int32_t n_seq, int32_t n_q_heads, int32_t n_heads, int32_t head_dim)
 {
     const int32_t group = n_q_heads / n_heads;
-    const int rows = rows::rows_of(n_tok, n_seq, group, head_dim);
-    return rows::Layout(rows::blocks(n_tok, n_seq, group, rows), n_seq, rows, head_dim).end;
+    size_t most = 0;
+    for (const bool f32 : {false, true}) {   // (whatever the type)
+        const int rows = rows::rows_of(n_tok, n_seq, group, head_dim, f32);
+        const size_t bytes = rows::Layout(rows::blocks(n_tok, n_seq, group, rows), n_seq, rows, head_dim).end;
+        if (bytes > most) most = bytes;
+    }
+    return most;
 }
 
 dsim_status launch_rows(const RowsArgs &a, hipStream_t s)
@@ -84,7 +91,7 @@ dsim_status launch_rows(const RowsArgs &a, hipStream_t s)
     p.table_width = a.c.table_width;
     p.window = a.q.window;
     p.group = a.q.n_q_heads / a.c.n_heads;
-    p.rows = rows_of(p.n_tok, p.n_seq, p.group, p.d);
+    p.rows = rows_of(p.n_tok, p.n_seq, p.group, p.d, a.q.dtype == DSIM_F32);
     p.max_blocks = blocks(p.n_tok, p.n_seq, p.group, p.rows);
     p.tree = a.tree;
     const Layout at(p.max_blocks, p.n_seq, p.rows, p.d);
