@@ -1181,21 +1181,22 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
         }
 
         // the halves' sums, and the waves that share the rows
+        const uint32_t mine = again(lane), r_ = mine & 31, g_ = mine >> 5;
         {
             const auto y = halves(l);
             l = y[0] + y[1];
         }
         if constexpr (WK > 1) {
-            if (g == 0) s_m[wave][r] = m;
+            if (g_ == 0) s_m[wave][r_] = m;
             __syncthreads();   // (and the last tile has been read)
             float top = m;
 #pragma unroll
-            for (int w = 0; w < WK; ++w) top = fmaxf(top, s_m[wr * WK + w][r]);
+            for (int w = 0; w < WK; ++w) top = fmaxf(top, s_m[wr * WK + w][r_]);
             const float f = rescale(m, top, sc.unit);
             l *= f;
             m = top;
-            if (g == 0) s_l[wave][r] = l;
-            f32x4 *const sums = reinterpret_cast<f32x4 *>(s_buf) + wr * (WK - 1) * (256 * OB) + lane;
+            if (g_ == 0) s_l[wave][r_] = l;
+            f32x4 *const sums = reinterpret_cast<f32x4 *>(s_buf) + wr * (WK - 1) * (256 * OB) + mine;
 #pragma unroll
             for (int e = 0; e < OB; ++e) {
                 o[e] *= f;
@@ -1208,7 +1209,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
             if (wk == 0) {
 #pragma unroll
                 for (int w = 1; w < WK; ++w) {
-                    l += s_l[wr * WK + w][r];
+                    l += s_l[wr * WK + w][r_];
 #pragma unroll
                     for (int e = 0; e < OB; ++e)
 #pragma unroll
@@ -1224,12 +1225,12 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
         if (wk == 0 && valid) {
             const float vs = (p.v_scale ? p.v_scale[kv] : 1.0f) * (whole ? share_of(l) : 1.0f);
             const Part part = Part::of(p, 2 * index + (t0 == 0 ? 1 : 0));
-            const int at = wr * 32 + r;
+            const int at = wr * 32 + r_;
 #pragma unroll
             for (int e = 0; e < OB; ++e)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const int d = 32 * e + 8 * k + 4 * g;
+                    const int d = 32 * e + 8 * k + 4 * g_;
                     if (d >= p.d) continue;
                     const f32x4 y = f32x4{o[e][4 * k], o[e][4 * k + 1], o[e][4 * k + 2], o[e][4 * k + 3]} * vs;
                     if (whole)
@@ -1237,7 +1238,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                     else
                         *reinterpret_cast<f32x4 *>(part.o + at * p.d + d) = y;
                 }
-            if (g == 0) {
+            if (g_ == 0) {
                 if (whole) {
                     write_lse(p, t, head, m, sc.unit, l, S::UP);
                 } else {
