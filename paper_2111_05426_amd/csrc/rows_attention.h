@@ -17,7 +17,7 @@ constexpr int kJoin = 256;           // threads of the join
 constexpr int kPlan = 1024;          // threads of the plan
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // What a block of rows costs beside its tiles, in tiles.
-constexpr int kExtra = 4;
+constexpr int extra(int rows) { return rows >= 128 ? 2 : 4; }
 constexpr int kMinTiles = 4;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -43,7 +43,7 @@ struct Params {
     float scale, cap;     // scale: natural units
     int32_t n_seq, n_heads, d, page_size, table_width, window, mask_words;
     int32_t group, n_q_heads, rows;   // rows of a block
-    bool tree, direct;
+    bool tree, direct, short_cap;
     uint32_t page_mul, page_shift, group_mul, group_shift;   // t / n = t * mul >> shift, 0 <= t < 2^31
 };
 
@@ -262,7 +262,7 @@ template <int KT> __global__ __launch_bounds__(kPlan) void k_plan(Params p)
     before = 0;
     for (int32_t b0 = 0; b0 < n; b0 += kPlan) {
         const int32_t b = b0 + threadIdx.x;
-        const int64_t cost = b < n ? tiles_of<KT>(p.span[b]) + kExtra : 0;
+        const int64_t cost = b < n ? tiles_of<KT>(p.span[b]) + extra(p.rows) : 0;
         const int64_t at = before + scan<kPlan>(cost, s_sum, total);
         if (b < n) p.cost[b] = at;
         before += total;
@@ -343,22 +343,11 @@ template <bool F32> __device__ inline float tanh_of(float y)
     }
 }
 
-// Scores over the cap become capped ones in base-2 units (cap2).  Where weights
-// are rounded to T's bits before the second product, a cap of at most 128
-// takes tanh as 1 - 2 / (exp(2 y) + 1), off by at most 2^-21 of 1: 2^-14 of a
-// weight.
-template <bool F32, bool EXACT> __device__ inline void cap_of(f32x16 &x, float cap, float cap2)
+// Scores over the cap become capped ones in base-2 units (cap2).
+template <bool F32> __device__ inline void cap_of(f32x16 &x, float cap2)
 {
-    if (!EXACT && cap <= 128.0f) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const float y = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[e] * (2.0f * kLog2e)) + 1.0f);
-            x[e] = __builtin_fmaf(y, -2.0f * cap2, cap2);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = tanh_of<F32>(x[e]) * cap2;
-    }
+    for (int e = 0; e < 16; ++e) x[e] = tanh_of<F32>(x[e]) * cap2;
 }
 
 // Sums held against the maximum `from`, against `to`: see paged_attention.h.
@@ -539,26 +528,31 @@ __device__ inline void write_row(const Params &p, int64_t t, int head, int d, f3
 // the sum 0, one that attends to a bad page NaN.)
 __device__ inline float share_of(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 
-__device__ inline void write_lse(const Params &p, int64_t t, int head, float m, float scale, float l, float up)
+__device__ inline void write_lse(const Params &p, int64_t t, int head, float m, float unit, float offset, float l, float up)
 {
-    if (p.lse) p.lse[t * p.n_q_heads + head] = l == 0.0f ? -HUGE_VALF : (m * scale + (__builtin_log2f(l) - up)) * kLn2;
+    if (p.lse)
+        p.lse[t * p.n_q_heads + head] = l == 0.0f ? -HUGE_VALF : (m * unit + offset + (__builtin_log2f(l) - up)) * kLn2;
 }
 
-// The scores' way from a product with a cache head's keys (times the sign of
-// the scale) to a base-2 exponent.
+// The scores' way from a product x with a cache head's keys (times the sign of
+// the scale) to a base-2 exponent, unit * score + offset.  Without cap and
+// slopes a score is the product itself; with a cap alone where cap_of's short
+// form will do, cap tanh(y) = cap - 2 cap / (exp(2 y) + 1), it is -1 / (exp(2 y)
+// + 1); else the exponent.
 struct Scores {
     float in, cap, slope;   // slope: of the row; all in base-2 units
-    float unit;             // base-2 units of what is kept as score
-    bool raw;               // scores are products
+    float unit, offset;
+    bool raw;
     __device__ static Scores of(const Params &p, int kv, float slope)
     {
         Scores s;
         const float scale = fabsf(p.scale) * (p.k_scale ? p.k_scale[kv] : 1.0f);
         s.raw = p.cap == 0.0f && !p.slopes;
-        s.in = p.cap > 0.0f ? scale / p.cap : scale * kLog2e;
         s.cap = p.cap * kLog2e;
+        s.in = p.short_cap ? scale / p.cap * (2.0f * kLog2e) : p.cap > 0.0f ? scale / p.cap : scale * kLog2e;
         s.slope = slope * kLog2e;
-        s.unit = s.raw ? s.in : 1.0f;
+        s.unit = s.raw ? s.in : p.short_cap ? 2.0f * s.cap : 1.0f;
+        s.offset = p.short_cap ? s.cap : 0.0f;
         return s;
     }
 };
@@ -664,10 +658,10 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
             x = seq_of(p, s);
             span = p.span[p.first[s] + b];
             tiles = tiles_of<KT>(span);
-            const int32_t cost = tiles + kExtra, c1 = (int32_t)(cost - c0 < left ? cost : c0 + left);
+            const int32_t cost = tiles + extra(M), c1 = (int32_t)(cost - c0 < left ? cost : c0 + left);
             left -= c1 - c0;
-            t0 = max(c0 - kExtra, 0);
-            n = max(c1 - kExtra, 0) - t0;
+            t0 = max(c0 - extra(M), 0);
+            n = max(c1 - extra(M), 0) - t0;
             if (n == 0) continue;   // the next run begins the block
         }
         t0 = uniform(t0);
@@ -1052,8 +1046,14 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
                         const int32_t kw = k0 + wk * S::KW + 32 * u;
+                        if (a.short_cap) {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                sx[u][e] = -__builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(sx[u][e] * sc.in) + 1.0f);
+                            continue;
+                        }
                         sx[u] *= sc.in;
-                        if (a.cap > 0.0f) cap_of<S::F32, S::F32 || S::SPLIT>(sx[u], a.cap, sc.cap);
+                        if (a.cap > 0.0f) cap_of<S::F32>(sx[u], sc.cap);
                         if (a.slopes) {
                             if (a.tree && kw + 32 > x.len) {
 #pragma unroll 1
@@ -1240,7 +1240,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                 }
             if (g_ == 0) {
                 if (whole) {
-                    write_lse(p, t, head, m, sc.unit, l, S::UP);
+                    write_lse(p, t, head, m, sc.unit, sc.offset, l, S::UP);
                 } else {
                     part.m[at] = m;
                     part.l[at] = l;
@@ -1311,7 +1311,7 @@ template <class T> __global__ __launch_bounds__(kJoin) void k_join(Params p, flo
             for (int w = 1; w < kWays; ++w) l += s_l[w][at];
             s_l[0][at] = l;
             const int32_t row = cut.w * p.rows + first + at, i = divide(row, p.group_mul, p.group_shift);
-            if (row < total_rows) write_lse(p, start + i, kv * p.group + row - i * p.group, m, sc.unit, l, up);
+            if (row < total_rows) write_lse(p, start + i, kv * p.group + row - i * p.group, m, sc.unit, sc.offset, l, up);
         }
         __syncthreads();
     }
