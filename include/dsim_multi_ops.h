@@ -66,7 +66,8 @@ DSIM_API dsim_status dsim_kv_append_axes(const dsim_kv_cache *cache, int64_t n_t
  *   x = x - slopes[h] * |p - j|, if there are slopes;
  *   o = sum_j exp(x_j) v_j / sum_j exp(x_j),   lse = log sum_j exp(x_j)
  * A token that attends to nothing has o = 0 and lse = -inf; keys that it does
- * not attend to weigh nothing whatever they hold.  Scores, statistics and
+ * not attend to weigh nothing whatever they hold, and an attended value that is
+ * not finite makes its element of o infinite or NaN.  Scores, statistics and
  * sums are fp32; the result is rounded once to out's type.
  *   q, out: n_tok rows of n_q_heads heads of `dtype`: the cache's type, or
  *           DSIM_F16 / DSIM_BF16 with an e4m3 cache; out may be q (with its
@@ -83,7 +84,7 @@ DSIM_API dsim_status dsim_kv_append_axes(const dsim_kv_cache *cache, int64_t n_t
  *   workspace: device buffer of at least dsim_prompt_attention_workspace(...)
  *           bytes, 16-byte aligned, in use until hip_stream has passed the
  *           call; it needs no clearing and keeps nothing for later calls.
- * n_tok * n_q_heads < 2^31, n_seq <= 2^20.
+ * n_tok * n_q_heads <= 2^31 - 256, n_seq <= 2^20.
  */
 typedef struct {
     dsim_rows q, out;
@@ -224,7 +225,8 @@ DSIM_API dsim_status dsim_kv_copy_pages(const dsim_kv_cache *layers, int32_t n_l
 /*
  * dsim_kv_compact -- of sequence s the places start[s] + keep[s][j], j <
  * n_keep[s], move to start[s] + j in every layer, as if all were read before
- * any is written.  keep[s] must ascend (from 0 or more); it ends before the
+ * any is written.  The pages that are written to must be held by one row of
+ * the table only, and once.  keep[s] must ascend (from 0 or more); it ends before the
  * first entry that does not.  What was behind the last of them stays as it is.
  *   layers:  as above, with layers[0]'s block table and n_seq
  *   keep:    device array [n_seq][keep_stride], keep_width entries that may

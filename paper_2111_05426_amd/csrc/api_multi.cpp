@@ -10,6 +10,7 @@
 namespace dsim {
 
 constexpr int kMaxCaches = 1024;
+constexpr int64_t kMaxRows = INT32_MAX - 255;   // blocks of up to 256 rows end in 32 bits
 
 static dsim_status check_queries(const dsim_kv_cache *c, const dsim_queries *q)
 {
@@ -19,8 +20,8 @@ static dsim_status check_queries(const dsim_kv_cache *c, const dsim_queries *q)
     if ((st = check_dtype(q->dtype, c))) return st;
     if (q->n_q_heads < 1 || q->n_q_heads > kMaxHeads || q->n_q_heads % c->n_heads)
         return fail(DSIM_ERANGE, "n_q_heads must be a multiple of n_heads (%d) and at most %d", c->n_heads, kMaxHeads);
-    if (q->n_tok < 0 || q->n_tok > INT32_MAX || q->n_tok * q->n_q_heads > INT32_MAX)
-        return fail(DSIM_ERANGE, "n_tok must be >= 0 and n_tok * n_q_heads below 2^31");
+    if (q->n_tok < 0 || q->n_tok > kMaxRows || q->n_tok * q->n_q_heads > kMaxRows)
+        return fail(DSIM_ERANGE, "n_tok must be >= 0 and n_tok * n_q_heads at most 2^31 - 256");
     if (!(std::fabs(q->scale) <= 0x1p126f)) return fail(DSIM_EINVAL, "scale must be in [-2^126, 2^126]");
     if (q->cap != 0.0f && !(q->cap >= 0x1p-60f && q->cap <= 0x1p60f)) return fail(DSIM_EINVAL, "cap must be 0 or in [2^-60, 2^60]");
     if (q->window < 0) return fail(DSIM_EINVAL, "window must be >= 0");
@@ -136,7 +137,7 @@ dsim_status dsim_kv_append_axes(const dsim_kv_cache *cache, int64_t n_tok, int32
 size_t dsim_prompt_attention_workspace(int64_t n_tok, int32_t n_seq, int32_t n_q_heads, int32_t n_heads, int32_t head_dim)
 {
     if (n_heads < 1 || n_q_heads < n_heads || n_q_heads > kMaxHeads || n_q_heads % n_heads || head_dim < 16 ||
-        head_dim > kMaxHeadDim || head_dim % 16 || n_tok < 0 || n_tok > INT32_MAX || n_tok * n_q_heads > INT32_MAX ||
+        head_dim > kMaxHeadDim || head_dim % 16 || n_tok < 0 || n_tok > kMaxRows || n_tok * n_q_heads > kMaxRows ||
         n_seq < 0 || n_seq > (1 << 20))
         return 0;
     return rows_workspace(n_tok, n_seq, n_q_heads, n_heads, head_dim);

@@ -93,7 +93,9 @@ template <int BLOCK> __global__ __launch_bounds__(BLOCK) void k_compact(Layers l
         // the next one reads is not written here, so nobody waits for stores.
 #pragma unroll
         for (int i = 0; i < kRows; ++i) asm volatile("" : "+v"(x[i]));
+        asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
 #pragma unroll
         for (int i = 0; i < kRows; ++i)
             if (now[i] >= 0) base[now[i]] = x[i];

@@ -534,19 +534,20 @@ __device__ inline void write_lse(const Params &p, int64_t t, int head, float m, 
         p.lse[t * p.n_q_heads + head] = l == 0.0f ? -HUGE_VALF : (m * unit + offset + (__builtin_log2f(l) - up)) * kLn2;
 }
 
-// The scores' way from a product x with a cache head's keys (times the sign of
-// the scale) to a base-2 exponent, unit * score + offset.  Without cap and
+// The scores' way from a product x with a cache head's keys (times the scales'
+// sign) to a base-2 exponent, unit * score + offset.  Without cap and
 // slopes a score is the product itself; with a cap alone where cap_of's short
 // form will do, cap tanh(y) = cap - 2 cap / (exp(2 y) + 1), it is -1 / (exp(2 y)
 // + 1); else the exponent.
 struct Scores {
     float in, cap, slope;   // slope: of the row; all in base-2 units
     float unit, offset;
-    bool raw;
+    bool raw, negative;
     __device__ static Scores of(const Params &p, int kv, float slope)
     {
         Scores s;
-        const float scale = fabsf(p.scale) * (p.k_scale ? p.k_scale[kv] : 1.0f);
+        const float signed_ = p.scale * (p.k_scale ? p.k_scale[kv] : 1.0f), scale = fabsf(signed_);
+        s.negative = signed_ < 0.0f;
         s.raw = p.cap == 0.0f && !p.slopes;
         s.cap = p.cap * kLog2e;
         s.in = p.short_cap ? scale / p.cap * (2.0f * kLog2e) : p.cap > 0.0f ? scale / p.cap : scale * kLog2e;
@@ -874,7 +875,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
         all_hi = uniform(all_hi);
         wave_lo = uniform(p.tree ? min(wave_lo, x.len) : wave_lo);
         wave_hi = uniform(p.tree ? x.keys : wave_hi);
-        if (p.scale < 0.0f) {
+        if (sc.negative) {
 #pragma unroll
             for (int k = 0; k < QV; ++k) q[k] = -q[k];
         }
@@ -1261,14 +1262,15 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                     if (page < 0 || page >= p.n_pages || tid >= p.d) continue;
                     const float v = value_of(vb[page * p.page_stride + (key - of * p.page_size) * p.slot_stride + tid]);
                     if (fabsf(v) < HUGE_VALF) continue;
+                    const float y = v * (p.v_scale ? p.v_scale[kv] : 1.0f);
                     for (int at = 0; at < M && b * M + at < total_rows; ++at) {
                         const int32_t i = (b * M + at) / p.group, h = b * M + at - i * p.group;
                         if (!attends(p, x, s, i, key)) continue;
                         if (whole) {
                             T *const to = static_cast<T *>(p.out) + (x.start + i) * p.out_row + (kv * p.group + h) * p.out_head + tid;
-                            *to = (T)((float)*to + v);
+                            *to = (T)((float)*to + y);
                         } else {
-                            part.o[at * p.d + tid] += v;
+                            part.o[at * p.d + tid] += y;
                         }
                     }
                 }

@@ -31,11 +31,12 @@ def ints(x):
 def weights_off(dtype, tokens, n_seq, group):
     """What a weight may be off before the second product: fp32's bits, two
     numbers of the type for few rows, one for many; and below what part of the
-    largest weight it is lost."""
+    largest weight it is lost (fp16 rounds to multiples of 2^-24, off by 2^-25,
+    and the weight of the score that others are held against is 2^11)."""
     if dtype == F32:
         return 0.0, 0.0
     few = tokens * group <= 64 * n_seq
-    return (HALF[dtype] ** 2 if few else HALF[dtype]), (2.0 ** -39 if dtype == F16 else 0.0)
+    return (HALF[dtype] ** 2 if few else HALF[dtype]), (2.0 ** -36 if dtype == F16 else 0.0)
 
 
 def random_tree(g, n):
