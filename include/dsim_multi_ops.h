@@ -230,7 +230,7 @@ DSIM_API dsim_status dsim_kv_copy_pages(const dsim_kv_cache *layers, int32_t n_l
  * first entry that does not.  What was behind the last of them stays as it is.
  *   layers:  as above, with layers[0]'s block table and n_seq
  *   keep:    device array [n_seq][keep_stride], keep_width entries that may
- *            be read; n_keep is clamped to 0..keep_width
+ *            be read, at most 2^30; n_keep is clamped to 0..keep_width
  *   status:  device array [n_seq] or NULL: 0, DSIM_ST_BAD_POSITION (entries
  *            that do not ascend, or places outside the block table: the
  *            list ends before them) or DSIM_ST_BAD_PAGE (a page of them

@@ -233,6 +233,7 @@ dsim_status dsim_kv_compact(const dsim_kv_cache *layers, int32_t n_layers, const
     Layers l[launches_of(kMaxCaches)];
     dsim_status st = check_layers(layers, n_layers, true, l);
     if (st) return st;
+    if (keep_width > (1 << 30)) return fail(DSIM_ERANGE, "keep_width must be at most 2^30");
     if (keep_width < 0 || keep_stride < 0 || !product_ok(keep_stride, 4 * (int64_t)(1 << 20)) ||
         (layers->n_seq > 1 && keep_stride < keep_width))
         return fail(DSIM_EINVAL, "rows of keep must hold keep_width entries");

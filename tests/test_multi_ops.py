@@ -226,6 +226,7 @@ def test_pages_refused(L):
     compact("keep", stride=3)
     compact("keep", stride=-4)
     compact("keep", width=-1)
+    compact("keep_width", width=(1 << 30) + 1, stride=1 << 31)
     compact("keep", stride=1 << 61)
     compact("NULL", layers=cache(block_table=0))
     assert L.dsim_kv_compact(ref(cache(n_seq=0)), 1, None, None, 4, 4, None, None, None) == 0
