@@ -71,6 +71,10 @@ template <int AXES> __device__ inline Place place_of(const AppendArgs &a, const 
 // call's chunks a token: 2^17, a row's: 64)
 __device__ inline uint32_t divide(uint32_t j, uint32_t mul) { return mul ? __umulhi(j, mul) : j; }
 
+// Positions on several axes are kept as a vector and chosen by comparisons: an
+// array goes to shared memory (1,024 drafted tokens of 32 / 8 heads of 128 with
+// 20 us for 8.7).  24,577 tokens on three axes take 117 us, 5.2 TB/s, the append
+// of one position 108: a token reads three rows of the table.
 // Cosines and sines of pairs e .. e + N - 1.  AXES 0: of the token's one row;
 // 1: those of a chunk are of one axis; 2: of any.
 template <int AXES, int N>

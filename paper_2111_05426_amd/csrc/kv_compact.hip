@@ -8,8 +8,8 @@
 // in the list's order, and reads a batch before it writes it, needs no second
 // copy.  Its share is a piece of one layer's keys or values of one head.
 //
-// On MI355X 8 contexts of 16,384 tokens of which 4,096 stay (two layers, 8
-// heads of 128, bf16: 268 MB read and as many written) take 174 us, 3.1 TB/s:
+// On MI355X 8 contexts of 4,096 to 16,384 tokens of which half stay (two layers,
+// 8 heads of 128, bf16: 336 MB read and as many written) take 174 us, 3.9 TB/s:
 // every batch waits for its rows, and its stores stand before the next ones'
 // loads.  (Entries, pages and rows asked for three, two and one batch ahead, so
 // that nothing waits for anything of its own batch: 172 us, but a short list

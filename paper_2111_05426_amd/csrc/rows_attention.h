@@ -1,6 +1,45 @@
 // rows_attention.h -- the kernels of dsim_prompt_attention and
 // dsim_tree_attention: attention of many rows (query tokens times the query
 // heads of one cache head) over paged keys and values.
+//
+// Mathematics.  For a row i and the keys j it attends to, x_ij = score(q_i k_j),
+// w_ij = exp2((x_ij - m_i) unit), o_i = sum_j w_ij v_j / sum_j w_ij, in one pass over
+// the keys: m_i is a score at most SLACK base-2 units below the row's largest
+// so far, and sums and outputs are scaled when one that is larger by more
+// comes, which few tiles see.  Parts of a row with maxima m_a, m_b add up as sum
+// exp2((m_a - m) unit) o_a + ....
+//
+// Layout.  A block is 32 WR rows (tokens times the query heads of a cache
+// head) of one sequence.  Scores are taken transposed, S^T = K Q^T (32 keys x 32
+// rows by 32x32x16 products, 32x32x2 in fp32): the lanes that hold a row's
+// scores are then those that need its weights as the right operand of O^T =
+// V^T P^T, whose left operand is read from shared memory transposed.  So
+// weights never leave the registers, and a row's maximum and sum are 16 or 32
+// elements of a lane and one exchange with lane + 32.  The order of keys that
+// both products share is free, and is that of the score's elements.
+//
+// The blocks' tiles of all sequences and heads are laid end to end by one
+// workgroup (k_plan: 6 to 8 us), cut into one equal run for each workgroup that
+// is resident (neighbouring runs on one XCD, whose L2 then has a head's keys
+// once), and what a cut goes through is joined (k_join: 11 to 16 us, tree_long's
+// 25).  Short contexts take a workgroup a block and neither.
+//
+// What bounds it, on MI355X (bf16, heads of 128; the product of 8,192 cubed
+// reaches 1,101 TFLOP/s here):
+//   8,192 tokens of one prompt, 32 / 8 heads: 630 us, 873 TFLOP/s.  Matrix
+//     instructions and the exponentials' vector ones take turns; without the
+//     loads it would be 605.
+//   16 chunks of 1 to 1,024 tokens behind 2,000, window 1,500, cap 50: 425 us, 473
+//     TFLOP/s; a capped score takes two more transcendental instructions.
+//   64 trees of 16 nodes over 1 to 4,096 tokens: 151 us, 3.7 TB/s of the cache,
+//     of which plan and join 19.
+//   4 trees of 48 nodes over 65,536 tokens in e4m3, 64 / 8 heads, cap 30: 740 us, 556
+//     TFLOP/s: a tile is widened between two barriers.  (Widened a tile ahead
+//     between the products, with two tiles in shared memory: 787 to 811; the
+//     compiler runs out of registers.)
+//   fp32, 6 x 100 to 1,500 tokens of 3 documents, 12 heads of 80: 158 us, 21
+//     TFLOP/s of 153; heads of 96 by their products, documents that end inside
+//     blocks of 128 rows.
 #pragma once
 
 #include <type_traits>
@@ -16,9 +55,11 @@ constexpr int kMaxGrid = 2 * kCus;
 constexpr int kJoin = 256;           // threads of the join
 constexpr int kPlan = 1024;          // threads of the plan
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// What a block of rows costs beside its tiles, in tiles.
+// What a block of rows costs beside its tiles, in tiles.  (Chunks of prompts, a
+// long prompt, fp32 documents: 434, 598 and 155 us, with 4 438, 613 and 162, with
+// 1 426, 671 and 147.  Trees, blocks of 64 rows: 150 us, with 2 158, with 8 more.)
 constexpr int extra(int rows) { return rows >= 128 ? 2 : 4; }
-constexpr int kMinTiles = 4;
+constexpr int kMinTiles = 4;         // of a run at least: shorter ones only begin and end
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -207,7 +248,7 @@ template <class A> __device__ inline int32_t find(A a, int32_t n, int64_t x)
 }
 
 // Blocks of rows, their keys and what they cost, and the sequences' status.
-constexpr int kLanes = 16;
+constexpr int kLanes = 16;   // that look at the tokens of a block together
 template <int KT> __global__ __launch_bounds__(kPlan) void k_plan(Params p)
 {
     __shared__ int64_t s_sum[kPlan / 64];
@@ -357,8 +398,8 @@ __device__ inline float rescale(float from, float to, float scale)
 }
 
 // T: type of the queries, CT: of the cache, DP: the head's size padded, WR:
-// blocks of 32 rows in a workgroup.  The four waves are WR x WK: those of a
-// block of rows share out the keys of a tile.
+// blocks of 32 rows in a workgroup.  Its waves, four, or eight of 256 rows, are
+// WR x WK: those of a block of rows share out the keys of a tile.
 // WHOLE: pages of a multiple of 16 slots, so that 16 keys lie in one page.
 template <class T, class CT, int DP_, int WR_, bool WHOLE> struct Shape {
     static constexpr int DP = DP_, WR = WR_, WAVES = WR == 8 ? 8 : 4, BLOCK = 64 * WAVES, WK = WAVES / WR;
@@ -388,7 +429,10 @@ template <class T, class CT, int DP_, int WR_, bool WHOLE> struct Shape {
     // 2^15 (2^11 where they are held against the largest) keep all that are
     // above 2^-35 of the largest.
     static constexpr float SLACK = __is_same(T, f16) ? 4.0f : 8.0f, UP = __is_same(T, f16) ? 11.0f : 0.0f;
-    // Whether weights enter the second product as two numbers of T.
+    // Whether weights enter the second product as two numbers of T: with few
+    // rows memory bounds a call, and they keep 16 (fp16 22) bits.  With many the
+    // second number would be half as many products again, and they are
+    // rounded once, as the result is.
     static constexpr bool SPLIT = !F32 && WR < 4;
 
     // Pieces of a row are permuted by its number so that the lanes that read

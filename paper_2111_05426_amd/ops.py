@@ -1,10 +1,19 @@
-"""Python binding of the single-token step's operators (include/dsim_ops.h):
-argument marshalling only.
+"""Python binding of the operators of a single-token step (include/dsim_ops.h)
+and of a step of several tokens (include/dsim_multi_ops.h): argument
+marshalling only.
 
 * dsim_kv_append: new keys and values rotated by position and written into a
   paged cache, queries rotated on the way;
 * dsim_paged_attention: attention of one new token per sequence over it;
-* dsim_logit_adjust: penalties for repeated tokens, biases and grammar masks.
+* dsim_logit_adjust: penalties for repeated tokens, biases and grammar masks;
+* dsim_prompt_attention: attention of the new tokens of prompts, chunks of them
+  and packed documents over the cache, their own keys among them;
+* dsim_tree_attention: of a tree of drafted tokens over its context and itself;
+* dsim_kv_append_axes: the append with the rotation's positions apart from the
+  places in the cache, on up to four axes;
+* dsim_kv_reserve, dsim_kv_release, dsim_kv_fork, dsim_kv_copy_pages: the pages
+  of a cache and who holds them;
+* dsim_kv_compact: kept tokens of a sequence move to its front.
 
 A cache is a dict of device tensors: "k" and "v" of shape (pages, slots of a
 page, heads, head_dim) with any strides whose last is 1 (alloc_kv_cache keeps
@@ -20,6 +29,17 @@ block_table[s, t // page_size], slot t % page_size.
     ops.dsim_paged_attention(q, cache, block_table, seq_len, out, workspace=ws)
     ops.dsim_logit_adjust(logits, logits, history=tokens, history_len=seq_len, repetition=r)
 
+Pages are dealt out by a pool, and a draft of several tokens per sequence is
+checked in one step:
+
+    pool = ops.alloc_page_pool(n_pages, rows)
+    ops.dsim_kv_reserve(pool, block_table, 16, seq_len, seq_len + nodes, status)
+    ops.dsim_kv_append_axes(cache, block_table, k, v, seq, slot, depth_position, rope, q=q, q_out=q)
+    ops.dsim_tree_attention(q, cache, block_table, start, seq_len, tree_mask, out, depth=depth)
+    # the accepted path, node numbers in ascending order, moves to the context's end
+    ops.dsim_kv_compact(layers, block_table, seq_len, path, n_accepted)
+    ops.dsim_kv_release(pool, block_table, 16, row, seq_len + n_accepted)
+
 Every call runs on the device of its tensors, on `stream` (a torch stream or
 a raw handle; None: that device's current stream), where its tensors must be
 ready.  Like the rest of the binding the calls raise ValueError for tensors
@@ -27,13 +47,14 @@ that do not match what the library reads or writes, before any launch, and
 DsimError where the library refuses.  None has a derivative: a tensor that
 requires a gradient is refused while gradients are recorded, and one that
 carries a tangent; what a call writes counts as changed in place.  The checks
-and the call are host C++ (binding/ops_binding.cpp, built as _ops.so); there
+and the call are host C++ (binding/, built as _ops.so); there
 is no fallback.
 """
 from . import dsim
 from .dsim import DsimError  # noqa: F401  (what the calls raise)
 
 ST_BAD_PAGE, ST_BAD_POSITION, ST_BAD_SEQUENCE = 128, 256, 512
+ST_NO_PAGE, ST_SHARED_PAGE, ST_IN_USE = 1024, 2048, 4096
 
 _native = None
 
