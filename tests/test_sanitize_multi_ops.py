@@ -8,7 +8,9 @@ import subprocess
 import pytest
 
 from paper_2111_05426_amd import build
-from test_sanitize_ops import CLANG, HERE
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+CLANG = "/opt/rocm/llvm/bin/clang++"
 
 
 @pytest.mark.skipif(not os.path.exists(CLANG), reason="the ROCm clang is not installed")
