@@ -37,9 +37,10 @@
 //     TFLOP/s: a tile is widened between two barriers.  (Widened a tile ahead
 //     between the products, with two tiles in shared memory: 787 to 811; the
 //     compiler runs out of registers.)
-//   fp32, 6 x 100 to 1,500 tokens of 3 documents, 12 heads of 80: 158 us, 21
-//     TFLOP/s of 153; heads of 96 by their products, documents that end inside
-//     blocks of 128 rows.
+//   fp32, 6 x 100 to 1,500 tokens of 3 documents, 12 heads of 80, a bias by
+//     distance: 123 us, 27 TFLOP/s of 153; heads of 96 by their products, 1.7
+//     times the pairs (documents end inside blocks of 128 rows), and 60 us to plan,
+//     begin, end and join blocks of 9 tiles.
 #pragma once
 
 #include <type_traits>
@@ -712,7 +713,13 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
         t0 = uniform(t0);
         n = uniform(n);
         span = make_int2(uniform(span.x), uniform(span.y));
-        const int32_t first_tile = span.x / KT;
+        // With a bias by distance from the last tile on: it makes the scores near
+        // a row's own place the largest, and where those come first, nothing is
+        // scaled.  (fp32 documents 123 us, from the first on 158; 4,096 tokens 911
+        // and 1,370.  Without a bias trees take 2 to 5% longer so.)
+        const int32_t ahead = p.slopes ? -KT : KT;   // keys from a tile to the next
+        const int32_t first_key = (span.x / KT + (p.slopes ? uniform(tiles) - 1 : 0)) * KT;   // of tile 0
+        const auto tile_key = [&](int32_t tile) { return first_key + tile * ahead; };
         if (span.y == 0) n = 0;   // (no keys: the rows are written all the same)
 
         __syncthreads();   // (the block before has been written)
@@ -818,7 +825,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
         auto fetch = [&](int32_t tile) {
 #pragma unroll
             for (int j = 0; j < S::GROUPS; ++j) {
-                const int32_t key = group_key((first_tile + min(tile, last - 1)) * KT, j);
+                const int32_t key = group_key(tile_key(min(tile, last - 1)), j);
                 const int32_t of = divide(key, page_mul, page_shift);
                 page[j] = entries[of];
                 slot[j] = key - of * page_size;
@@ -879,12 +886,12 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
         if (n > 0) {
             if constexpr (S::DMA) {
                 fetch(t0);
-                send((first_tile + t0) * KT, t0 & 1);
+                send(tile_key(t0), t0 & 1);
                 fetch(t0 + 1);
             } else {
-                look((first_tile + t0) * KT);
-                load((first_tile + t0) * KT);
-                look((first_tile + t0 + 1) * KT);
+                look(tile_key(t0));
+                load(tile_key(t0));
+                look(tile_key(t0 + 1));
             }
         }
         // the lane's row
@@ -981,7 +988,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                 const int32_t tile = step / S::H, half = step - tile * S::H;
                 const int turn = tile & 1;
                 const uint32_t now = (S::DMA ? turn * 2 * S::TILE : 0) + half * (S::KS * S::PITCH);   // the step's place in s_buf
-                const int32_t k0 = first_tile * KT + step * S::KS;
+                const int32_t k0 = tile_key(tile) + half * S::KS;
                 partial = !(k0 >= all_lo && k0 + S::KS <= all_hi);
                 const bool skip = k0 + wk * S::KW >= wave_hi || k0 + (wk + 1) * S::KW <= wave_lo;
                 bool spread = false;
@@ -999,13 +1006,13 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                             spread = exact && !skip;
 #pragma unroll
                             for (int j = 0; j < S::GROUPS; ++j) {
-                                const int32_t key = k0 + KT + wave * S::SHARE + j * S::GROUP;
+                                const int32_t key = k0 + ahead + wave * S::SHARE + j * S::GROUP;
                                 const uint32_t of = (uint32_t)uniform(page[j]);
                                 spread &= key >= least_key && key + S::GROUP - 1 <= last_key && of < n_pages;
                                 from[j] = of * page_bytes + (int64_t)((uint64_t)(uint32_t)uniform(slot[j]) * slot_bytes);
                             }
                             if (!spread) {
-                                send(k0 + KT, turn ^ 1);
+                                send(k0 + ahead, turn ^ 1);
                                 fetch(tile + 2);
                             }
                         }
@@ -1036,8 +1043,8 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                         if (tid < KT / 32) s_bad[turn ^ 1][tid] = 0;
                         __syncthreads();
                         if (tile + 1 < last) {
-                            load(k0 + KT);
-                            look(k0 + 2 * KT);
+                            load(k0 + ahead);
+                            look(k0 + 2 * ahead);
                         }
                         note = uniform((int32_t)s_note[turn]);
                     }
@@ -1299,7 +1306,8 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                 // to them: infinities and NaN, a thread a column.
                 __threadfence();
                 const Part part = Part::of(p, 2 * index + (t0 == 0 ? 1 : 0));
-                for (int32_t key = max((first_tile + t0) * KT, span.x); key < min((first_tile + last) * KT, span.y); ++key) {
+                const int32_t a = tile_key(t0), z = tile_key(last - 1);
+                for (int32_t key = max(min(a, z), span.x); key < min(max(a, z) + KT, span.y); ++key) {
                     const int32_t k0 = key / KT * KT;
                     if (k0 >= all_lo && k0 + KT <= all_hi) continue;   // (was not cleaned)
                     const int32_t of = divide(key, p.page_mul, p.page_shift), page = table[of];

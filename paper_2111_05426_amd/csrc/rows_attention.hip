@@ -11,7 +11,7 @@ namespace rows {
 // rows a sequence, 32 9.6, 64 9.9; 60 rows, 64 8.7, 32 9.6, 128 9.1; 64 rows over
 // 64 contexts, 64 151, 32 278, 128 163; a prompt of 32,768 rows, 256 632, 128 665; 384
 // rows over an e4m3 cache, 128 740, 256 846.  fp32 has no registers for 256, and with
-// blocks of 64 documents take 199 for 158.
+// blocks of 64 documents took 199 for 158.
 static int rows_of(int64_t n_tok, int32_t n_seq, int32_t group, int32_t head_dim, bool f32)
 {
     const int64_t average = n_seq > 0 ? (n_tok * group + n_seq - 1) / n_seq : 0;

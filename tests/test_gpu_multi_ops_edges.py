@@ -122,6 +122,32 @@ def test_values_that_are_not_finite(dtype, cache, n, length, width, tree):
 @pytest.mark.parametrize("n,length", SIZES)
 @pytest.mark.parametrize("width", [None, 100])
 @pytest.mark.parametrize("tree", [False, True])
+def test_special_values_with_a_bias(dtype, cache, n, length, width, tree):
+    """The same where a bias by distance turns the order of the tiles."""
+    slopes = torch.tensor([0.0, 0.7], device="cuda")
+    c = Call(dtype, cache, 2, 2, 64, 16, [n, 3], [length - n, 9] if tree else [length, 9], tree=tree, width=width, slopes=slopes)
+    want, want_lse, _ = c.results()
+    odd = torch.zeros(want.shape, dtype=torch.bool)
+    bad = torch.zeros(want.shape[0], dtype=torch.bool)
+    for head, key, element in ((0, length - 1, 5), (1, length - n // 2 - 1, 17)):
+        page, slot = c.place(0, key)
+        c.v[page, slot, head, element] = math.nan
+        odd[rows_of(c, 0), head, element] |= c.attends(0, key)
+    first = (length - n) // 16
+    for key in range(first * 16, min((first + 1) * 16, length)):
+        bad[rows_of(c, 0)] |= c.attends(0, key)
+    out, lse, _ = c.results()
+    assert torch.equal(lse, want_lse) and torch.equal(out[~odd], want[~odd]) and not out[odd].isfinite().any()
+    c.table[0, first] = -1
+    out, lse, status = c.results()
+    assert status.tolist() == [128, 0] and out[bad].isnan().all() and lse[bad].isnan().all()
+    assert torch.equal(lse[~bad], want_lse[~bad]) and torch.equal(out[~bad][~odd[~bad]], want[~bad][~odd[~bad]])
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("n,length", SIZES)
+@pytest.mark.parametrize("width", [None, 100])
+@pytest.mark.parametrize("tree", [False, True])
 def test_keys_that_are_nan(dtype, cache, n, length, width, tree):
     c = Call(dtype, cache, 2, 1, 64, 16, [n, 3], [length - n, 9] if tree else [length, 9], tree=tree, width=width)
     want, want_lse, _ = c.results()
@@ -230,6 +256,16 @@ def test_large_scores(dtype, cache, width):
     for scale in (3.0, -3.0):
         check(dtype, cache, 4, 2, 64, 16, [150, 3], [400, 9], scale=scale, spread=8.0, width=width)
         check(dtype, cache, 4, 2, 64, 16, [15, 3], [400, 9], scale=scale, spread=8.0, width=width, tree=True)
+
+
+@pytest.mark.parametrize("dtype,cache", [(F32, F32), (F16, F16), (BF16, BF16), (F16, E4M3)])
+@pytest.mark.parametrize("n", [20, 300])
+def test_steep_biases_over_cut_blocks(dtype, cache, n):
+    """A bias that grows by more than the weights' room from tile to tile."""
+    def edit(x):
+        x["slope"].copy_(torch.tensor([3.0, 0.5, -0.6, 0.001]))
+    for tree in (False, True):
+        check(dtype, cache, 4, 2, 64, 16, [n, 3], [1500, 900], slopes=True, width=200, edit=edit, tree=tree)
 
 
 @pytest.mark.parametrize("n,cap", [(20, 0.0), (300, 0.0), (300, 20.0)])
