@@ -26,14 +26,14 @@
 //
 // What bounds it, on MI355X (bf16, heads of 128; the product of 8,192 cubed
 // reaches 1,101 TFLOP/s here):
-//   8,192 tokens of one prompt, 32 / 8 heads: 630 us, 873 TFLOP/s.  Matrix
+//   8,192 tokens of one prompt, 32 / 8 heads: 606 to 632 us, 870 to 908 TFLOP/s.  Matrix
 //     instructions and the exponentials' vector ones take turns; without the
 //     loads it would be 605.
 //   16 chunks of 1 to 1,024 tokens behind 2,000, window 1,500, cap 50: 425 us, 473
 //     TFLOP/s; a capped score takes two more transcendental instructions.
 //   64 trees of 16 nodes over 1 to 4,096 tokens: 151 us, 3.7 TB/s of the cache,
 //     of which plan and join 19.
-//   4 trees of 48 nodes over 65,536 tokens in e4m3, 64 / 8 heads, cap 30: 740 us, 556
+//   4 trees of 48 nodes over 65,536 tokens in e4m3, 64 / 8 heads, cap 30: 723 us, 570
 //     TFLOP/s: a tile is widened between two barriers.  (Widened a tile ahead
 //     between the products, with two tiles in shared memory: 787 to 811; the
 //     compiler runs out of registers.)

@@ -9,15 +9,16 @@ namespace rows {
 // Rows of a block: about what the average sequence has (more are multiplied as
 // padding, fewer read the keys again).  us with the size taken and another: 8
 // rows a sequence, 32 9.6, 64 9.9; 60 rows, 64 8.7, 32 9.6, 128 9.1; 64 rows over
-// 64 contexts, 64 151, 32 278, 128 163; a prompt of 32,768 rows, 256 632, 128 665; 384
-// rows over an e4m3 cache, 128 740, 256 846.  fp32 has no registers for 256, and with
+// 64 contexts, 64 151, 32 278, 128 163; 384 rows over an e4m3 cache, 128 740, 256 846; 32
+// prompts of 1,200 rows, 128 102, 256 115; 64 of 2,200, 256 482, 128 540; one of 32,768,
+// 256 632, 128 665.  fp32 has no registers for 256, and with
 // blocks of 64 documents took 199 for 158.
 static int rows_of(int64_t n_tok, int32_t n_seq, int32_t group, int32_t head_dim, bool f32)
 {
     const int64_t average = n_seq > 0 ? (n_tok * group + n_seq - 1) / n_seq : 0;
     if (average <= 32 && head_dim <= 128) return 32;
     if (average <= 64) return 64;
-    return average <= 512 || head_dim > 128 || f32 ? 128 : 256;
+    return average <= 1536 || head_dim > 128 || f32 ? 128 : 256;
 }
 
 static int64_t blocks(int64_t n_tok, int32_t n_seq, int32_t group, int rows)
@@ -121,10 +122,12 @@ dsim_status launch_rows(const RowsArgs &a, hipStream_t s)
     divisor(p.page_size, p.page_mul, p.page_shift);
     divisor(p.group, p.group_mul, p.group_shift);
     // A workgroup a block, without plan and join, where no block is long and
-    // two rounds of workgroups hold them all: one request's prompt of 60 tokens 8.7
-    // us, planned and joined 16.1, its drafts 9.6 and 17.1.
+    // there are few: one request's prompt of 60 tokens 8.7 us, planned and joined
+    // 16.1, its drafts 9.6 and 17.1; 128 prompts of 10 to 100 tokens of 32 / 8 heads
+    // 59.6 and 71.6 (512 of them 296 and 269), 256 drafts over 10 to 500 keys of 12
+    // heads of 64 84.4 and 88.9, of 32 / 8 heads of 128 165.7 and 159.7.
     const int64_t most = (int64_t)p.table_width * p.page_size;
-    p.direct = most <= 1024 && p.max_blocks * p.n_heads <= 2 * kMaxGrid;
+    p.direct = most <= 1024 && p.max_blocks * p.n_heads <= 8 * kMaxGrid;
     if (a.q.dtype == DSIM_F32) return rows::launch_f32(p, s);
     return (a.q.dtype == DSIM_F16 ? rows::launch_f16 : rows::launch_bf16)(p, a.c.dtype == DSIM_E4M3, s);
 }

@@ -31,12 +31,15 @@ def ints(x):
 def weights_off(dtype, tokens, n_seq, group):
     """What a weight may be off before the second product: fp32's bits, two
     numbers of the type for few rows, one for many; and below what part of the
-    largest weight it is lost (fp16 rounds to multiples of 2^-24, off by 2^-25,
-    and the weight of the score that others are held against is 2^11)."""
+    largest weight it is lost.  fp16 rounds to multiples of 2^-24, off by 2^-25,
+    and the weight of the score that others are held against is 2^11.  Else
+    exponentials end at 2^-126, where fp32's numbers of full precision do: the
+    score that others are held against is not above the largest, whose weight is
+    1 or more, so what is lost is less than 2^-126 of it."""
     if dtype == F32:
-        return 0.0, 0.0
+        return 0.0, 2.0 ** -126
     few = tokens * group <= 64 * n_seq
-    return (HALF[dtype] ** 2 if few else HALF[dtype]), (2.0 ** -36 if dtype == F16 else 0.0)
+    return (HALF[dtype] ** 2 if few else HALF[dtype]), (2.0 ** -36 if dtype == F16 else 2.0 ** -126)
 
 
 def random_tree(g, n):
@@ -234,3 +237,17 @@ def test_scales(scale):
     check(F32, F32, 4, 2, 64, 16, [2, 6], [50, 60], scale=scale, tree=True)
     if scale != 1e-30:
         check(F16, F16, 4, 2, 64, 16, [20, 60], [50, 60], scale=scale, cap=10.0)
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("heads,kv,d,slots", [(8, 1, 128, 16), (16, 2, 64, 48), (8, 1, 80, 7), (10, 1, 112, 32), (8, 1, 32, 16)])
+def test_largest_blocks(dtype, cache, heads, kv, d, slots):
+    """More than 1,536 rows a sequence on average, in blocks of their own and
+    cut ones."""
+    new, lens = [330, 100], [330, 500]
+    for width in (None, 2000 // slots):
+        check(dtype, cache, heads, kv, d, slots, new, lens, seed=2, width=width)
+        check(dtype, cache, heads, kv, d, slots, new, lens, seed=3, window=133, cap=30.0, prefix=[40, 300], width=width)
+        check(dtype, cache, heads, kv, d, slots, new, lens, seed=4, slopes=True, cap=200.0, width=width)
+        check(dtype, cache, heads, kv, d, slots, new, [40, 300], seed=5, tree=True, width=width)
+    check(dtype, cache, heads, kv, d, slots, new, lens, seed=6, docs=[i // 97 * 97 for i in range(330)] + [350] * 100, scale=2.0)

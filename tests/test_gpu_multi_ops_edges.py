@@ -383,3 +383,33 @@ def test_versions():
         x.run(clear=False)
         with pytest.raises(RuntimeError, match="modified by an inplace operation"):
             y.backward()
+
+
+@pytest.mark.parametrize("dtype,cache", [(F16, F16), (BF16, BF16), (F16, E4M3), (BF16, E4M3)])
+@pytest.mark.parametrize("slots", [16, 48, 5])
+@pytest.mark.parametrize("width", [None, 400])
+@pytest.mark.parametrize("tree", [False, True])
+def test_special_values_in_the_largest_blocks(dtype, cache, slots, width, tree):
+    """More than 1,536 rows a sequence on average: blocks of 256."""
+    n, length = 500, 620
+    c = Call(dtype, cache, 16, 2, 64, slots, [n, 3], [length - n, 9] if tree else [length, 9], tree=tree, width=width)
+    want, want_lse, _ = c.results()
+    odd, nan = torch.zeros(want.shape, dtype=torch.bool), torch.zeros(want.shape[:2], dtype=torch.bool)
+    for head, key, element in ((0, length - 1, 5), (1, length - n // 2 - 1, 17), (1, length - n, 63)):
+        page, slot = c.place(0, key)
+        c.v[page, slot, head, element] = math.nan
+        odd[rows_of(c, 0), 8 * head:8 * head + 8, element] |= c.attends(0, key)[:, None]
+    out, lse, _ = c.results()
+    assert torch.equal(lse, want_lse) and torch.equal(out[~odd], want[~odd]) and not out[odd].isfinite().any()
+    page, slot = c.place(0, length - 40)
+    c.k[page, slot, 0, 3] = math.nan
+    nan[rows_of(c, 0), :8] |= c.attends(0, length - 40)[:, None]
+    at = (length - 90) // slots
+    c.table[0, at] = c.k.shape[0]
+    for key in range(at * slots, (at + 1) * slots):
+        nan[rows_of(c, 0)] |= c.attends(0, key)[:, None]
+    out, lse, status = c.results()
+    assert status.tolist() == [128, 0]
+    assert out[nan].isnan().all() and lse[nan].isnan().all() and torch.equal(lse[~nan], want_lse[~nan])
+    rest = ~(odd | nan[:, :, None])
+    assert torch.equal(out[rest], want[rest])
