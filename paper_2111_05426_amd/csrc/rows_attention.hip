@@ -125,9 +125,10 @@ dsim_status launch_rows(const RowsArgs &a, hipStream_t s)
     // there are few: one request's prompt of 60 tokens 8.7 us, planned and joined
     // 16.1, its drafts 9.6 and 17.1; 128 prompts of 10 to 100 tokens of 32 / 8 heads
     // 59.6 and 71.6 (512 of them 296 and 269), 256 drafts over 10 to 500 keys of 12
-    // heads of 64 84.4 and 88.9, of 32 / 8 heads of 128 165.7 and 159.7.
+    // heads of 64 84.4 and 88.9, of 32 / 8 heads of 128 165.7 and 159.7.  Each finds
+    // its sequence among all, 64 at a time, so there are few of those too.
     const int64_t most = (int64_t)p.table_width * p.page_size;
-    p.direct = most <= 1024 && p.max_blocks * p.n_heads <= 8 * kMaxGrid;
+    p.direct = most <= 1024 && p.n_seq <= 256 && p.max_blocks * p.n_heads <= 8 * kMaxGrid;
     if (a.q.dtype == DSIM_F32) return rows::launch_f32(p, s);
     return (a.q.dtype == DSIM_F16 ? rows::launch_f16 : rows::launch_bf16)(p, a.c.dtype == DSIM_E4M3, s);
 }

@@ -288,6 +288,19 @@ def test_more_sequences_than_threads(dtype, tree):
     check(dtype, dtype, 2, 1, 16, 16, new, lens, tree=tree, width=100)
 
 
+@pytest.mark.parametrize("n_seq", [63, 64, 65, 200, 256, 257])
+@pytest.mark.parametrize("tree", [False, True])
+def test_sequences_among_many(n_seq, tree):
+    """Blocks find theirs among many, of which some have none."""
+    g = gen(n_seq)
+    new = (torch.randint(-20, 40, (n_seq,), generator=g).clamp(min=0)).tolist()
+    lens = [n + int(x) for n, x in zip(new, torch.randint(0, 40, (n_seq,), generator=g))]
+    for i in range(3, n_seq, 17):
+        lens[i] = -1
+    check(BF16, BF16, 4, 2, 32, 16, new, lens, tree=tree)
+    check(F32, F32, 4, 1, 16, 16, new, lens, tree=tree)
+
+
 @pytest.mark.parametrize("cache,order", [(BF16, "head"), (E4M3, "head"), (F32, "slot")])
 def test_a_cache_beyond_32_bits(cache, order):
     """Pages whose first element is number 2^32 and more (2^31 and 2^32 bytes
