@@ -398,6 +398,17 @@ __device__ inline float rescale(float from, float to, float scale)
     return from == -HUGE_VALF ? 1.0f : __builtin_amdgcn_exp2f((from - to) * scale);
 }
 
+// The largest score that is weighed against m: `slack` base-2 units above it.
+// Where fp32's own steps are that wide, m alone: rounded up to the next one the
+// sum may be twice the slack above m, and fp16's weight of a score that high
+// infinite (2^(11 + 4) is the largest that it is meant to have; half a unit
+// more is in its range).
+__device__ inline float limit_of(float m, float slack, float unit)
+{
+    const float y = m + slack / unit;
+    return (y - m) * unit > slack + 0.5f ? m : y;
+}
+
 // T: type of the queries, CT: of the cache, DP: the head's size padded, WR:
 // blocks of 32 rows in a workgroup.  Its waves, four, or eight of 256 rows, are
 // WR x WK: those of a block of rows share out the keys of a tile.
@@ -1181,7 +1192,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                     if (fresh && __builtin_amdgcn_ballot_w64(top > limit && m != -HUGE_VALF) != 0) break;
                     // rows that had none: nothing to scale
                     m = m == -HUGE_VALF ? top : m;
-                    limit = m == -HUGE_VALF ? m : m + S::SLACK / sc.unit;
+                    limit = m == -HUGE_VALF ? m : limit_of(m, S::SLACK, sc.unit);
                 }
                 // outputs (rows) of the rows (columns); the first values come
                 // while the weights are computed
@@ -1227,7 +1238,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
 #pragma unroll
                 for (int e = 0; e < OB; ++e) o[e] *= f;
                 m = to;
-                limit = m == -HUGE_VALF ? m : m + S::SLACK / sc.unit;
+                limit = m == -HUGE_VALF ? m : limit_of(m, S::SLACK, sc.unit);
             }
             fresh = false;
         }
