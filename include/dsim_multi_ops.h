@@ -165,13 +165,16 @@ typedef struct {
  * stays as it is).  The lowest-numbered free pages are dealt out in order of
  * rows and places.  A row whose pages cannot all be had gets none, and neither
  * do the rows after it that need some.
- *   seq_len: device array [n_seq]: the places in use.  Where the row is to
- *            grow beyond them and the last lies in the middle of a page that
- *            other rows hold too, writing on would change theirs:
- *            DSIM_ST_SHARED_PAGE, no pages (dsim_kv_fork makes a copy).
+ *   seq_len: device array [n_seq]: the places in use.  A row that is to grow
+ *            beyond them writes to the pages that it holds already from place
+ *            seq_len on, up to new_len: where other rows hold one of those too,
+ *            writing would change theirs: DSIM_ST_SHARED_PAGE, no pages.
+ *            (dsim_kv_release gives back those that lie behind seq_len,
+ *            dsim_kv_fork makes a copy of the one in which it ends.)
  *   status:  device array [n_seq]: 0, DSIM_ST_NO_PAGE, DSIM_ST_SHARED_PAGE,
  *            DSIM_ST_BAD_POSITION (more places than the table has, or
- *            seq_len outside what the row holds) or DSIM_ST_BAD_PAGE
+ *            seq_len outside what the row holds) or DSIM_ST_BAD_PAGE (one of
+ *            those pages lies outside the cache)
  */
 DSIM_API dsim_status dsim_kv_reserve(const dsim_page_pool *pool, const int32_t *seq_len, const int32_t *new_len,
                                      int32_t *status, void *hip_stream);

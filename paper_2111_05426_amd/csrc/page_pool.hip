@@ -11,9 +11,10 @@
 //
 // On MI355X a beam search's step over 128 rows (64 released, as many forked over
 // 1 to 2,048 tokens with a half page of four layers each, a place reserved in
-// each; 16 MB) takes 24.4 us in its calls' four launches: release 3.9, fork 7.2,
-// copy 6.8, reserve 6.3, each a chain of three or four loads and the barriers of
-// its sums.
+// each; 16 MB) takes 24.8 us in its calls' four launches: release 3.9, fork 7.2,
+// copy 6.8, reserve 6.7, each a chain of three or four loads and the barriers of
+// its sums.  A reserve for rows that hold pages in advance looks at those that the
+// row grows into: 128 rows of 500 of them 22 us, 4 rows of 4,096 20.
 #include "multi_ops.h"
 #include "numeric.h"
 
@@ -66,9 +67,11 @@ struct Need {
 
 // Deals free pages to n takers in order.  take(i) is what i needs, got(i,
 // status) is told once whether it gets it, put(i, j, page) where its j-th page
-// is.  take must give the same until all is dealt.
-template <class Take, class Got, class Put>
-__device__ inline void deal(const dsim_page_pool &p, int64_t n, Take take, Got got, Put put)
+// is.  take must give the same until all is dealt.  All threads call it together,
+// also for i >= n, who need nothing, and settle(i, need) behind a barrier: what the
+// threads have to find together.
+template <class Take, class Settle, class Got, class Put>
+__device__ inline void deal(const dsim_page_pool &p, int64_t n, Take take, Settle settle, Got got, Put put)
 {
     __shared__ int64_t s_sum[kDealWaves];
     __shared__ int32_t s_page[kWindow];
@@ -76,15 +79,22 @@ __device__ inline void deal(const dsim_page_pool &p, int64_t n, Take take, Got g
     const int64_t words = (p.n_pages + 31) / 32;
     int64_t total, mine = 0;
     for (int64_t w = tid; w < words; w += kDeal) mine += __popc(free_word(p, w));
+    // (what the first kDeal need is kept: it takes three loads in a row)
+    Need mine_ = take(tid);
     scan(mine, s_sum, total);
     const int64_t avail = total;
+    settle(tid, mine_);
+    const auto later = [&](int64_t i) {
+        Need x = take(i);
+        __syncthreads();
+        settle(i, x);
+        return x;
+    };
 
-    // (what the first kDeal need is kept: it takes three loads in a row)
-    const Need mine_ = tid < n ? take(tid) : Need{0, 0, true};
     int64_t before = 0, dealt = 0, at_ = 0;
     for (int64_t i0 = 0; i0 < n; i0 += kDeal) {
         const int64_t i = i0 + tid;
-        const Need x = i0 == 0 ? mine_ : i < n ? take(i) : Need{0, 0, true};
+        const Need x = i0 == 0 ? mine_ : later(i);
         const int64_t at = before + scan(x.pages, s_sum, total);
         if (i0 == 0) at_ = at;
         const bool enough = x.pages == 0 || at + x.pages <= avail;
@@ -119,7 +129,7 @@ __device__ inline void deal(const dsim_page_pool &p, int64_t n, Take take, Got g
         before = 0;
         for (int64_t i0 = 0; i0 < n && before < r1; i0 += kDeal) {
             const int64_t i = i0 + tid;
-            const Need x = i0 == 0 ? mine_ : i < n ? take(i) : Need{0, 0, true};
+            const Need x = i0 == 0 ? mine_ : later(i);
             int64_t at = at_;
             if (n > kDeal) at = before + scan(x.pages, s_sum, total);
             if (at + x.pages <= avail)
@@ -132,26 +142,84 @@ __device__ inline void deal(const dsim_page_pool &p, int64_t n, Take take, Got g
 
 __device__ inline int64_t pages_of(int64_t places, int32_t page_size) { return (places + page_size - 1) / page_size; }
 
+// Why a page of a row may not be written to, in bits.
+__device__ inline int32_t unwritable(const dsim_page_pool &p, int32_t page)
+{
+    return page < 0 || page >= p.n_pages ? DSIM_ST_BAD_PAGE : p.refs[page] > 1 ? DSIM_ST_SHARED_PAGE : 0;
+}
+
+// Of entries first, first + step, ... below end of a row of the table, four at a
+// time, all of them together.
+__device__ inline int32_t unwritable(const dsim_page_pool &p, const int32_t *entries, int32_t first, int32_t end, int32_t step)
+{
+    constexpr int kAtOnce = 4;
+    int32_t found = 0;
+    for (int64_t j0 = first; j0 < end; j0 += kAtOnce * step) {
+        int32_t page[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) page[k] = entries[min(j0 + k * step, (int64_t)end - 1)];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) found |= unwritable(p, page[k]);
+    }
+    return found;
+}
+
 __global__ __launch_bounds__(kDeal) void k_reserve(dsim_page_pool p, const int32_t *seq_len, const int32_t *new_len,
                                                    int32_t *status)
 {
+    // Rows grow into pages that they hold already, from that of place seq_len on.
+    // Mostly that is one, in which a row's tokens end; of a row that went back, or
+    // holds pages in advance, it may be thousands, and those are shared out among
+    // the waves.
+    constexpr int kAlone = 16;
+    __shared__ int32_t s_much, s_first[kDeal], s_end[kDeal], s_found[kDeal];
+    const auto told = [](int32_t found) { return found & DSIM_ST_BAD_PAGE ? DSIM_ST_BAD_PAGE : found; };
+    const auto range = [&](int64_t s, int64_t want, int64_t len, int64_t held) {
+        return make_int2((int32_t)len / p.page_size, (int32_t)min(held, pages_of(want, p.page_size)));
+    };
+    if (threadIdx.x == 0) s_much = 0;
+    __syncthreads();
     auto take = [&](int64_t s) {
-        Need x{0, 0, false};
+        Need x{0, 0, true};
+        if (s >= p.n_seq) return x;
         const int64_t want = new_len[s], len = seq_len[s], held = p.held[s], pages = pages_of(want, p.page_size);
-        if (want < 0) return Need{0, 0, true};
-        if (pages > p.table_width || held < 0 || held > p.table_width || len < 0 || len > held * p.page_size)
+        x.skip = want < 0;
+        if (x.skip) return x;
+        if (pages > p.table_width || held < 0 || held > p.table_width || len < 0 || len > held * p.page_size) {
             x.status = DSIM_ST_BAD_POSITION;
-        else if (want > len && len % p.page_size) {
-            const int32_t last = p.block_table[s * p.table_stride + len / p.page_size];
-            if (last < 0 || last >= p.n_pages)
-                x.status = DSIM_ST_BAD_PAGE;
-            else if (p.refs[last] > 1)
-                x.status = DSIM_ST_SHARED_PAGE;
+        } else if (want > len) {
+            const int2 grown = range(s, want, len, held);
+            const int32_t *entries = p.block_table + s * p.table_stride;
+            if (grown.y - grown.x > kAlone)
+                s_much = 1;   // (stays so: settle looks for such rows)
+            else if (grown.x < grown.y)
+                x.status = told(unwritable(p, entries[grown.x]) | unwritable(p, entries, grown.x + 1, grown.y, 1));
         }
         if (!x.status && pages > held) x.pages = pages - held;
         return x;
     };
-    deal(p, p.n_seq, take, [&](int64_t s, int32_t st) { status[s] = st; },
+    auto settle = [&](int64_t s, Need &x) {
+        if (s_much == 0) return;
+        const int tid = threadIdx.x, lane = tid & 63;
+        int2 grown = make_int2(0, 0);
+        if (!x.skip && !x.status && new_len[s] > seq_len[s]) grown = range(s, new_len[s], seq_len[s], p.held[s]);
+        const bool much = grown.y - grown.x > kAlone;
+        s_first[tid] = grown.x;
+        s_end[tid] = much ? grown.y : grown.x;
+        __syncthreads();
+        for (int t = tid >> 6; t < kDeal; t += kDealWaves) {
+            const int32_t first = s_first[t], end = s_end[t];
+            if (first == end) continue;
+            int32_t found = 0;
+            if (first + lane < end) found = unwritable(p, p.block_table + (s - tid + t) * p.table_stride, first + lane, end, 64);
+            const bool bad = __builtin_amdgcn_ballot_w64(found & DSIM_ST_BAD_PAGE) != 0;
+            const bool shared = __builtin_amdgcn_ballot_w64(found & DSIM_ST_SHARED_PAGE) != 0;
+            if (lane == 0) s_found[t] = (bad ? DSIM_ST_BAD_PAGE : 0) | (shared ? DSIM_ST_SHARED_PAGE : 0);
+        }
+        __syncthreads();
+        if (much && s_found[tid]) x = Need{0, told(s_found[tid]), false};
+    };
+    deal(p, p.n_seq, take, settle, [&](int64_t s, int32_t st) { status[s] = st; },
          [&](int64_t s, int64_t j, int32_t page) { p.block_table[s * p.table_stride + p.held[s] + j] = page; });
     for (int64_t s = threadIdx.x; s < p.n_seq; s += kDeal) {
         const int64_t want = new_len[s], more = pages_of(want, p.page_size) - p.held[s];
@@ -205,7 +273,8 @@ __global__ __launch_bounds__(kDeal) void k_fork(dsim_page_pool p, int32_t *seq_l
     }
     __syncthreads();
     auto take = [&](int64_t i) {
-        Need x{0, 0, false};
+        Need x{0, 0, i >= n};
+        if (i >= n) return x;
         const int32_t d = dst[i], s = src[i];
         if (d < 0) return x;
         if (d >= p.n_seq || s < 0 || s >= p.n_seq) {
@@ -223,7 +292,7 @@ __global__ __launch_bounds__(kDeal) void k_fork(dsim_page_pool p, int32_t *seq_l
         }
         return x;
     };
-    deal(p, n, take, [&](int64_t i, int32_t st) { status[i] = st; },
+    deal(p, n, take, [](int64_t, Need &) {}, [&](int64_t i, int32_t st) { status[i] = st; },
          [&](int64_t i, int64_t, int32_t page) {
              p.block_table[dst[i] * p.table_stride + seq_len[src[i]] / p.page_size] = page;
          });
