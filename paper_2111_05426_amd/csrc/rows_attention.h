@@ -190,9 +190,11 @@ __device__ inline int2 span_of(const Params &p, const Seq &x, int s, int32_t i0,
     return lo < hi ? make_int2(lo, hi) : make_int2(0, 0);
 }
 
+// (A last key may be 2^31 - 2: here and below nothing is added to a key that a tile
+// further on might not fit.)
 template <int KT> __device__ inline int32_t tiles_of(int2 span)
 {
-    return max((span.y + KT - 1) / KT - span.x / KT, 1);
+    return span.y > 0 ? (span.y - 1) / KT + 1 - span.x / KT : 1;
 }
 
 // Sum of x over the workgroup's threads before this one, and the total.
@@ -902,7 +904,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
             } else {
                 look(tile_key(t0));
                 load(tile_key(t0));
-                look(tile_key(t0 + 1));
+                look(tile_key(min(t0 + 1, last - 1)));
             }
         }
         // the lane's row
@@ -1000,13 +1002,13 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                 const int turn = tile & 1;
                 const uint32_t now = (S::DMA ? turn * 2 * S::TILE : 0) + half * (S::KS * S::PITCH);   // the step's place in s_buf
                 const int32_t k0 = tile_key(tile) + half * S::KS;
-                partial = !(k0 >= all_lo && k0 + S::KS <= all_hi);
-                const bool skip = k0 + wk * S::KW >= wave_hi || k0 + (wk + 1) * S::KW <= wave_lo;
+                partial = !(k0 >= all_lo && k0 <= all_hi - S::KS);
+                const bool skip = k0 + wk * S::KW >= wave_hi || k0 <= wave_lo - (wk + 1) * S::KW;
                 bool spread = false;
                 int64_t from[S::GROUPS];
                 uint32_t without = 0;   // groups of the tile without a page
                 if (fresh && half == 0) {
-                    const bool any = !(k0 >= all_lo && k0 + KT <= all_hi);
+                    const bool any = !(k0 >= all_lo && k0 <= all_hi - KT);
                     if constexpr (S::DMA) {
                         arrived();
                         __syncthreads();   // the tile is there, the one before has been read
@@ -1055,7 +1057,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                         __syncthreads();
                         if (tile + 1 < last) {
                             load(k0 + ahead);
-                            look(k0 + 2 * ahead);
+                            look(tile_key(min(tile + 2, last - 1)));
                         }
                         note = uniform((int32_t)s_note[turn]);
                     }
@@ -1118,7 +1120,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                         sx[u] *= sc.in;
                         if (a.cap > 0.0f) cap_of<S::F32>(sx[u], sc.cap);
                         if (a.slopes) {
-                            if (a.tree && kw + 32 > x.len) {
+                            if (a.tree && kw > x.len - 32) {
 #pragma unroll 1
                                 for (int e = 0; e < 16; ++e) {   // (keys of nodes are where their nodes are)
                                     int32_t at = kw + 8 * (e / 4) + 4 * g + e % 4;
@@ -1143,7 +1145,7 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                         const int32_t kw = k0 + wk * S::KW + 32 * u;
                         const int32_t lo = min(max(in.lo - kw, 0), 32), hi = min(max(in.hi - kw, 0), 32);
                         in32[u] = (uint32_t)((1ull << hi) - 1) & ~(uint32_t)((1ull << lo) - 1);
-                        if (a.tree && kw + 32 > x.len && kw < x.keys) {
+                        if (a.tree && kw > x.len - 32 && kw < x.keys) {
                             // bits of the nodes from the first of these keys on
                             const int32_t node = kw - x.len, w = max(node, 0) >> 5;
                             uint64_t bits = mask[w];
@@ -1318,9 +1320,10 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                 __threadfence();
                 const Part part = Part::of(p, 2 * index + (t0 == 0 ? 1 : 0));
                 const int32_t a = tile_key(t0), z = tile_key(last - 1);
-                for (int32_t key = max(min(a, z), span.x); key < min(max(a, z) + KT, span.y); ++key) {
+                const int32_t end = span.y - max(a, z) < KT ? span.y : max(a, z) + KT;
+                for (int32_t key = max(min(a, z), span.x); key < end; ++key) {
                     const int32_t k0 = key / KT * KT;
-                    if (k0 >= all_lo && k0 + KT <= all_hi) continue;   // (was not cleaned)
+                    if (k0 >= all_lo && k0 <= all_hi - KT) continue;   // (was not cleaned)
                     const int32_t of = divide(key, p.page_mul, p.page_shift), page = table[of];
                     if (page < 0 || page >= p.n_pages || tid >= p.d) continue;
                     const float v = value_of(vb[page * p.page_stride + (key - of * p.page_size) * p.slot_stride + tid]);
