@@ -68,7 +68,10 @@ DSIM_API dsim_status dsim_kv_append_axes(const dsim_kv_cache *cache, int64_t n_t
  * A token that attends to nothing has o = 0 and lse = -inf; keys that it does
  * not attend to weigh nothing whatever they hold, and an attended value that is
  * not finite makes its element of o infinite or NaN.  Scores, statistics and
- * sums are fp32; the result is rounded once to out's type.
+ * sums are fp32 (exponentials off by 2^-21, in 16 bits tanh by 2^-20 of itself or
+ * 2^-21 of the cap); in 16 bits a weight enters the second sum as two numbers of
+ * the type (off by 2^-16, fp16 2^-22, and fp16's below 2^-36 of the largest are
+ * 0); the result is rounded once to out's type.
  *   q, out: n_tok rows of n_q_heads heads of `dtype`: the cache's type, or
  *           DSIM_F16 / DSIM_BF16 with an e4m3 cache; out may be q (with its
  *           strides), it must not overlap otherwise

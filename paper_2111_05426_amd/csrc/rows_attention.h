@@ -26,17 +26,17 @@
 //
 // What bounds it, on MI355X (bf16, heads of 128; the product of 8,192 cubed
 // reaches 1,101 TFLOP/s here):
-//   8,192 tokens of one prompt, 32 / 8 heads: 606 to 632 us, 870 to 908 TFLOP/s.  Matrix
-//     instructions and the exponentials' vector ones take turns; without the
-//     loads it would be 605.
-//   16 chunks of 1 to 1,024 tokens behind 2,000, window 1,500, cap 50: 425 us, 473
+//   8,192 tokens of one prompt, 32 / 8 heads: 817 us, 673 TFLOP/s of the formula's
+//     products, 1,010 of those that are made: the second is made twice, for
+//     weights of two numbers.
+//   16 chunks of 1 to 1,024 tokens behind 2,000, window 1,500, cap 50: 491 us, 410
 //     TFLOP/s; a capped score takes two more transcendental instructions.
 //   64 trees of 16 nodes over 1 to 4,096 tokens: 151 us, 3.7 TB/s of the cache,
 //     of which plan and join 19.
-//   4 trees of 48 nodes over 65,536 tokens in e4m3, 64 / 8 heads, cap 30: 723 us, 570
+//   4 trees of 48 nodes over 65,536 tokens in e4m3, 64 / 8 heads, cap 30: 885 us, 466
 //     TFLOP/s: a tile is widened between two barriers.  (Widened a tile ahead
-//     between the products, with two tiles in shared memory: 787 to 811; the
-//     compiler runs out of registers.)
+//     between the products, with two tiles in shared memory, and with weights of
+//     one number 787 to 811 for 723; the compiler runs out of registers.)
 //   fp32, 6 x 100 to 1,500 tokens of 3 documents, 12 heads of 80, a bias by
 //     distance: 123 us, 27 TFLOP/s of 153; heads of 96 by their products, 1.7
 //     times the pairs (documents end inside blocks of 128 rows), and 60 us to plan,
@@ -441,14 +441,8 @@ template <class T, class CT, int DP_, int WR_, bool WHOLE> struct Shape {
     static constexpr int LOADS = GROUP / RI;                   // loads of a group's keys
     // Offset for the weights' exponents.  fp16 ends at 2^-24: weights up to
     // 2^15 (2^11 where they are held against the largest) keep all that are
-    // above 2^-35 of the largest.
+    // above 2^-36 of the largest, in steps of 2^-35 at the end.
     static constexpr float SLACK = __is_same(T, f16) ? 4.0f : 8.0f, UP = __is_same(T, f16) ? 11.0f : 0.0f;
-    // Whether weights enter the second product as two numbers of T: with few
-    // rows memory bounds a call, and they keep 16 (fp16 22) bits.  With many the
-    // second number would be half as many products again, and they are
-    // rounded once, as the result is.
-    static constexpr bool SPLIT = !F32 && WR < 4;
-
     // Pieces of a row are permuted by its number so that the lanes that read
     // a column meet different banks: 16 rows' pieces of keys (16 bytes a
     // lane), 4 rows of 64 bytes of values (read transposed).
@@ -1214,6 +1208,11 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
                 } else {
                     const uint32_t v_now = again(v_at + now);
                     const auto read = [&](int i) { return values<T, S::PITCH>(v_now ^ 64 * (i % OB), i / OB); };
+                    // A weight enters the product as two numbers of T, 16 bits (fp16
+                    // 22).  (As one, rounded as the result is: 8,192 tokens of one
+                    // prompt 606 us for 817, capped chunks 426 for 491, e4m3 trees
+                    // 718 for 885, and outputs off by 2.2e-3 of their norm in bf16 for
+                    // 1.65e-3, one rounding's.)
                     vec<T, 8> a[4], w[2 * U], w2[2 * U];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) a[i] = read(i);
@@ -1224,11 +1223,11 @@ __attribute__((amdgpu_waves_per_eu((Shape<T, CT, DP, WR, WHOLE>::PER_SIMD), (Sha
 #pragma unroll
                         for (int e = 0; e < 8; ++e) y[e] = sx[k / 2][8 * (k % 2) + e];
                         w[k] = from_f32<T, 8>(y);
-                        if constexpr (S::SPLIT) w2[k] = from_f32<T, 8>(y - to_f32<T, 8>(w[k]));
+                        w2[k] = from_f32<T, 8>(y - to_f32<T, 8>(w[k]));
                     }
                     in_order<2 * U * OB>(a, read, [&](int i, const vec<T, 8> &x) {
                         o[i % OB] = Mfma<T>::mul(x, w[i / OB], o[i % OB]);
-                        if constexpr (S::SPLIT) o[i % OB] = Mfma<T>::mul(x, w2[i / OB], o[i % OB]);
+                        o[i % OB] = Mfma<T>::mul(x, w2[i / OB], o[i % OB]);
                     }, [](int) {});
                 }
             }

@@ -98,9 +98,9 @@ dsim_status launch_rows(const RowsArgs &a, hipStream_t s)
     p.window = a.q.window;
     p.group = a.q.n_q_heads / a.c.n_heads;
     p.rows = rows_of(p.n_tok, p.n_seq, p.group, p.d, a.q.dtype == DSIM_F32);
-    // Where weights are rounded to their type's bits before the second product,
-    // a cap of at most 128 takes tanh's short form: off by 2^-21 of the cap, 2^-14
-    // of a weight.
+    // A cap of at most 128 takes tanh's short form over many rows of 16 bits: off
+    // by 2^-21 of the cap, what the longer one is of a score half as large, and at
+    // most 2^-14 of a weight.
     p.short_cap = p.cap > 0.0f && p.cap <= 128.0f && !p.slopes && a.q.dtype != DSIM_F32 && p.rows >= 128;
     p.max_blocks = blocks(p.n_tok, p.n_seq, p.group, p.rows);
     p.tree = a.tree;
