@@ -75,8 +75,10 @@ DSIM_API dsim_status dsim_kv_append_axes(const dsim_kv_cache *cache, int64_t n_t
  *   q, out: n_tok rows of n_q_heads heads of `dtype`: the cache's type, or
  *           DSIM_F16 / DSIM_BF16 with an e4m3 cache; out may be q (with its
  *           strides), it must not overlap otherwise
- *   scale:  in [-2^126, 2^126];   cap: 0 (none) or in [2^-60, 2^60]; with a
- *           cap or slopes the scores themselves have to stay in fp32's range
+ *   scale:  in [-2^126, 2^126];   cap: 0 (none) or in [2^-60, 2^60], and
+ *           |scale| / cap 0 or in [2^-126, 2^126]; with a cap or slopes the
+ *           scores themselves have to stay in fp32's range, and scale times
+ *           k_scale in the ranges of scale
  *   slopes: device array [n_q_heads] or NULL
  *   lse:    device array [n_tok][n_q_heads] or NULL
  *   status: device array [n_seq] or NULL: 0 or DSIM_ST_* bits.  BAD_POSITION:

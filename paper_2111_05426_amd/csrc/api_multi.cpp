@@ -24,6 +24,11 @@ static dsim_status check_queries(const dsim_kv_cache *c, const dsim_queries *q)
         return fail(DSIM_ERANGE, "n_tok must be >= 0 and n_tok * n_q_heads at most 2^31 - 256");
     if (!(std::fabs(q->scale) <= 0x1p126f)) return fail(DSIM_EINVAL, "scale must be in [-2^126, 2^126]");
     if (q->cap != 0.0f && !(q->cap >= 0x1p-60f && q->cap <= 0x1p60f)) return fail(DSIM_EINVAL, "cap must be 0 or in [2^-60, 2^60]");
+    // (a capped score is taken times their quotient: infinite it would make NaN of a
+    // score of 0, and 0 of every other where it has no bits left)
+    const float quotient = std::fabs(q->scale) / q->cap;
+    if (q->cap != 0.0f && q->scale != 0.0f && !(quotient >= 0x1p-126f && quotient <= 0x1p126f))
+        return fail(DSIM_EINVAL, "scale / cap must be 0 or in [2^-126, 2^126]");
     if (q->window < 0) return fail(DSIM_EINVAL, "window must be >= 0");
     if (c->n_seq == 0) return DSIM_OK;
     if (q->n_tok > 0) {
