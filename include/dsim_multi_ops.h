@@ -135,8 +135,10 @@ DSIM_API dsim_status dsim_prompt_attention(const dsim_kv_cache *cache, const dsi
  * position p = L + depth[t] and attends to the context's keys
  *   max(0, p + 1 - window (if window > 0))  <=  j  <  L
  * and to the nodes m whose bit m % 32 of word m / 32 of its row of the mask
- * is 1 (its ancestors and itself; the window does not cut them).  A node's
- * position is that of its key too.
+ * is 1 (its ancestors and itself; the window does not cut them: where a tree is
+ * as deep as the window, its caller clears the bits of ancestors that a
+ * token on its own would not attend to).  A node's position is that of its key
+ * too.
  *   mask:  device array [n_tok][mask_stride] of 32-bit words, mask_words
  *          that are read; a sequence of more than 32 * mask_words nodes sets
  *          DSIM_ST_BAD_POSITION
@@ -207,15 +209,17 @@ DSIM_API dsim_status dsim_kv_release(const dsim_page_pool *pool, int64_t n, cons
  *           looked at)
  *   status: device array [n]: 0 or
  *           DSIM_ST_BAD_SEQUENCE  dst[i] or src[i] outside the table, or
- *                                 src[i] among the call's dst
+ *                                 src[i] an empty row among the call's dst
  *           DSIM_ST_IN_USE        dst[i] holds pages, or an earlier fork of
- *                                 the call has it
+ *                                 the call has it, also one that is refused
  *           DSIM_ST_BAD_POSITION  seq_len[src[i]] outside what the row holds
  *           DSIM_ST_NO_PAGE       no page is left for it (nor for later ones
  *                                 that need one)
  *           and then nothing of the fork is done; with DSIM_ST_BAD_PAGE
  *           (entries of src outside the cache) it is, without those.
- * dst[i] < 0 is padding: nothing is done, and its status is 0.
+ * dst[i] < 0 is padding: nothing is done, and its status is 0.  A row that
+ * holds pages stays as it is though it is among the call's dst, and may be
+ * another fork's src.
  */
 DSIM_API dsim_status dsim_kv_fork(const dsim_kv_cache *layers, int32_t n_layers, const dsim_page_pool *pool,
                                   int32_t *seq_len, int64_t n, const int32_t *src, const int32_t *dst,
@@ -241,7 +245,7 @@ DSIM_API dsim_status dsim_kv_copy_pages(const dsim_kv_cache *layers, int32_t n_l
  *            be read, at most 2^30; n_keep is clamped to 0..keep_width
  *   status:  device array [n_seq] or NULL: 0, DSIM_ST_BAD_POSITION (entries
  *            that do not ascend, or places outside the block table: the
- *            list ends before them) or DSIM_ST_BAD_PAGE (a page of them
+ *            list ends before them) or DSIM_ST_BAD_PAGE (of those that move a page
  *            outside the cache: that place is left out)
  * The accepted path of a drafted tree moves so to the end of its context, and
  * a context from which tokens are dropped closes up.

@@ -135,7 +135,8 @@ dsim_status launch_compact(const Layers &l, const CompactArgs &args, hipStream_t
     a.div_mul = (uint32_t)((((uint64_t)1 << a.div_shift) + l.page_size - 1) / l.page_size);
     const int64_t columns = (int64_t)l.n_heads * l.chunks;
     const int block = a.keep_width > 64 ? 512 : 256;
-    // as many columns as leave enough ways for the list at once, 128 bytes at least
+    // as many columns as leave enough ways for the list at once, 128 bytes at least,
+    // shared out evenly (of 9 pieces of 16 bytes 5 and 4)
     int64_t per = (int64_t)block * rows_at_once(block) / (a.keep_width > 0 ? a.keep_width : 1);
     per = per < 8 ? 8 : per > block ? block : per;
     if (per > columns) per = columns;
