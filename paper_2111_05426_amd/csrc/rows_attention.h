@@ -26,9 +26,9 @@
 //
 // What bounds it, on MI355X (bf16, heads of 128; the product of 8,192 cubed
 // reaches 1,101 TFLOP/s here):
-//   8,192 tokens of one prompt, 32 / 8 heads: 817 us, 673 TFLOP/s of the formula's
-//     products, 1,010 of those that are made: the second is made twice, for
-//     weights of two numbers.
+//   8,192 tokens of one prompt, 32 / 8 heads: 797 to 856 us, 642 to 690 TFLOP/s of
+//     the formula's products, 963 to 1,035 of those that are made: the second is
+//     made twice, for weights of two numbers.
 //   16 chunks of 1 to 1,024 tokens behind 2,000, window 1,500, cap 50: 491 us, 410
 //     TFLOP/s; a capped score takes two more transcendental instructions.
 //   64 trees of 16 nodes over 1 to 4,096 tokens: 151 us, 3.7 TB/s of the cache,
@@ -57,8 +57,8 @@ constexpr int kJoin = 256;           // threads of the join
 constexpr int kPlan = 1024;          // threads of the plan
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // What a block of rows costs beside its tiles, in tiles.  (Chunks of prompts, a
-// long prompt, fp32 documents: 434, 598 and 155 us, with 4 438, 613 and 162, with
-// 1 426, 671 and 147.  Trees, blocks of 64 rows: 150 us, with 2 158, with 8 more.)
+// long prompt, fp32 documents: 489, 797 and 123 us, with 4 493, 815 and 130, with
+// 1 491, 840 and 118.  Trees, blocks of 64 rows: 150 us, with 2 158, with 8 more.)
 constexpr int extra(int rows) { return rows >= 128 ? 2 : 4; }
 constexpr int kMinTiles = 4;         // of a run at least: shorter ones only begin and end
 

@@ -8,11 +8,12 @@ namespace rows {
 
 // Rows of a block: about what the average sequence has (more are multiplied as
 // padding, fewer read the keys again).  us with the size taken and another: 8
-// rows a sequence, 32 9.6, 64 9.9; 60 rows, 64 8.7, 32 9.6, 128 9.1; 64 rows over
-// 64 contexts, 64 151, 32 278, 128 163; 384 rows over an e4m3 cache, 128 740, 256 846; 32
-// prompts of 1,200 rows, 128 102, 256 115; 64 of 2,200, 256 482, 128 540; one of 32,768,
-// 256 632, 128 665.  fp32 has no registers for 256, and with
-// blocks of 64 documents took 199 for 158.
+// rows a sequence, 32 9.6, 64 9.9; 60 rows, 64 9.0, 32 9.6, 128 9.7; 64 rows over
+// 64 contexts, 64 153, 32 278, 128 178; 384 rows over an e4m3 cache, 128 865, 256 979; 32
+// prompts of 1,200 rows, 128 116, 256 125; 64 of 2,200, 256 523, 128 575; one of 32,768,
+// 256 797, 128 856.  (Against it: drafts of 32 rows over 64 and 256 contexts of some
+// hundred tokens, heads of 128, 32 42 and 169, 128 36 and 126.)  fp32 has no registers
+// for 256, and with blocks of 64 documents took 199 for 158.
 static int rows_of(int64_t n_tok, int32_t n_seq, int32_t group, int32_t head_dim, bool f32)
 {
     const int64_t average = n_seq > 0 ? (n_tok * group + n_seq - 1) / n_seq : 0;
@@ -100,7 +101,9 @@ dsim_status launch_rows(const RowsArgs &a, hipStream_t s)
     p.rows = rows_of(p.n_tok, p.n_seq, p.group, p.d, a.q.dtype == DSIM_F32);
     // A cap of at most 128 takes tanh's short form over many rows of 16 bits: off
     // by 2^-21 of the cap, what the longer one is of a score half as large, and at
-    // most 2^-14 of a weight.
+    // most 2^-14 of a weight.  Chunks of prompts 489 us, by the longer form 652; trees
+    // over e4m3 866 and 1,107; 64 trees of 16 nodes over 1 to 4,096 tokens would take
+    // 167 for 181, but few rows keep their scores' bits.
     p.short_cap = p.cap > 0.0f && p.cap <= 128.0f && !p.slopes && a.q.dtype != DSIM_F32 && p.rows >= 128;
     p.max_blocks = blocks(p.n_tok, p.n_seq, p.group, p.rows);
     p.tree = a.tree;
@@ -122,11 +125,13 @@ dsim_status launch_rows(const RowsArgs &a, hipStream_t s)
     divisor(p.page_size, p.page_mul, p.page_shift);
     divisor(p.group, p.group_mul, p.group_shift);
     // A workgroup a block, without plan and join, where no block is long and
-    // there are few: one request's prompt of 60 tokens 8.7 us, planned and joined
-    // 16.1, its drafts 9.6 and 17.1; 128 prompts of 10 to 100 tokens of 32 / 8 heads
-    // 59.6 and 71.6 (512 of them 296 and 269), 256 drafts over 10 to 500 keys of 12
-    // heads of 64 84.4 and 88.9, of 32 / 8 heads of 128 165.7 and 159.7.  Each finds
-    // its sequence among all, 64 at a time, so there are few of those too.
+    // there are few: one request's prompt of 60 tokens 9.0 us, planned and joined
+    // 16.4, its drafts 9.9 and 17.4; 128 prompts of 10 to 100 tokens of 32 / 8 heads
+    // 75 and 83 (512 of them 305 and 272), 256 drafts over 10 to 500 keys of 12
+    // heads of 64 94.6 and 100, of 32 / 8 heads of 128 169 and 163.  Each finds
+    // its sequence among all, 64 at a time, so there are few of those too.  (By the
+    // table's room, for lengths are on the device: under a table of more places a
+    // short request is planned.)
     const int64_t most = (int64_t)p.table_width * p.page_size;
     p.direct = most <= 1024 && p.n_seq <= 256 && p.max_blocks * p.n_heads <= 8 * kMaxGrid;
     if (a.q.dtype == DSIM_F32) return rows::launch_f32(p, s);
